@@ -366,6 +366,111 @@ rs_status rs_dense_attn_prefill(const rs_qkv *qkv, const rs_unit *units, int32_t
                                 void *o, int64_t so_h, int64_t so_t, float *lse, void *ws,
                                 size_t ws_bytes, rs_stream stream);
 
+/* ---- key/value cache of a batch of sequences (decoding) ---------------------------------
+ * Rows (tokens) of `nseq` sequences in pages.  Row j of sequence b and key/value head g is, for K
+ * (V alike), d contiguous elements at
+ *   k + page_id * sk_p + g * sk_h + (j % page) * sk_t,
+ *   page_id = table[b * max_pages + j / page], or b * max_pages + j / page without a table.
+ * A prefill writes the same rows: with head-major pages a prompt's K and V of rs_qkv are pages.
+ *  - One sequence holds at most cap = max_pages * page rows, cap <= 262144.  page is a multiple
+ *    of 64, or any size where max_pages == 1.  Pages of different sequences are distinct.
+ *  - len (device) counts the rows held; it is read clamped to [0, cap].  Rows behind it are neither
+ *    read nor, but by rs_cache_append, written.
+ *  - A table entry outside [0, npages) names no page: rows there are not written, and no query sees
+ *    them.
+ *  - kmean (optional): bf16 [npages][hkv][ceil(page / 64)][d], the mean of the K rows of each complete
+ *    block of 64 rows (sum in fp64, rounded once).  rs_cache_commit and rs_cache_evict keep it.
+ *  - acc, pos (optional): [nseq][hkv][cap], the accumulated attention weight and the position in the
+ *    sequence of every row; seen (optional, device [nseq]): tokens that a sequence has had.  An
+ *    evicted cache holds fewer rows than that, in an order of its own, each head its own rows.
+ * Strides are in elements, 16-byte multiples.  dtype is that of K, V and of the queries; fp32 values
+ * enter the products as two bf16 parts each, hi = bf16(x) and lo = bf16(x - hi), without lo.lo
+ * (within about 2^-16 of sum_d |q_d k_d| x scale of the exact logit). */
+typedef struct rs_cache {
+  void *k, *v;               /* device */
+  int32_t dtype, nseq, hkv, d;
+  int32_t page, npages, max_pages, _pad0;
+  const int32_t *table;      /* device [nseq][max_pages], or NULL */
+  int32_t *len;              /* device [nseq] */
+  int64_t sk_p, sk_h, sk_t;  /* element strides of k (page, head, row) */
+  int64_t sv_p, sv_h, sv_t;
+  void *kmean;               /* device, or NULL */
+  float *acc;                /* device, or NULL */
+  int32_t *pos;              /* device, or NULL */
+  int32_t *seen;             /* device, or NULL */
+} rs_cache;
+
+/* New (drafted) tokens of the batch, one row each: row r of sequence b is r = start[b] + i for
+ * i < t_b = start[b + 1] - start[b], read clamped so that 0 <= t_b <= max_rows and the rows lie in
+ * [0, nrows).  Its key and value are the cache's row len[b] + i (rs_cache_append writes them).  It
+ * sees the sequence's len[b] cached rows and the drafted rows i' whose bit (word i' / 32, bit i' % 32)
+ * is set in its mask row; without a mask the rows i' <= i.  One row per sequence without a mask is a
+ * plain decode step, a chain of rows a chunk, and a mask of every row's ancestors a tree.  Rows that
+ * belong to no sequence are neither read nor written. */
+typedef struct rs_draft {
+  const void *q;             /* device [nrows][hq][d] with element strides (sq_t, sq_h) */
+  int32_t hq, nrows, max_rows, nwords;  /* max_rows <= 256; nwords: words per mask row, 32 nwords >= max_rows */
+  int64_t sq_t, sq_h;
+  const int32_t *start;      /* device [nseq + 1]; NULL: sequence b's rows are [b * max_rows, (b + 1) * max_rows) */
+  const uint32_t *mask;      /* device [nrows][nwords], or NULL */
+  float scale;               /* logit scale; 0 => 1/sqrt(d) */
+  int32_t _pad0;
+} rs_draft;
+
+/* Writes new rows into the cache: k_new, v_new (device [nrows][hkv][d], the cache's dtype, element
+ * strides (token, head)), row start[b] + i to row len[b] + i of sequence b (rows behind cap are left
+ * out).  len stays: the rows are drafts until rs_cache_commit.  max_rows bounds t_b (any size up to
+ * cap here).  acc of the written rows, if any, becomes 0. */
+rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *v_new, int64_t sk_t, int64_t sk_h,
+                          int64_t sv_t, int64_t sv_h, const int32_t *start, int32_t nrows, int32_t max_rows,
+                          rs_stream stream);
+/* Keeps naccept[b] (device; clamped to [0, max_new]) of the rows behind len[b]: row len + i takes the
+ * row len + path[b * max_new + i] (K, V and acc) for i < naccept[b]; path must ascend (entries outside
+ * [i, max_new) are read as i); NULL: the first ones.  With a path max_new <= 256.  Then writes pos =
+ * seen + i, the block means that the rows complete, and adds naccept to len (at most cap) and seen. */
+rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const int32_t *path, int32_t max_new,
+                          rs_stream stream);
+
+/* Attention of the drafted rows over the cache: O (bf16 [nrows][hq][d], element strides so_t, so_h)
+ * and, if lse != NULL, lse[head * nrows + row] = log of the sum of the exp of its logits (-inf, and O = 0,
+ * for a row that sees nothing).  Long sequences are split over workgroups and joined; the workspace
+ * holds the pieces. */
+size_t rs_draft_attn_workspace_size(const rs_cache *cache, const rs_draft *draft);
+rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, int64_t so_t, int64_t so_h, float *lse,
+                        void *ws, size_t ws_bytes, rs_stream stream);
+
+/* The same over blocks that each row selects.  Of the F = floor(len / 64) complete blocks a row and
+ * key/value head reads min(nsel, F): the first nsink, the last nlocal (nsink + nlocal <= nsel), and
+ * those of the largest score
+ *   score(c) = max over the head's query heads of q . kmean_c
+ * (exact: products of bf16 means and q are summed in fp64; equal scores, the lower block first; NaN
+ * counts as minus infinity), and always the rows behind the last complete block.  blocks (optional,
+ * device int32 [nrows][hkv][nsel]): the selected blocks ascending, -1 behind them.  1 <= nsel <= 4096. */
+size_t rs_select_attn_workspace_size(const rs_cache *cache, const rs_draft *draft, int32_t nsel);
+rs_status rs_select_attn(const rs_cache *cache, const rs_draft *draft, int32_t nsel, int32_t nsink, int32_t nlocal,
+                         void *o, int64_t so_t, int64_t so_h, float *lse, int32_t *blocks, void *ws, size_t ws_bytes,
+                         rs_stream stream);
+
+/* Attention weight that the drafted rows put on each cached row, summed over the rows and the query
+ * heads of each key/value head:
+ *   acc_out[b][g][j] = acc_in[b][g][j] + sum over rows i and heads h of g of row_w[i] exp(l_hij - lse_hi)
+ * for j < len[b] + t_b that row i sees; other entries are left as they are.  lse: as rs_draft_attn
+ * wrote it; row_w (device [nrows], NULL: 1): 0 for drafts that were not accepted; acc_in (NULL: 0) may
+ * be acc_out.  Both are [nseq][hkv][cap] as rs_cache.acc. */
+rs_status rs_attn_weights(const rs_cache *cache, const rs_draft *draft, const float *lse, const float *row_w,
+                          const float *acc_in, float *acc_out, rs_stream stream);
+
+/* Leaves `budget` rows of every sequence that holds more: per key/value head those with pos < nsink or
+ * pos >= seen - nrecent (the lower ones, should there be more), then those of the largest acc (total order of the index construction: score
+ * descending, -0.0 after +0.0, row ascending).  The kept rows behind the budget move to the places that
+ * evicted rows leave before it, the i-th to the i-th, with their acc and pos; all other rows stay where
+ * they are.  So a step that evicts one row moves one row, whatever the length.  len becomes budget and
+ * the means of the blocks that received rows are rewritten.  Needs acc, pos and seen; nsink + nrecent <=
+ * budget. */
+size_t rs_cache_evict_workspace_size(const rs_cache *cache, int32_t budget);
+rs_status rs_cache_evict(const rs_cache *cache, int32_t budget, int32_t nsink, int32_t nrecent, void *ws,
+                         size_t ws_bytes, rs_stream stream);
+
 /* Message describing the last failure of the calling thread ("" if none). */
 const char *rs_last_error(void);
 /* Library version string. */

@@ -24,6 +24,9 @@ EXPORTS = ["rs_unit_table_size", "rs_unit_table_init",
            "rs_sparse_attn_prefill", "rs_dense_attn_prefill", "rs_error_predict",
            "rs_route_layer_device_workspace_size", "rs_route_layer_device", "rs_route_layer_device_noalloc",
            "rs_routed_attn_workspace_size", "rs_routed_attn_prefill", "rs_vt_bytes", "rs_transpose_v",
+           "rs_cache_append", "rs_cache_commit", "rs_draft_attn_workspace_size", "rs_draft_attn",
+           "rs_select_attn_workspace_size", "rs_select_attn", "rs_attn_weights",
+           "rs_cache_evict_workspace_size", "rs_cache_evict",
            "rs_last_error", "rs_version"]
 
 P = C.c_void_p
@@ -100,6 +103,18 @@ class RsRouteDevOut(C.Structure):
                 ("risk", P), ("m_lower", P), ("status", P), ("totals", P)]
 
 
+class RsCache(C.Structure):
+    _fields_ = [("k", P), ("v", P), ("dtype", I32), ("nseq", I32), ("hkv", I32), ("d", I32), ("page", I32),
+                ("npages", I32), ("max_pages", I32), ("_pad0", I32), ("table", P), ("len", P), ("sk_p", I64),
+                ("sk_h", I64), ("sk_t", I64), ("sv_p", I64), ("sv_h", I64), ("sv_t", I64), ("kmean", P),
+                ("acc", P), ("pos", P), ("seen", P)]
+
+
+class RsDraft(C.Structure):
+    _fields_ = [("q", P), ("hq", I32), ("nrows", I32), ("max_rows", I32), ("nwords", I32), ("sq_t", I64),
+                ("sq_h", I64), ("start", P), ("mask", P), ("scale", C.c_float), ("_pad0", I32)]
+
+
 _lib = None
 
 
@@ -114,7 +129,8 @@ def lib():
         L.rs_version.restype = C.c_char_p
         for name in ("rs_unit_table_size", "rs_probe_workspace_size", "rs_build_indices_workspace_size",
                      "rs_attn_workspace_size", "rs_route_layer_device_workspace_size",
-                     "rs_routed_attn_workspace_size", "rs_vt_bytes"):
+                     "rs_routed_attn_workspace_size", "rs_vt_bytes", "rs_draft_attn_workspace_size",
+                     "rs_select_attn_workspace_size", "rs_cache_evict_workspace_size"):
             getattr(L, name).restype = C.c_size_t
         L.rs_unit_table_size.argtypes = [C.POINTER(RsQkv), C.POINTER(RsUnit), I32, C.POINTER(RsProbeCfg)]
         L.rs_unit_table_init.argtypes = [C.POINTER(RsQkv), C.POINTER(RsUnit), I32, C.POINTER(RsProbeCfg), P,
@@ -145,6 +161,19 @@ def lib():
         L.rs_routed_attn_prefill.argtypes = [C.POINTER(RsQkv), C.POINTER(RsUnit), I32, C.POINTER(RsCandidate),
                                              I32, C.POINTER(RsIndexSet), P, P, I64, I64, P, P, C.c_size_t,
                                              C.POINTER(P), P]
+        ca, dr = C.POINTER(RsCache), C.POINTER(RsDraft)
+        L.rs_cache_append.argtypes = [ca, P, P, I64, I64, I64, I64, P, I32, I32, P]
+        L.rs_cache_commit.argtypes = [ca, P, P, I32, P]
+        L.rs_draft_attn_workspace_size.argtypes = [ca, dr]
+        L.rs_draft_attn.argtypes = [ca, dr, P, I64, I64, P, P, C.c_size_t, P]
+        L.rs_select_attn_workspace_size.argtypes = [ca, dr, I32]
+        L.rs_select_attn.argtypes = [ca, dr, I32, I32, I32, P, I64, I64, P, P, P, C.c_size_t, P]
+        L.rs_attn_weights.argtypes = [ca, dr, P, P, P, P, P]
+        L.rs_cache_evict_workspace_size.argtypes = [ca, I32]
+        L.rs_cache_evict.argtypes = [ca, I32, I32, I32, P, C.c_size_t, P]
+        for name in ("rs_cache_append", "rs_cache_commit", "rs_draft_attn", "rs_select_attn", "rs_attn_weights",
+                     "rs_cache_evict"):
+            getattr(L, name).restype = C.c_int
         for name in ("rs_unit_table_init", "rs_probe", "rs_build_indices", "rs_route_layer", "rs_sparse_attn_prefill",
                      "rs_dense_attn_prefill", "rs_error_predict", "rs_route_layer_device",
                      "rs_route_layer_device_noalloc",
@@ -479,3 +508,162 @@ def rs_routed_attn_prefill(qkv, units, nunits, grid, ncand, idx, choice, o, lse,
         C.byref(qkv), units, nunits, grid, ncand, C.byref(idx.c) if idx is not None else None, _ptr(choice),
         _ptr(o), o.stride(0), o.stride(1), _ptr(lse), _ptr(ws), ws.numel() if ws is not None else 0, ev,
         _stream(stream)))
+
+
+# ---- decoding over a key/value cache ------------------------------------------------------
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(fn, device, stream, args):
+    """fn(*args, stream) on `stream` (default: the current stream of `device`), launched with `device` current."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return _check(fn(*args, _stream(stream)))
+    with torch.cuda.device(device):
+        return _check(fn(*args, _stream(stream)))
+
+
+class KvCache:
+    """Descriptor (rs_cache) over caller-owned device tensors:
+    k, v: [npages, hkv, page, d] (bf16 or float32, any strides, last dim contiguous); length: int32 [nseq];
+    table: int32 [nseq, max_pages] (None: npages / nseq pages per sequence, in order); kmean: bf16
+    [npages, hkv, ceil(page / 64), d]; acc: float32, pos: int32 [nseq, hkv, max_pages * page]; seen: int32 [nseq].
+    The tensors are kept alive and the calls below read and write them."""
+
+    def __init__(self, k, v, length, table=None, kmean=None, acc=None, pos=None, seen=None):
+        import torch
+        _want(k.dim() == 4 and v.shape == k.shape, "k and v must be [npages, hkv, page, d]")
+        _want(k.dtype in (torch.bfloat16, torch.float32) and v.dtype == k.dtype, "k and v must both be bf16 or float32")
+        _want(k.stride(3) == 1 and v.stride(3) == 1, "the last dimension of k and v must be contiguous")
+        npages, hkv, page, d = k.shape
+        nseq = length.numel()
+        _want(nseq > 0 and (table is not None or npages % nseq == 0), "without a table every sequence has the same number of pages")
+        max_pages = table.shape[1] if table is not None else npages // nseq
+        cap = max_pages * page
+        i32 = torch.int32
+        for name, t, dt, shape in (("length", length, i32, (nseq,)), ("table", table, i32, (nseq, max_pages)),
+                                   ("kmean", kmean, torch.bfloat16, (npages, hkv, (page + 63) // 64, d)),
+                                   ("acc", acc, torch.float32, (nseq, hkv, cap)), ("pos", pos, i32, (nseq, hkv, cap)),
+                                   ("seen", seen, i32, (nseq,))):
+            _want(t is None or (t.dtype == dt and tuple(t.shape) == shape and t.is_contiguous() and t.device == k.device),
+                  f"{name} must be a contiguous {dt} tensor of shape {shape} on the device of k")
+        _want(v.device == k.device, "v must be on the device of k")
+        self.k, self.v, self.length, self.table, self.kmean = k, v, length, table, kmean
+        self.acc, self.pos, self.seen = acc, pos, seen
+        self.nseq, self.hkv, self.page, self.d, self.cap, self.device, self.dtype = nseq, hkv, page, d, cap, k.device, k.dtype
+        p = lambda t: None if t is None else t.data_ptr()
+        self.c = RsCache(k=p(k), v=p(v), dtype=RS_BF16 if k.dtype == torch.bfloat16 else RS_F32, nseq=nseq, hkv=hkv, d=d,
+                         page=page, npages=npages, max_pages=max_pages, table=p(table), len=p(length),
+                         sk_p=k.stride(0), sk_h=k.stride(1), sk_t=k.stride(2), sv_p=v.stride(0), sv_h=v.stride(1),
+                         sv_t=v.stride(2), kmean=p(kmean), acc=p(acc), pos=p(pos), seen=p(seen))
+        self.ref = C.byref(self.c)
+
+
+class Draft:
+    """Descriptor (rs_draft) of new rows: q: [nrows, hq, d] (last dim contiguous); start: int32 [nseq + 1] (None:
+    max_rows rows per sequence); mask: int32 [nrows, nwords], bit i of a row: it sees drafted row i."""
+
+    def __init__(self, q, max_rows=1, start=None, mask=None, scale=0.0):
+        import torch
+        _want(q.dim() == 3 and (q.stride(2) == 1 or not q.numel()), "q must be [nrows, hq, d] with a contiguous last dimension")
+        for name, t in (("start", start), ("mask", mask)):
+            _want(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == q.device),
+                  f"{name} must be a contiguous int32 tensor on the device of q")
+        _want(mask is None or (mask.dim() == 2 and mask.shape[0] == q.shape[0]), "mask must be [nrows, nwords]")
+        self.q, self.start, self.mask = q, start, mask
+        self.nrows, self.hq, self.d, self.device = q.shape[0], q.shape[1], q.shape[2], q.device
+        self.c = RsDraft(q=q.data_ptr(), hq=q.shape[1], nrows=q.shape[0], max_rows=max_rows,
+                         nwords=mask.shape[1] if mask is not None else 0, sq_t=q.stride(0), sq_h=q.stride(1),
+                         start=start.data_ptr() if start is not None else None,
+                         mask=mask.data_ptr() if mask is not None else None, scale=scale)
+        self.ref = C.byref(self.c)
+
+
+def _check_pair(cache, draft):
+    _want(draft.q.dtype == cache.dtype and draft.d == cache.d and draft.device == cache.device,
+          "q must have the dtype, head dimension and device of the cache")
+    _want(draft.start is None or draft.start.numel() == cache.nseq + 1, "start must have nseq + 1 entries")
+
+
+def _check_rows_out(cache, draft, o, lse):
+    import torch
+    _check_pair(cache, draft)
+    _want(o.dtype == torch.bfloat16 and o.shape == draft.q.shape and (o.stride(2) == 1 or not o.numel()) and o.device == cache.device,
+          "o must be bf16 [nrows, hq, d] with a contiguous last dimension")
+    _want(lse is None or (lse.dtype == torch.float32 and lse.shape == (draft.hq, draft.nrows) and lse.is_contiguous()
+                          and lse.device == cache.device), "lse must be contiguous float32 [hq, nrows]")
+
+
+def rs_cache_append(cache, k_new, v_new, max_rows=1, start=None, stream=None):
+    """k_new, v_new: [nrows, hkv, d] of the cache's dtype (last dim contiguous)."""
+    import torch
+    _want(k_new.dim() == 3 and k_new.shape == v_new.shape and tuple(k_new.shape[1:]) == (cache.hkv, cache.d)
+          and k_new.dtype == cache.dtype == v_new.dtype and (k_new.stride(2) == v_new.stride(2) == 1 or not k_new.numel())
+          and k_new.device == cache.device == v_new.device, "k_new and v_new must be [nrows, hkv, d] like the cache")
+    _want(start is None or (start.dtype == torch.int32 and start.numel() == cache.nseq + 1 and start.is_contiguous()
+                            and start.device == cache.device), "start must be int32 with nseq + 1 entries")
+    return _on_device(lib().rs_cache_append, cache.device, stream,
+                      (cache.ref, _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), v_new.stride(0),
+                       v_new.stride(1), _ptr(start), k_new.shape[0], max_rows))
+
+
+def rs_cache_commit(cache, naccept, max_new, path=None, stream=None):
+    """naccept: int32 [nseq]; path: int32 [nseq, max_new] or None."""
+    import torch
+    for name, t, shape in (("naccept", naccept, (cache.nseq,)), ("path", path, (cache.nseq, max_new))):
+        _want(t is None or (t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == cache.device),
+              f"{name} must be contiguous int32 {shape}")
+    return _on_device(lib().rs_cache_commit, cache.device, stream, (cache.ref, _ptr(naccept), _ptr(path), max_new))
+
+
+def rs_draft_attn_workspace_size(cache, draft):
+    return lib().rs_draft_attn_workspace_size(cache.ref, draft.ref)
+
+
+def rs_draft_attn(cache, draft, o, lse, ws, stream=None):
+    """o: bf16 [nrows, hq, d]; lse: float32 [hq, nrows] or None."""
+    _check_rows_out(cache, draft, o, lse)
+    return _on_device(lib().rs_draft_attn, cache.device, stream,
+                      (cache.ref, draft.ref, _ptr(o), o.stride(0), o.stride(1), _ptr(lse), _ptr(ws),
+                       ws.numel() if ws is not None else 0))
+
+
+def rs_select_attn_workspace_size(cache, draft, nsel):
+    return lib().rs_select_attn_workspace_size(cache.ref, draft.ref, nsel)
+
+
+def rs_select_attn(cache, draft, nsel, nsink, nlocal, o, lse, ws, blocks=None, stream=None):
+    """As rs_draft_attn over nsel selected blocks per row and key/value head; blocks: int32 [nrows, hkv, nsel] or None."""
+    import torch
+    _check_rows_out(cache, draft, o, lse)
+    _want(blocks is None or (blocks.dtype == torch.int32 and tuple(blocks.shape) == (draft.nrows, cache.hkv, nsel)
+                             and blocks.is_contiguous() and blocks.device == cache.device),
+          "blocks must be contiguous int32 [nrows, hkv, nsel]")
+    return _on_device(lib().rs_select_attn, cache.device, stream,
+                      (cache.ref, draft.ref, nsel, nsink, nlocal, _ptr(o), o.stride(0), o.stride(1), _ptr(lse),
+                       _ptr(blocks), _ptr(ws), ws.numel() if ws is not None else 0))
+
+
+def rs_attn_weights(cache, draft, lse, acc_in, acc_out, row_w=None, stream=None):
+    """lse: float32 [hq, nrows]; row_w: float32 [nrows] or None; acc_in (or None), acc_out: float32 [nseq, hkv, cap]."""
+    import torch
+    _check_pair(cache, draft)
+    for name, t, shape in (("lse", lse, (draft.hq, draft.nrows)), ("row_w", row_w, (draft.nrows,)),
+                           ("acc_in", acc_in, (cache.nseq, cache.hkv, cache.cap)),
+                           ("acc_out", acc_out, (cache.nseq, cache.hkv, cache.cap))):
+        _want(t is None or (t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous()
+                            and t.device == cache.device), f"{name} must be contiguous float32 {shape}")
+    return _on_device(lib().rs_attn_weights, cache.device, stream,
+                      (cache.ref, draft.ref, _ptr(lse), _ptr(row_w), _ptr(acc_in), _ptr(acc_out)))
+
+
+def rs_cache_evict_workspace_size(cache, budget):
+    return lib().rs_cache_evict_workspace_size(cache.ref, budget)
+
+
+def rs_cache_evict(cache, budget, nsink, nrecent, ws, stream=None):
+    return _on_device(lib().rs_cache_evict, cache.device, stream,
+                      (cache.ref, budget, nsink, nrecent, _ptr(ws), ws.numel() if ws is not None else 0))

@@ -22,10 +22,10 @@ LIB = os.path.join(HERE, "librs.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
-HIP_SOURCES = ["attn.hip", "probe.hip", "topk.hip", "route_dev.hip"]
+HIP_SOURCES = ["attn.hip", "probe.hip", "topk.hip", "route_dev.hip", "decode.hip", "cache.hip"]
 # sources whose fp64 operation order is part of their definition
 NO_CONTRACT = {"route_dev.hip"}
-HOST_HIP_SOURCES = ["api.cpp"]
+HOST_HIP_SOURCES = ["api.cpp", "cache_api.cpp"]
 PLAIN_SOURCES = ["route.cpp"]
 
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",

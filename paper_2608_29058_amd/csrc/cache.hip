@@ -1,0 +1,392 @@
+// The key/value cache between the attention calls: new rows in, accepted rows kept, rows of least
+// accumulated weight out.  All of it is copying: what bounds these kernels is memory and, for the
+// short calls, the launch itself, so each call is one launch where its parts allow that.
+#include "common.h"
+#include "cache.h"
+
+namespace rs {
+
+namespace {
+
+// ---- append --------------------------------------------------------------------------------
+// A workgroup writes up to kAppendRows rows of one sequence, all heads, in pieces of 16 bytes; K and V of
+// a piece by the same thread, so that both loads are in flight before either store.
+constexpr int kAppendRows = 16;
+
+__global__ __launch_bounds__(256) void append_kernel(CacheView c, const char *kn, const char *vn, int64_t skt, int64_t skh,
+                                                     int64_t svt, int64_t svh, const int32_t *start, int nrows,
+                                                     int max_rows, int lp) {  // 1 << lp pieces per row
+  const int b = blockIdx.y, r0 = blockIdx.x * kAppendRows;
+  const RowRange rr = new_rows(start, b, nrows, max_rows);
+  const int len = cache_len(c, b);
+  const int most = rr.count < c.cap - len ? rr.count : c.cap - len;
+  const int rows = most - r0 < kAppendRows ? most - r0 : kAppendRows;
+  if (rows <= 0) return;
+  const int per_row = c.hkv << lp, total = rows * per_row;
+  for (int x = threadIdx.x; x < total; x += 256) {
+    const int i = x / per_row, y = x - i * per_row, g = y >> lp, o = (y & ((1 << lp) - 1)) * 16;
+    const int j = len + r0 + i, p = page_of(c, j), id = page_id(c, b, p);
+    if (id < 0) continue;
+    const int64_t row = rr.first + r0 + i;
+    const u32x4 kk = *(const u32x4 *)(kn + row * skt + g * skh + o), vv = *(const u32x4 *)(vn + row * svt + g * svh + o);
+    *(u32x4 *)(c.k + k_offset(c, id, p, j, g) + o) = kk;
+    *(u32x4 *)(c.v + v_offset(c, id, p, j, g) + o) = vv;
+    if (c.acc && o == 0) c.acc[((int64_t)b * c.hkv + g) * c.cap + j] = 0.f;
+  }
+}
+
+// ---- block means ---------------------------------------------------------------------------
+// Mean of the 64 K rows of block blk, by one wave: lane l sums rows l / (D / 8), ... of its 8 dimensions in
+// fp64 (bf16 sums of 64 rows are exact there, so no order shows), the lanes of equal dimensions add up, and
+// the mean is rounded to bf16 once: it is a score's factor, and 8 bits of it rank blocks as well as 24.
+template <typename T, int D>
+__device__ void block_mean(const CacheView &c, int b, int g, int blk, int lane) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes per row, rows per step
+  const int p = page_of(c, blk * 64), id = page_id(c, b, p);
+  if (id < 0) return;
+  const char *base = c.k + k_offset(c, id, p, blk * 64, g);
+  const int dl = lane % LPR, r0 = lane / LPR;
+  double s[8] = {};
+  for (int r = r0; r < 64; r += RPI) {
+    const T *x = (const T *)(base + r * c.sk_t) + dl * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += (double)(float)x[e];
+  }
+#pragma unroll
+  for (int m = LPR; m < 64; m <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += __shfl_xor(s[e], m);
+  if (r0 == 0) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2((float)(s[2 * e] * 0.015625), (float)(s[2 * e + 1] * 0.015625));
+    *(u32x4 *)((bf16 *)c.kmean + mean_offset(c, id, p, blk, g, D) + dl * 8) = w;
+  }
+}
+
+// ---- commit --------------------------------------------------------------------------------
+// Few rows: one workgroup per sequence moves the rows of the path, then writes positions, means and the
+// new length, in one launch.  The path ascends, so row i comes from a row at or behind it: what a step
+// reads before its barrier lies behind everything that earlier steps wrote, and its own writes follow the
+// barrier.
+constexpr int kCommitThreads = 1024, kCommitPieces = 4;
+
+template <typename T, int D>
+__global__ __launch_bounds__(kCommitThreads) void commit_kernel(CacheView c, const int32_t *naccept, const int32_t *path,
+                                                                int max_new) {
+  __shared__ int sp[kMaxDraft];
+  constexpr int NP = D * (int)sizeof(T) / 16;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int len = cache_len(c, b);
+  int na = clampi(naccept[b], 0, max_new);
+  na = na < c.cap - len ? na : c.cap - len;
+  const int seen = c.seen ? c.seen[b] : 0;
+  if (path) {
+    for (int i = tid; i < na; i += kCommitThreads) {
+      int x = path[(int64_t)b * max_new + i];
+      if (x < i || x >= max_new || len + x >= c.cap) x = i;
+      sp[i] = x;
+    }
+    __syncthreads();
+    const int per_row = c.hkv * NP, total = na * per_row;  // a piece: 16 bytes of K and the same of V
+    for (int x0 = 0; x0 < total; x0 += kCommitThreads * kCommitPieces) {
+      u32x4 kk[kCommitPieces], vv[kCommitPieces];
+      float a[kCommitPieces];
+      int64_t ko[kCommitPieces], vo[kCommitPieces], ao[kCommitPieces];
+#pragma unroll
+      for (int u = 0; u < kCommitPieces; ++u) {
+        const int x = x0 + u * kCommitThreads + tid;
+        ko[u] = -1;
+        if (x >= total) continue;
+        const int i = x / per_row, y = x - i * per_row, g = y / NP, o = (y % NP) * 16;
+        if (sp[i] == i) continue;
+        const int js = len + sp[i], jd = len + i, ps = page_of(c, js), pd = page_of(c, jd);
+        const int is = page_id(c, b, ps), id = page_id(c, b, pd);
+        if (is < 0 || id < 0) continue;
+        kk[u] = *(const u32x4 *)(c.k + k_offset(c, is, ps, js, g) + o);
+        vv[u] = *(const u32x4 *)(c.v + v_offset(c, is, ps, js, g) + o);
+        ko[u] = k_offset(c, id, pd, jd, g) + o;
+        vo[u] = v_offset(c, id, pd, jd, g) + o;
+        ao[u] = -1;
+        if (c.acc && o == 0) {
+          const int64_t h = ((int64_t)b * c.hkv + g) * c.cap;
+          a[u] = c.acc[h + js];
+          ao[u] = h + jd;
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kCommitPieces; ++u)
+        if (ko[u] >= 0) {
+          *(u32x4 *)(c.k + ko[u]) = kk[u];
+          *(u32x4 *)(c.v + vo[u]) = vv[u];
+          if (ao[u] >= 0) c.acc[ao[u]] = a[u];
+        }
+      __syncthreads();
+    }
+  }
+  if (c.pos)
+    for (int x = tid; x < na * c.hkv; x += kCommitThreads) {
+      const int g = x / na, i = x - g * na;
+      c.pos[((int64_t)b * c.hkv + g) * c.cap + len + i] = seen + i;
+    }
+  if (c.kmean) {
+    const int b0 = len >> 6, nb = ((len + na) >> 6) - b0;
+    for (int x = tid >> 6; x < nb * c.hkv; x += kCommitThreads / 64) block_mean<T, D>(c, b, x / nb, b0 + x % nb, tid & 63);
+  }
+  // every wave of this workgroup has read len by now; no other workgroup reads this sequence's
+  __syncthreads();
+  if (tid == 0) {
+    c.len[b] = len + na;
+    if (c.seen) c.seen[b] = seen + na;
+  }
+}
+
+// Many rows (a prompt, a chunk): a wave per block of 64 rows and head; the lengths follow in a launch of
+// their own, since all workgroups of this one read them.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void commit_rows_kernel(CacheView c, const int32_t *naccept, int max_new) {
+  const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x & 63;
+  const int len = cache_len(c, b);
+  int na = clampi(naccept[b], 0, max_new);
+  na = na < c.cap - len ? na : c.cap - len;
+  const int blk = (len >> 6) + blockIdx.x * 4 + (threadIdx.x >> 6), j = blk * 64 + lane;
+  if (blk * 64 >= len + na) return;
+  if (c.pos && j >= len && j < len + na) c.pos[((int64_t)b * c.hkv + g) * c.cap + j] = (c.seen ? c.seen[b] : 0) + j - len;
+  if (c.kmean && blk * 64 + 64 <= len + na) block_mean<T, D>(c, b, g, blk, lane);
+}
+
+__global__ void commit_len_kernel(CacheView c, const int32_t *naccept, int max_new) {
+  const int b = blockIdx.x * 64 + threadIdx.x;
+  if (b >= c.nseq) return;
+  const int len = cache_len(c, b);
+  int na = clampi(naccept[b], 0, max_new);
+  na = na < c.cap - len ? na : c.cap - len;
+  c.len[b] = len + na;
+  if (c.seen) c.seen[b] += na;
+}
+
+// ---- eviction ------------------------------------------------------------------------------
+// Plan, one workgroup per sequence and head: the `budget` first rows of the order (firm rows, then acc
+// descending, then row ascending) are found by a radix selection over 32-bit keys with the counts in LDS,
+// the rows read again from cache in each pass.  The first digit has 12 bits: weights lie in a few
+// octaves, and with 8 bits nearly all of a wave's counts would go to the same word.  One more pass lists,
+// in row order, the places before the budget whose row goes and the rows behind it that stay.
+struct EvictPlan {
+  int32_t *count;  // [nseq * hkv] rows that move; -1: the sequence is not over its budget
+  int32_t *hole;   // [nseq * hkv][most]
+  int32_t *mover;  // [nseq * hkv][most]
+  int most;
+};
+
+constexpr int kPlanThreads = 1024;
+
+// Key of a row in the order of the selection: firm rows share the highest, which no finite weight has.
+__device__ __forceinline__ uint32_t evict_key(float a, int pos, int nsink, int firm_from) {
+  return pos < nsink || pos >= firm_from ? 0xffffffffu : float_key(a);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(CacheView c, int budget, int nsink, int nrecent, EvictPlan pl) {
+  constexpr int kBins = 4096, kPer = 8;  // bins of a pass at most; consecutive rows per thread and step of the last
+  __shared__ int hist[kBins], sw[kPlanThreads / 64], pick[3];
+  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
+  const int64_t item = (int64_t)b * c.hkv + g;
+  const int n = cache_len(c, b);
+  if (n <= budget) {
+    if (tid == 0) pl.count[item] = -1;
+    return;
+  }
+  const float *acc = c.acc + item * c.cap;
+  const int *pos = c.pos + item * c.cap;
+  const int seen = c.seen[b], firm_from = (seen > 0 ? seen : 0) - nrecent;
+  // the budget-th largest key: its digits found so far (those under `have`), how many rows share them,
+  // and how many of these still stay
+  uint32_t prefix = 0, have = 0;
+  int need = budget, equal = n, all;
+  for (int pass = 0; pass < 3 && need < equal; ++pass) {
+    const int bits = pass ? 10 : 12, sh = pass == 0 ? 20 : pass == 1 ? 10 : 0, bins = 1 << bits;
+    for (int x = tid; x < bins; x += kPlanThreads) hist[x] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += kPlanThreads) {
+      const uint32_t key = evict_key(acc[j], pos[j], nsink, firm_from);
+      if ((key & have) == prefix) atomicAdd(&hist[(key >> sh) & (bins - 1)], 1);
+    }
+    __syncthreads();
+    // thread t counts the t-th highest group of bins; the one where the count reaches `need` picks
+    const int per = bins / kPlanThreads, top = bins - 1 - tid * per;
+    int sum = 0;
+    for (int x = 0; x < per; ++x) sum += hist[top - x];
+    int before = block_scan<kPlanThreads>(sum, sw, &all);
+    if (before < need && before + sum >= need) {
+      int x = top;
+      while (before + hist[x] < need) before += hist[x--];
+      pick[0] = x;
+      pick[1] = need - before;
+      pick[2] = hist[x];
+    }
+    __syncthreads();
+    prefix |= (uint32_t)pick[0] << sh;
+    have |= (uint32_t)(bins - 1) << sh;
+    need = pick[1];
+    equal = pick[2];
+    __syncthreads();
+  }
+  // rows above `prefix` stay, and the first `need` of those that share it
+  const bool ties = need < equal;
+  int ranked = 0, holes = 0, movers = 0;
+  for (int j0 = 0; j0 < n; j0 += kPlanThreads * kPer) {
+    const int jt = j0 + tid * kPer;
+    uint32_t key[kPer];
+    int e = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      key[x] = jt + x < n ? evict_key(acc[jt + x], pos[jt + x], nsink, firm_from) & have : 0;
+      e += jt + x < n && key[x] == prefix;
+    }
+    int at = 0;
+    if (ties) {
+      at = ranked + block_scan<kPlanThreads>(e, sw, &all);
+      ranked += all;
+    }
+    uint32_t hole = 0, mover = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int j = jt + x;
+      const bool eq = key[x] == prefix;
+      const bool stay = j < n && (key[x] > prefix || (eq && (!ties || at < need)));
+      at += eq;
+      hole |= (uint32_t)(j < budget && !stay) << x;
+      mover |= (uint32_t)(j >= budget && stay) << x;
+    }
+    const int hm = block_scan<kPlanThreads>(__popc(hole) | (__popc(mover) << 16), sw, &all);  // at most 8192 of each in a step
+    int h = holes + (hm & 0xffff), m = movers + (hm >> 16);
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      if (hole >> x & 1) pl.hole[item * pl.most + h++] = jt + x;
+      if (mover >> x & 1) pl.mover[item * pl.most + m++] = jt + x;
+    }
+    holes += all & 0xffff;
+    movers += all >> 16;
+  }
+  if (tid == 0) pl.count[item] = movers;
+}
+
+// The planned moves: places before the budget receive rows behind it, so nothing is read that is written.
+// The lengths change here, where only the plan is read.
+constexpr int kMoveRows = 64;
+
+__global__ __launch_bounds__(256) void evict_move_kernel(CacheView c, int budget, EvictPlan pl, int lp) {
+  const int b = blockIdx.z, g = blockIdx.y;
+  const int64_t item = (int64_t)b * c.hkv + g;
+  const int count = pl.count[item];
+  if (count < 0) return;
+  if (blockIdx.x == 0 && g == 0 && threadIdx.x == 0) c.len[b] = budget;
+  const int i0 = blockIdx.x * kMoveRows;
+  const int rows = count - i0 < kMoveRows ? count - i0 : kMoveRows;
+  for (int x = threadIdx.x; x < rows << lp; x += 256) {
+    const int i = i0 + (x >> lp), o = (x & ((1 << lp) - 1)) * 16;
+    const int js = pl.mover[item * pl.most + i], jd = pl.hole[item * pl.most + i];
+    if (o == 0) {
+      c.acc[item * c.cap + jd] = c.acc[item * c.cap + js];
+      c.pos[item * c.cap + jd] = c.pos[item * c.cap + js];
+    }
+    const int ps = page_of(c, js), pd = page_of(c, jd), is = page_id(c, b, ps), id = page_id(c, b, pd);
+    if (is < 0 || id < 0) continue;
+    const u32x4 kk = *(const u32x4 *)(c.k + k_offset(c, is, ps, js, g) + o), vv = *(const u32x4 *)(c.v + v_offset(c, is, ps, js, g) + o);
+    *(u32x4 *)(c.k + k_offset(c, id, pd, jd, g) + o) = kk;
+    *(u32x4 *)(c.v + v_offset(c, id, pd, jd, g) + o) = vv;
+  }
+}
+
+// Means of the complete blocks that received rows, a wave each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void evict_means_kernel(CacheView c, int budget, EvictPlan pl) {
+  const int b = blockIdx.z, g = blockIdx.y, blk = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t item = (int64_t)b * c.hkv + g;
+  const int count = pl.count[item];
+  if (count < 0 || blk * 64 + 64 > budget) return;
+  const int *hole = pl.hole + item * pl.most;  // ascending: the first at or behind the block's first row
+  int lo = 0, hi = count;
+  while (lo < hi) {
+    const int m = (lo + hi) >> 1;
+    if (hole[m] < blk * 64)
+      lo = m + 1;
+    else
+      hi = m;
+  }
+  if (lo < count && hole[lo] < blk * 64 + 64) block_mean<T, D>(c, b, g, blk, threadIdx.x & 63);
+}
+
+EvictPlan plan_at(Arena &a, int64_t items, int budget, int cap) {
+  EvictPlan pl{};
+  pl.most = budget < cap - budget ? budget : cap - budget;
+  if (pl.most < 0) pl.most = 0;
+  pl.count = a.take<int32_t>((size_t)items);
+  pl.hole = a.take<int32_t>((size_t)items * pl.most);
+  pl.mover = a.take<int32_t>((size_t)items * pl.most);
+  return pl;
+}
+
+int log2i(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+template <typename F>
+void by_type(int dtype, int d, F f) {
+  if (dtype == RS_BF16)
+    d == 128 ? f(bf16{}, std::integral_constant<int, 128>{}) : f(bf16{}, std::integral_constant<int, 64>{});
+  else
+    d == 128 ? f(float{}, std::integral_constant<int, 128>{}) : f(float{}, std::integral_constant<int, 64>{});
+}
+
+}  // namespace
+
+rs_status append_launch(const CacheView &c, int dtype, int d, const void *kn, const void *vn, int64_t skt, int64_t skh,
+                        int64_t svt, int64_t svh, const int32_t *start, int nrows, int max_rows, hipStream_t st) {
+  const int e = dtype == RS_BF16 ? 2 : 4;
+  append_kernel<<<dim3((max_rows + kAppendRows - 1) / kAppendRows, c.nseq), 256, 0, st>>>(
+      c, (const char *)kn, (const char *)vn, skt * e, skh * e, svt * e, svh * e, start, nrows, max_rows, log2i(d * e / 16));
+  RS_HIP(hipGetLastError());
+  return RS_OK;
+}
+
+rs_status commit_launch(const CacheView &c, int dtype, int d, const int32_t *naccept, const int32_t *path, int max_new,
+                        hipStream_t st) {
+  by_type(dtype, d, [&](auto t, auto dd) {
+    using T = decltype(t);
+    constexpr int D = decltype(dd)::value;
+    if (max_new <= kMaxDraft) {
+      commit_kernel<T, D><<<c.nseq, kCommitThreads, 0, st>>>(c, naccept, path, max_new);
+      return;
+    }
+    if (c.pos || c.kmean)
+      commit_rows_kernel<T, D><<<dim3((max_new / 64 + 2 + 3) / 4, c.hkv, c.nseq), 256, 0, st>>>(c, naccept, max_new);
+    commit_len_kernel<<<(c.nseq + 63) / 64, 64, 0, st>>>(c, naccept, max_new);
+  });
+  RS_HIP(hipGetLastError());
+  return RS_OK;
+}
+
+size_t evict_ws_bytes(int64_t items, int budget, int cap) {
+  Arena a(nullptr, 0);
+  plan_at(a, items, budget, cap);
+  return a.off + 256;
+}
+
+rs_status evict_launch(const CacheView &c, int dtype, int d, int budget, int nsink, int nrecent, void *ws, size_t ws_bytes,
+                       hipStream_t st) {
+  if (budget >= c.cap) return RS_OK;  // no sequence can hold more
+  Arena a(ws, ws_bytes);
+  const EvictPlan pl = plan_at(a, (int64_t)c.nseq * c.hkv, budget, c.cap);
+  if (!ws || !a.ok())
+    return fail(RS_ERR_WORKSPACE, "eviction workspace too small: need " + std::to_string(evict_ws_bytes((int64_t)c.nseq * c.hkv, budget, c.cap)));
+  evict_plan_kernel<<<dim3(c.hkv, c.nseq), kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+  const int e = dtype == RS_BF16 ? 2 : 4;
+  evict_move_kernel<<<dim3((pl.most + kMoveRows - 1) / kMoveRows, c.hkv, c.nseq), 256, 0, st>>>(c, budget, pl, log2i(d * e / 16));
+  if (c.kmean && budget >= 64)
+    by_type(dtype, d, [&](auto t, auto dd) {
+      evict_means_kernel<decltype(t), decltype(dd)::value><<<dim3((budget / 64 + 3) / 4, c.hkv, c.nseq), 256, 0, st>>>(c, budget, pl);
+    });
+  RS_HIP(hipGetLastError());
+  return RS_OK;
+}
+
+}  // namespace rs

@@ -1,0 +1,1054 @@
+// Attention of new (drafted) rows over the key/value cache: all cached rows (rs_draft_attn), blocks that a
+// score selects (rs_select_attn), and the weight that each cached row receives (rs_attn_weights).
+//
+// For a row r of key/value head g (a query head of a new token) over its visible rows j:
+//   l_j = scale q_r . k_j,  p_j = exp(l_j - max l),  O = sum p_j v_j / sum p_j.
+// A decode step reads every cached row for at most a few rows r, so memory bounds it: 4 d bytes of K and V
+// per row and head against 4 d (hq / hkv) t flops.  The kernels therefore stream K and V from memory
+// straight into the registers that the matrix instructions read, without LDS and without barriers:
+//   S^T [32 rows x 16] = K Q^T: lane (m = lane % 16, h = lane / 16) holds row m and 8 dimensions of it per
+//     instruction (v_mfma_f32_16x16x32_bf16), which is 16 contiguous bytes of K;
+//   O^T [d x 16] += V^T P^T: the contraction runs over rows in the order 4h + 0..3, 16 + 4h + 0..3, the rows
+//     whose S the lane holds, so P needs no exchange of lanes; and the lane reads dimensions
+//     (d / 16) m ... of those 8 rows, a whole row per 16 lanes, whose transposition into the instructions'
+//     operands (dimension (d / 16) m + t of the t-th) stays inside the lane: one v_perm per two values.
+// Each wave takes every fourth tile of 32 rows with a running maximum and sum of its own and keeps the next
+// tile in flight; the four waves are joined once, through LDS, at the end.
+#include "common.h"
+#include "cache.h"
+
+namespace rs {
+
+namespace {
+
+constexpr int kTile = 32, kWaves = 4, kGroup = kTile * kWaves;  // rows per wave and step, per workgroup and step
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+
+// Values of lanes i, i ^ 16, i ^ 32 and i ^ 48 joined, in all four.
+template <typename F>
+__device__ __forceinline__ float join4(float x, F f) {
+  x = f(x, __shfl_xor(x, 16));
+  return f(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float max4(float x) { return join4(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float sum4(float x) { return join4(x, [](float a, float b) { return a + b; }); }
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x as hi + lo, both bf16 (8 + 8 bits of its 24)
+__device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
+  hi = pack_bf16x2(a, b);
+  lo = pack_bf16x2(a - __builtin_bit_cast(float, hi << 16), b - __builtin_bit_cast(float, hi & 0xffff0000u));
+}
+
+// 8 fp32 values (two 16-byte registers) as two bf16 operands
+__device__ __forceinline__ void split8(f32x4 a, f32x4 b, u32x4 &hi, u32x4 &lo) {
+  uint32_t h, l;
+  split2(a[0], a[1], h, l), hi[0] = h, lo[0] = l;
+  split2(a[2], a[3], h, l), hi[1] = h, lo[1] = l;
+  split2(b[0], b[1], h, l), hi[2] = h, lo[2] = l;
+  split2(b[2], b[3], h, l), hi[3] = h, lo[3] = l;
+}
+
+// Wave-uniform loads through the scalar cache of arrays that the kernel does not write.
+__device__ __forceinline__ int uload(const int32_t *p, int64_t i) {
+  typedef const __attribute__((address_space(4))) int32_t cint;
+  return ((cint *)p)[i];
+}
+
+// ---- one tile of K and V in registers --------------------------------------------------------
+// CH: 16-byte pieces of a lane per K row part of 32 dimensions (1 bf16, 2 fp32).
+template <bool F32, int D>
+struct Tile {
+  static constexpr int KC = D / 32, CH = F32 ? 2 : 1, DT = D / 16;  // DT: output tiles, dimensions per lane of V
+  static constexpr int VW = DT * (F32 ? 4 : 2) / 4;                 // words of V per lane and row
+  u32x4 k[2][KC][CH];
+  uint32_t v[8][VW];
+};
+
+// The rows of a tile: page and first row in it; rows behind `last` are read as the last (and masked).
+struct TileAt {
+  const char *k, *v;
+  int last;   // last row of the tile that may be read, 0 .. 31
+  bool ok;    // the table names a page
+};
+
+template <bool F32, int D>
+__device__ __forceinline__ void load_k(Tile<F32, D> &t, const TileAt &at, int64_t sk, int m, int h) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int r = 16 * s + m;
+    const char *p = at.k + (r < at.last ? r : at.last) * sk + h * (F32 ? 32 : 16);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int x = 0; x < Tile<F32, D>::CH; ++x) t.k[s][c][x] = *(const u32x4 *)(p + c * (F32 ? 128 : 64) + x * 16);
+  }
+}
+
+template <bool F32, int D>
+__device__ __forceinline__ void load_v(Tile<F32, D> &t, const TileAt &at, int64_t sv, int m, int h) {
+  constexpr int VW = Tile<F32, D>::VW;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = (i < 4 ? i : 12 + i) + 4 * h;
+    const char *p = at.v + (r < at.last ? r : at.last) * sv + m * (VW * 4);
+    if constexpr (VW == 2) {
+      const u32x2 x = *(const u32x2 *)p;
+      t.v[i][0] = x[0], t.v[i][1] = x[1];
+    } else {
+#pragma unroll
+      for (int w = 0; w < VW / 4; ++w) {
+        const u32x4 x = *(const u32x4 *)(p + 16 * w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t.v[i][4 * w + e] = x[e];
+      }
+    }
+  }
+}
+
+// The operand V^T of output tile t: dimension DT * m + t of the lane's 8 rows (lo: fp32 only).
+template <bool F32, int D>
+__device__ __forceinline__ void v_operand(const Tile<F32, D> &T, int t, u32x4 &hi, u32x4 &lo) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32) {
+      uint32_t x, y;
+      split2(__builtin_bit_cast(float, T.v[2 * i][t]), __builtin_bit_cast(float, T.v[2 * i + 1][t]), x, y);
+      hi[i] = x, lo[i] = y;
+    } else {
+      hi[i] = __builtin_amdgcn_perm(T.v[2 * i + 1][t / 2], T.v[2 * i][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
+    }
+  }
+}
+
+// ---- the work of a workgroup -------------------------------------------------------------------
+// Sequences differ in length, and their lengths are known on the device only.  Every workgroup reads all
+// lengths and derives the same plan: the pieces of every item (sequence, head, row tile) in groups of 128
+// rows, equal to within one, so that all items together make about `slots` pieces.
+// Pieces of a sequence of `tiles` groups at `per` groups a piece.
+RS_HD int pieces_of(int tiles, int per) { return tiles > per ? (tiles + per - 1) / per : 1; }
+
+struct DraftArgs {
+  CacheView c;
+  DraftView q;
+  char *o;
+  int64_t so_t, so_h;
+  float *lse;
+  float *po, *pml;   // pieces: O (unnormalised), then (max, sum) of every row
+  int rtiles;        // row tiles of a sequence with max_rows rows
+  int slots;         // pieces that all items together may have beyond one each
+  const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
+  int nsel, pieces;  // with a list: pieces per item
+};
+
+// Rows of keys of sequence b that the kernels walk: cached rows and drafts.
+__device__ __forceinline__ int walk_len(const DraftArgs &a, int len, int t) {
+  return len + t < a.c.cap ? len + t : a.c.cap;
+}
+
+// What a workgroup works on.
+struct Item {
+  int b, g, rt, piece, npieces, slot0;  // slot0: the item's first slot of pieces
+  int len, t, first;                    // rows held, new rows and the first of them
+};
+
+// Groups per piece: the same from the lengths alone in every workgroup and in the joining kernel.
+__device__ int plan_groups(const DraftArgs &a, int lane) {
+  long long work = 0;
+  for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
+    const int b = b0 + lane;
+    if (b < a.c.nseq) {
+      const RowRange r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+      if (r.count > 0) work += (walk_len(a, cache_len(a.c, b), r.count) + kGroup - 1) / kGroup;
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) work += __shfl_xor(work, m);
+  const long long per = (long long)a.c.hkv * a.rtiles, total = work * per;
+  // with pieces of at most C = ceil(total / slots) groups an item of n groups has less than n / C + 1 of them:
+  // all together at most slots + the number of items, which is what the host counts
+  const long long groups = (total + a.slots - 1) / a.slots;
+  return groups > 0 ? (int)groups : 1;
+}
+
+// The piece-th piece overall; false: there are fewer.
+__device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
+  const int groups = plan_groups(a, lane);
+  const int per = a.c.hkv * a.rtiles;
+  int base = 0;
+  for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
+    const int b = b0 + lane;
+    int np = 0;
+    if (b < a.c.nseq) {
+      const RowRange r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+      if (r.count > 0) np = pieces_of((walk_len(a, cache_len(a.c, b), r.count) + kGroup - 1) / kGroup, groups);
+    }
+    int s = np * per;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int y = __shfl_up(s, m);
+      if (lane >= m) s += y;
+    }
+    const int all = __shfl(s, 63);
+    if (id < base + all) {
+      const unsigned long long hit = __ballot(id < base + s);
+      const int l = __builtin_ctzll(hit);
+      it.b = b0 + l;
+      it.npieces = __shfl(np, l);
+      const int x = id - (base + __shfl(s, l) - it.npieces * per);  // piece-major: all heads' row tiles of a piece adjacent
+      it.slot0 = base + __shfl(s, l) - it.npieces * per;
+      it.piece = x / per;
+      const int y = x - it.piece * per;
+      it.rt = y / a.c.hkv;
+      it.g = y - it.rt * a.c.hkv;
+      return true;
+    }
+    base += all;
+  }
+  return false;
+}
+
+// NQ: 16-row tiles of Q per wave.
+template <bool F32, int D, int NQ, bool SEL>
+__global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const DraftArgs a) {
+  using T = Tile<F32, D>;
+  constexpr int KC = T::KC, DT = T::DT, E = F32 ? 4 : 2, QP = F32 ? 2 : 1;
+  constexpr int LD = D + 4;  // row of O in LDS, padded
+  __shared__ float so[kWaves][16 * NQ][LD];
+  __shared__ float sml[kWaves][16 * NQ][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m = lane & 15, h = lane >> 4;
+  Item it;
+  int row_t0 = 0;  // with a list: the new row of the item
+  if constexpr (SEL) {
+    const int r = blockIdx.x / a.pieces;
+    it.g = blockIdx.y % a.c.hkv;
+    it.rt = blockIdx.y / a.c.hkv;
+    it.piece = blockIdx.x - r * a.pieces;
+    it.npieces = a.pieces;
+    it.b = -1;
+    for (int b0 = 0; b0 < a.c.nseq && it.b < 0; b0 += 64) {
+      const int b = b0 + lane;
+      RowRange x{0, 0};
+      if (b < a.c.nseq) x = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+      const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        it.b = b0 + l;
+        it.first = __shfl(x.first, l);
+        it.t = __shfl(x.count, l);
+      }
+    }
+    if (it.b < 0) return;  // a row of no sequence
+    row_t0 = r - it.first;
+    it.slot0 = ((r * a.rtiles + it.rt) * a.c.hkv + it.g) * a.pieces;
+  } else {
+    if (!find_item(a, blockIdx.x, lane, it)) return;
+    const RowRange x = new_rows(a.q.start, it.b, a.q.nrows, a.q.max_rows);
+    it.first = x.first;
+    it.t = x.count;
+  }
+  it.b = __builtin_amdgcn_readfirstlane(it.b);
+  it.g = __builtin_amdgcn_readfirstlane(it.g);
+  it.first = __builtin_amdgcn_readfirstlane(it.first);
+  it.t = __builtin_amdgcn_readfirstlane(it.t);
+  const CacheView &c = a.c;
+  const int len = __builtin_amdgcn_readfirstlane(cache_len(c, it.b));
+  const int G = a.q.hq / c.hkv, nr = SEL ? G : G * it.t;  // rows of this sequence (and token) and head
+  const int r0 = it.rt * 16 * NQ;
+  if (r0 >= nr) return;
+  // the walk: rows [0, total), or the selected blocks' rows and then those behind the last complete block
+  const int total = walk_len(a, len, it.t), full = len >> 6;
+  const int nblk = SEL ? (a.nsel < full ? a.nsel : full) : 0;
+  const int steps = SEL ? nblk * 64 + (total - full * 64) : total;
+  const int ngroups = (steps + kGroup - 1) / kGroup;
+  const int g0 = (int)((long long)ngroups * it.piece / it.npieces), g1 = (int)((long long)ngroups * (it.piece + 1) / it.npieces);
+  const int32_t *list = SEL ? a.list + ((int64_t)(it.first + row_t0) * c.hkv + it.g) * a.nsel : nullptr;
+
+  // Q: rows beyond the last are read as the last and not stored
+  u32x4 q[NQ][KC][QP];
+  int tq[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    int r = r0 + 16 * n + m;
+    r = r < nr ? r : nr - 1;
+    tq[n] = SEL ? row_t0 : r / G;
+    const int hh = it.g * G + (SEL ? r : r - tq[n] * G);
+    const char *p = (const char *)a.q.q + ((it.first + tq[n]) * a.q.sq_t + hh * a.q.sq_h) * E + h * 8 * E;
+#pragma unroll
+    for (int x = 0; x < KC; ++x) {
+      if constexpr (F32)
+        split8(*(const f32x4 *)(p + x * 128), *(const f32x4 *)(p + x * 128 + 16), q[n][x][0], q[n][x][1]);
+      else
+        q[n][x][0] = *(const u32x4 *)(p + x * 64);
+    }
+  }
+
+  f32x4 oacc[NQ][DT];
+  float mx[NQ], sum[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    mx[n] = -__builtin_inff();
+    sum[n] = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) oacc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // first row of the tile at step s of the walk
+  auto row_of = [&](int s) {
+    if constexpr (SEL) {
+      if (s < nblk * 64) return uload(list, s >> 6) * 64 + (s & 63);
+      return full * 64 + s - nblk * 64;
+    } else {
+      return s;
+    }
+  };
+  auto place = [&](int s, int &j) {
+    j = __builtin_amdgcn_readfirstlane(row_of(s));
+    const int p = page_of(c, j);
+    const int raw = c.table ? uload(c.table, (int64_t)it.b * c.max_pages + p) : it.b * c.max_pages + p;
+    int id = checked_page(c, raw);
+    TileAt at;
+    at.ok = id >= 0;
+    id = at.ok ? id : 0;
+    at.k = c.k + k_offset(c, id, p, j, it.g);
+    at.v = c.v + v_offset(c, id, p, j, it.g);
+    at.last = total - 1 - j < kTile - 1 ? total - 1 - j : kTile - 1;
+    if (!at.ok) at.last = 0;  // page 0 has a row 0 ... and its rows are masked
+    if (!at.ok) {
+      at.k = c.k + it.g * c.sk_h;
+      at.v = c.v + it.g * c.sv_h;
+    }
+    return at;
+  };
+
+  auto compute = [&](T &kv, const TileAt &at, int j) {
+    // a tile that any row may not see in whole: its end, drafted rows, no page
+    const bool edge = j + kTile > len || !at.ok;
+    u32x4 pb[NQ], pvis[NQ];
+    bool odd = false;  // values that a zero weight does not silence, in an edge tile
+    if (edge) {
+      int bad = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < T::VW; ++w) {
+          const uint32_t x = kv.v[i][w];
+          if constexpr (F32)
+            bad |= (x & 0x7f800000u) == 0x7f800000u;
+          else
+            bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+        }
+      odd = __any(bad);
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      f32x4 s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < KC; ++x) {
+          if constexpr (F32) {
+            u32x4 kh, kl;
+            split8(__builtin_bit_cast(f32x4, kv.k[u][x][0]), __builtin_bit_cast(f32x4, kv.k[u][x][1]), kh, kl);
+            s[u] = mfma16(kl, q[n][x][0], s[u]);
+            s[u] = mfma16(kh, q[n][x][1], s[u]);
+            s[u] = mfma16(kh, q[n][x][0], s[u]);
+          } else {
+            s[u] = mfma16(kv.k[u][x][0], q[n][x][0], s[u]);
+          }
+        }
+      }
+      float tm = -__builtin_inff();
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[u][e] *= a.q.c;
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = j + 16 * u + 4 * h + e - len;  // drafted row, negative: a cached one
+            bool see = i < 0 || (i < it.t && i <= tq[n]);
+            if (i >= 0 && i < it.t && a.q.mask)
+              see = a.q.mask[(int64_t)(it.first + tq[n]) * a.q.nwords + (i >> 5)] >> (i & 31) & 1;
+            see = see && at.ok && j + 16 * u + 4 * h + e < total;
+            s[u][e] = see ? s[u][e] : -__builtin_inff();
+          }
+        if (odd) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            pvis[n][w] = (s[w >> 1][2 * (w & 1)] == -__builtin_inff() ? 0u : 0x3f80u) |
+                         (s[w >> 1][2 * (w & 1) + 1] == -__builtin_inff() ? 0u : 0x3f800000u);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tm = fmaxf(tm, s[u][e]);
+      tm = fmaxf(max4(tm), mx[n]);
+      if (__any(tm > mx[n])) {
+        const float al = tm == -__builtin_inff() ? 1.f : exp2_fast(mx[n] - tm);
+        mx[n] = tm;
+        sum[n] *= al;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) oacc[n][t] *= al;
+      }
+      const float base = mx[n] == -__builtin_inff() ? 0.f : mx[n];
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = exp2_fast(s[e >> 2][e & 3] - base);
+        sum[n] += p[e];
+      }
+      // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-9
+      // of the output at most); its sum is taken before
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pb[n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
+    }
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      u32x4 vh, vl;
+      v_operand<F32, D>(kv, t, vh, vl);
+      if (odd) {
+        // infinities and NaN count only where they are seen: finite values go through the product, the
+        // others through products of 0 and 1 that tell which rows see one
+#pragma unroll
+        for (int kind = 0; kind < 3; ++kind) {
+          u32x4 one, clean = vh;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t o2 = 0, c2 = 0;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const uint32_t x = vh[w] >> (16 * z) & 0xffffu;
+              const bool hit = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
+              o2 |= (hit ? 0x3f80u : 0u) << (16 * z);
+              c2 |= ((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) << (16 * z);
+            }
+            one[w] = o2;
+            clean[w] &= c2;
+            if (F32 && kind == 2) vl[w] &= c2;
+          }
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            const f32x4 cnt = mfma16(one, pvis[n], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (cnt[e] > 0.f)
+                oacc[n][t][e] += kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
+          }
+          if (kind == 2) vh = clean;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if constexpr (F32) oacc[n][t] = mfma16(vl, pb[n], oacc[n][t]);
+        oacc[n][t] = mfma16(vh, pb[n], oacc[n][t]);
+      }
+    }
+  };
+
+  // two tiles take turns: one is in flight while the other is used
+  const int s_end = g1 * kGroup < steps ? g1 * kGroup : steps;
+  int s = g0 * kGroup + wave * kTile;
+  if (s < s_end) {
+    T ta, tb;
+    int ja, jb = 0;
+    TileAt aa = place(s, ja), ab{};
+    load_k<F32, D>(ta, aa, c.sk_t, m, h);
+    load_v<F32, D>(ta, aa, c.sv_t, m, h);
+    while (true) {
+      s += kGroup;
+      const bool more = s < s_end;
+      if (more) {
+        ab = place(s, jb);
+        load_k<F32, D>(tb, ab, c.sk_t, m, h);
+        load_v<F32, D>(tb, ab, c.sv_t, m, h);
+      }
+      compute(ta, aa, ja);
+      if (!more) break;
+      s += kGroup;
+      const bool again = s < s_end;
+      if (again) {
+        aa = place(s, ja);
+        load_k<F32, D>(ta, aa, c.sk_t, m, h);
+        load_v<F32, D>(ta, aa, c.sv_t, m, h);
+      }
+      compute(tb, ab, jb);
+      if (!again) break;
+    }
+  }
+
+  // join the waves: lane (m, h) holds dimensions [D / 4 h, D / 4 (h + 1)) of row m
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const float z = sum4(sum[n]);
+    if (h == 0) {
+      sml[wave][16 * n + m][0] = mx[n];
+      sml[wave][16 * n + m][1] = z;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) so[wave][16 * n + m][h * (D / 4) + e * DT + t] = oacc[n][t][e];
+  }
+  __syncthreads();
+  const bool whole = it.npieces == 1;
+  const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
+  for (int x = tid; x < 16 * NQ * (D / 4); x += 256) {
+    const int r = x / (D / 4), o4 = x % (D / 4) * 4;
+    if (r0 + r >= nr) continue;
+    float M = -__builtin_inff(), w[kWaves], z = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sml[k][r][0]);
+    const float base = M == -__builtin_inff() ? 0.f : M;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      w[k] = exp2_fast(sml[k][r][0] - base);
+      z += w[k] * sml[k][r][1];
+      const float *p = &so[k][r][o4];
+      if (sml[k][r][0] != -__builtin_inff())
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[k] * p[e];
+    }
+    if (whole) {
+      const int t = SEL ? row_t0 : (r0 + r) / G, hh = it.g * G + (SEL ? r0 + r : r0 + r - t * G);
+      const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
+      u32x2 w2;
+      w2[0] = pack_bf16x2(v[0] * inv, v[1] * inv);
+      w2[1] = pack_bf16x2(v[2] * inv, v[3] * inv);
+      *(u32x2 *)(a.o + ((it.first + t) * a.so_t + hh * a.so_h + o4) * 2) = w2;
+      if (a.lse && o4 == 0)
+        a.lse[(int64_t)hh * a.q.nrows + it.first + t] = z == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(z)) * kLn2;
+    } else {
+      *(f32x4 *)(a.po + ((int64_t)slot * 16 * NQ + r) * D + o4) = v;
+      if (o4 == 0) {
+        float *ml = a.pml + ((int64_t)slot * 16 * NQ + r) * 2;
+        ml[0] = M;
+        ml[1] = z;
+      }
+    }
+  }
+}
+
+// Joins the pieces of every item: a workgroup per new row and head; its waves take pieces in turn, lanes
+// the dimensions, and LDS joins the waves.
+template <int D, int NQ, bool SEL>
+__global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
+  __shared__ float so[kWaves][D];
+  __shared__ float sml[kWaves][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const CacheView &c = a.c;
+  const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = blockIdx.y, g = hh / G;
+  int slot, np, stride, row;
+  if constexpr (SEL) {
+    const int rr = hh - g * G, rt = rr / (16 * NQ);
+    row = rr - rt * 16 * NQ;
+    slot = ((r * a.rtiles + rt) * c.hkv + g) * a.pieces;
+    np = a.pieces;
+    stride = 1;
+    bool any = false;
+    for (int b0 = 0; b0 < c.nseq && !any; b0 += 64) {
+      RowRange x{0, 0};
+      if (b0 + lane < c.nseq) x = new_rows(a.q.start, b0 + lane, a.q.nrows, a.q.max_rows);
+      any = __any(r >= x.first && r < x.first + x.count);
+    }
+    if (!any) return;
+  } else {
+    const int groups = plan_groups(a, lane), per = c.hkv * a.rtiles;
+    int base = 0, b = -1, first = 0;
+    np = 0;
+    for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
+      RowRange x{0, 0};
+      int k = 0;
+      if (b0 + lane < c.nseq) x = new_rows(a.q.start, b0 + lane, a.q.nrows, a.q.max_rows);
+      if (x.count > 0) k = pieces_of((walk_len(a, cache_len(c, b0 + lane), x.count) + kGroup - 1) / kGroup, groups);
+      int s = k * per;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const int y = __shfl_up(s, m);
+        if (lane >= m) s += y;
+      }
+      const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        b = b0 + l;
+        first = __shfl(x.first, l);
+        np = __shfl(k, l);
+        base += __shfl(s, l) - np * per;
+      } else {
+        base += __shfl(s, 63);
+      }
+    }
+    if (b < 0) return;
+    const int rr = (r - first) * G + hh - g * G, rt = rr / (16 * NQ);
+    row = rr - rt * 16 * NQ;
+    slot = base + rt * c.hkv + g;
+    stride = per;
+  }
+  if (np <= 1) return;
+  float M = -__builtin_inff(), z = 0.f, v[D / 64];
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) v[e] = 0.f;
+#pragma unroll 4
+  for (int k = wave; k < np; k += kWaves) {
+    const int64_t at = (int64_t)(slot + k * stride) * 16 * NQ + row;
+    const float pm = a.pml[at * 2], pz = a.pml[at * 2 + 1];
+    const float *p = a.po + at * D + lane * (D / 64);
+    const float m2 = fmaxf(M, pm), base = m2 == -__builtin_inff() ? 0.f : m2;
+    const float wo = exp2_fast(M - base), wn = exp2_fast(pm - base);
+    z = z * wo + pz * wn;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) v[e] = v[e] * wo + (pm == -__builtin_inff() ? 0.f : p[e] * wn);
+    M = m2;
+  }
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) so[wave][lane * (D / 64) + e] = v[e];
+  if (lane == 0) {
+    sml[wave][0] = M;
+    sml[wave][1] = z;
+  }
+  __syncthreads();
+  if (tid >= D / 2) return;
+  M = -__builtin_inff();
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sml[k][0]);
+  const float base = M == -__builtin_inff() ? 0.f : M;
+  float x = 0.f, y = 0.f;
+  z = 0.f;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    const float w = exp2_fast(sml[k][0] - base);
+    z += w * sml[k][1];
+    if (sml[k][0] != -__builtin_inff()) {
+      x += w * so[k][2 * tid];
+      y += w * so[k][2 * tid + 1];
+    }
+  }
+  const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
+  *(uint32_t *)(a.o + (r * a.so_t + hh * a.so_h + 2 * tid) * 2) = pack_bf16x2(x * inv, y * inv);
+  if (a.lse && tid == 0)
+    a.lse[(int64_t)hh * a.q.nrows + r] = z == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(z)) * kLn2;
+}
+
+// ---- scores and selection of blocks ------------------------------------------------------------
+// score(c) = max over the heads h of g of q_h . mean_c, in fp64: products of bf16 means and bf16 (or fp32) q
+// are exact, and so are the sums as long as their terms lie within 2^37 of each other, so that the
+// selection does not depend on the order of a sum.  A wave holds 64 blocks, one per lane, their means
+// staged through LDS; q comes as LDS broadcasts.  fp64 FMAs run at half the fp32 rate: the means' bytes and
+// the launch bound this kernel, not its arithmetic.
+struct SelectArgs {
+  CacheView c;
+  DraftView q;
+  double *score;  // [nrows * hkv][fcap]
+  int32_t *list;  // [nrows * hkv][nsel]
+  int fcap, nsel, nsink, nlocal;
+};
+
+// Sequence of new row r, by the wave; -1: none.
+__device__ __forceinline__ int seq_of_row(const CacheView &c, const DraftView &q, int r, int lane) {
+  for (int b0 = 0; b0 < c.nseq; b0 += 64) {
+    RowRange x{0, 0};
+    if (b0 + lane < c.nseq) x = new_rows(q.start, b0 + lane, q.nrows, q.max_rows);
+    const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+    if (hit) return b0 + __builtin_ctzll(hit);
+  }
+  return -1;
+}
+
+template <bool F32, int D>
+__global__ __launch_bounds__(64) void score_kernel(const SelectArgs a) {
+  constexpr int HB = 8, LPR = D / 8;  // heads at a time; lanes per mean
+  __shared__ uint32_t sm[64][D / 2 + 4];
+  __shared__ double sq[HB][D];
+  const int lane = threadIdx.x, r = blockIdx.x, g = blockIdx.y, c0 = blockIdx.z * 64;
+  const int b = seq_of_row(a.c, a.q, r, lane);
+  if (b < 0) return;
+  const int F = cache_len(a.c, b) >> 6;
+  if (c0 >= F || F <= a.nsel) return;  // (all blocks are taken: no scores)
+  const int G = a.q.hq / a.c.hkv;
+#pragma unroll 4
+  for (int x = lane / LPR; x < 64; x += 64 / LPR) {
+    const int blk = c0 + x < F ? c0 + x : F - 1, p = page_of(a.c, blk * 64), id = page_id(a.c, b, p);
+    u32x4 w{0, 0, 0, 0};
+    if (id >= 0) w = *(const u32x4 *)((const bf16 *)a.c.kmean + mean_offset(a.c, id, p, blk, g, D) + lane % LPR * 8);
+    *(u32x4 *)&sm[x][lane % LPR * 4] = w;
+  }
+  double best = -__builtin_inf();
+  for (int h0 = 0; h0 < G; h0 += HB) {
+    const int nh = G - h0 < HB ? G - h0 : HB;
+    __syncthreads();
+    for (int x = lane; x < nh * D; x += 64) {
+      const int64_t at = r * a.q.sq_t + (int64_t)(g * G + h0 + x / D) * a.q.sq_h + x % D;
+      sq[x / D][x % D] = F32 ? (double)((const float *)a.q.q)[at] : (double)(float)((const bf16 *)a.q.q)[at];
+    }
+    __syncthreads();
+    double s[HB] = {};
+    for (int d0 = 0; d0 < D; d0 += 8) {
+      const u32x4 w = *(const u32x4 *)&sm[lane][d0 / 2];
+      double k[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[2 * e] = (double)__builtin_bit_cast(float, w[e] << 16);
+        k[2 * e + 1] = (double)__builtin_bit_cast(float, w[e] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int h = 0; h < HB; ++h)
+        if (h < nh)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[h] = __builtin_fma(sq[h][d0 + e], k[e], s[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+      if (h < nh && s[h] > best) best = s[h];
+  }
+  if (c0 + lane < F) a.score[((int64_t)r * a.c.hkv + g) * a.fcap + c0 + lane] = best;
+}
+
+// The selected blocks of a row and head, ascending: a radix selection over the scores as ordered 64-bit keys
+// (11 bits a pass, ended as soon as all of the last digit's blocks stay), then their places by a prefix sum.
+__device__ __forceinline__ uint64_t double_key(double f) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, f + 0.0);  // -0.0 equals 0.0
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+
+constexpr int kSelThreads = 256, kSelPer = kMaxN / 64 / kSelThreads;
+
+__global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a) {
+  constexpr int kBins = 2048;
+  __shared__ int hist[kBins], sw[kSelThreads / 64], pick[3];
+  const int tid = threadIdx.x, r = blockIdx.x, g = blockIdx.y;
+  const int b = seq_of_row(a.c, a.q, r, tid & 63);
+  if (b < 0) return;
+  const int F = cache_len(a.c, b) >> 6;
+  const int64_t item = (int64_t)r * a.c.hkv + g;
+  int32_t *list = a.list + item * a.nsel;
+  const int nb = a.nsel < F ? a.nsel : F;
+  for (int x = nb + tid; x < a.nsel; x += kSelThreads) list[x] = -1;
+  if (F <= a.nsel) {
+    for (int x = tid; x < F; x += kSelThreads) list[x] = x;
+    return;
+  }
+  const int per = (F + kSelThreads - 1) / kSelThreads, c0 = tid * per;
+  uint64_t key[kSelPer];
+#pragma unroll
+  for (int x = 0; x < kSelPer; ++x) {
+    const int c = c0 + x;
+    key[x] = 0;  // (below every key)
+    if (x < per && c < F) key[x] = c < a.nsink || c >= F - a.nlocal ? ~0ull : double_key(a.score[item * a.fcap + c]);
+  }
+  uint64_t prefix = 0, have = 0;
+  int need = nb, equal = F, all;
+  for (int sh = 53; need < equal; sh -= 11) {
+    const int low = sh > 0 ? sh : 0, bins = sh > 0 ? kBins : kBins >> -sh;  // the last digit has 9 bits
+    for (int x = tid; x < bins; x += kSelThreads) hist[x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kSelPer; ++x)
+      if (x < per && c0 + x < F && (key[x] & have) == prefix) atomicAdd(&hist[(key[x] >> low) & (bins - 1)], 1);
+    __syncthreads();
+    const int pb = bins / kSelThreads, top = bins - 1 - tid * pb;
+    int sum = 0;
+    for (int x = 0; x < pb; ++x) sum += hist[top - x];
+    int before = block_scan<kSelThreads>(sum, sw, &all);
+    if (before < need && before + sum >= need) {
+      int x = top;
+      while (before + hist[x] < need) before += hist[x--];
+      pick[0] = x;
+      pick[1] = need - before;
+      pick[2] = hist[x];
+    }
+    __syncthreads();
+    prefix |= (uint64_t)pick[0] << low;
+    have |= (uint64_t)(bins - 1) << low;
+    need = pick[1];
+    equal = pick[2];
+    __syncthreads();
+    if (low == 0) break;
+  }
+  int e = 0, above = 0;
+#pragma unroll
+  for (int x = 0; x < kSelPer; ++x)
+    if (x < per && c0 + x < F) {
+      e += (key[x] & have) == prefix;
+      above += (key[x] & have) > prefix;
+    }
+  // blocks before this thread's that equal the border: the first `need` of them stay, so the thread's place
+  // is known from both counts
+  const int both = block_scan<kSelThreads>(above | e << 16, sw, &all);
+  int eq = both >> 16, at = (both & 0xffff) + (eq < need ? eq : need);
+#pragma unroll
+  for (int x = 0; x < kSelPer; ++x)
+    if (x < per && c0 + x < F) {
+      const uint64_t k = key[x] & have;
+      if (k > prefix || (k == prefix && eq < need)) list[at++] = c0 + x;
+      eq += k == prefix;
+    }
+}
+
+// ---- accumulated weights -------------------------------------------------------------------------
+// acc_j += sum over rows r of w_r exp(l_rj - lse_r): the S^T tiles of the attention again, without V, summed over
+// the 16 rows of a tile in the lanes that hold them.  K is read once, into registers (NT tiles of 32 rows per
+// wave), and the rows' Q tiles pass over it; a row of the cache belongs to one wave, so nothing is added in
+// an order that varies.
+struct WeightArgs {
+  CacheView c;
+  DraftView q;
+  const float *lse, *row_w, *acc_in;
+  float *acc_out;
+};
+
+template <bool F32, int D>
+__global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
+  using T = Tile<F32, D>;
+  constexpr int KC = T::KC, E = F32 ? 4 : 2, NT = F32 ? 2 : 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, h = lane >> 4, g = blockIdx.y, b = blockIdx.z;
+  const CacheView &c = a.c;
+  const RowRange rr = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+  const int len = cache_len(c, b), total = len + rr.count < c.cap ? len + rr.count : c.cap;
+  const int j0 = (blockIdx.x * kWaves + wave) * NT * kTile;
+  if (j0 >= total || rr.count == 0) return;
+  const int G = a.q.hq / c.hkv, nr = G * rr.count;
+  u32x4 k[NT][2][KC][T::CH];
+  bool ok[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    int j = j0 + n * kTile;
+    j = j < total ? j : j0;  // a tile behind the end: read as the first and not stored
+    const int p = page_of(c, j), id = page_id(c, b, p);
+    ok[n] = id >= 0;
+    const char *base = ok[n] ? c.k + k_offset(c, id, p, j, g) : c.k + g * c.sk_h;
+    int last = total - 1 - j < kTile - 1 ? total - 1 - j : kTile - 1;
+    if (!ok[n]) last = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 16 * u + m;
+      const char *q = base + (r < last ? r : last) * c.sk_t + h * (F32 ? 32 : 16);
+#pragma unroll
+      for (int x = 0; x < KC; ++x)
+#pragma unroll
+        for (int y = 0; y < T::CH; ++y) k[n][u][x][y] = *(const u32x4 *)(q + x * (F32 ? 128 : 64) + y * 16);
+    }
+  }
+  float sum[NT][8];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[n][e] = 0.f;
+  const bool edge = j0 + NT * kTile > len;
+  for (int r0 = 0; r0 < nr; r0 += 16) {
+    const bool mine = r0 + m < nr;
+    const int r = mine ? r0 + m : nr - 1, t = r / G, hh = g * G + r - t * G;
+    const int64_t row = rr.first + t;
+    const char *p = (const char *)a.q.q + (row * a.q.sq_t + hh * a.q.sq_h) * E + h * 8 * E;
+    u32x4 q[KC][F32 ? 2 : 1];
+#pragma unroll
+    for (int x = 0; x < KC; ++x) {
+      if constexpr (F32)
+        split8(*(const f32x4 *)(p + x * 128), *(const f32x4 *)(p + x * 128 + 16), q[x][0], q[x][1]);
+      else
+        q[x][0] = *(const u32x4 *)(p + x * 64);
+    }
+    const float l2 = a.lse[(int64_t)hh * a.q.nrows + row] * kLog2e, w = mine ? (a.row_w ? a.row_w[row] : 1.f) : 0.f;
+    const bool on = w != 0.f && l2 != -__builtin_inff();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      f32x4 s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < KC; ++x) {
+          if constexpr (F32) {
+            u32x4 kh, kl;
+            split8(__builtin_bit_cast(f32x4, k[n][u][x][0]), __builtin_bit_cast(f32x4, k[n][u][x][1]), kh, kl);
+            s[u] = mfma16(kl, q[x][0], s[u]);
+            s[u] = mfma16(kh, q[x][1], s[u]);
+            s[u] = mfma16(kh, q[x][0], s[u]);
+          } else {
+            s[u] = mfma16(k[n][u][x][0], q[x][0], s[u]);
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bool see = on;
+        if (edge) {
+          const int i = j0 + n * kTile + 16 * (e >> 2) + 4 * h + (e & 3) - len;
+          if (i >= 0) {
+            bool v = i < rr.count && i <= t;
+            if (i < rr.count && a.q.mask) v = a.q.mask[row * a.q.nwords + (i >> 5)] >> (i & 31) & 1;
+            see = see && v;
+          }
+        }
+        const float x = w * exp2_fast(s[e >> 2][e & 3] * a.q.c - l2);
+        sum[n][e] += see ? x : 0.f;
+      }
+    }
+  }
+  const int64_t at = ((int64_t)b * c.hkv + g) * c.cap;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x = sum[n][e];
+#pragma unroll
+      for (int y = 1; y < 16; y <<= 1) x += __shfl_xor(x, y);
+      const int j = j0 + n * kTile + 16 * (e >> 2) + 4 * h + (e & 3);
+      if (m == (e & 15) && j < total && ok[n]) a.acc_out[at + j] = (a.acc_in ? a.acc_in[at + j] : 0.f) + x;
+    }
+}
+
+// ---- launches --------------------------------------------------------------------------------------
+// Row tiles of Q per wave: as few as hold the rows of one item, so that K and V are read once; more rows
+// than 64 (32 in fp32, whose tiles take twice the registers) become row tiles of their own.
+int row_tiles(bool f32, int rows) { return rows <= 16 ? 1 : rows <= 32 || f32 ? 2 : 4; }
+
+struct DraftShape {
+  int nq, rtiles, slots, grid, pieces;
+};
+
+// Workgroups that the chip holds at once: two per CU with one row tile of bf16, else one.
+DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int nsel) {
+  DraftShape s{};
+  const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
+  s.nq = row_tiles(f32, rows);
+  s.rtiles = (rows + 16 * s.nq - 1) / (16 * s.nq);
+  const int resident = !f32 && s.nq == 1 ? 512 : 256;
+  if (nsel) {
+    const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
+    const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
+    int64_t p = items ? resident / items : 1;
+    p = p < most ? p : most;
+    s.pieces = p > 1 ? (int)p : 1;
+    s.grid = (int)(items * s.pieces);
+    return s;
+  }
+  const int64_t items = (int64_t)c.nseq * c.hkv * s.rtiles, most = items * ((c.cap + kGroup - 1) / kGroup);
+  // few items: one round of workgroups; many: pieces of a quarter of a round, so that the last round is short
+  s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
+  const int64_t grid = items + s.slots;
+  s.grid = (int)(grid < most ? grid : most);
+  return s;
+}
+
+template <typename F>
+void by_tiles(bool f32, int d, int nq, F f) {
+  auto with_d = [&](auto x, auto dd) {
+    using N1 = std::integral_constant<int, 1>;
+    using N2 = std::integral_constant<int, 2>;
+    using N4 = std::integral_constant<int, 4>;
+    if (nq == 1)
+      f(x, dd, N1{});
+    else if (nq == 2)
+      f(x, dd, N2{});
+    else if constexpr (!decltype(x)::value)
+      f(x, dd, N4{});
+  };
+  auto with_t = [&](auto x) {
+    d == 128 ? with_d(x, std::integral_constant<int, 128>{}) : with_d(x, std::integral_constant<int, 64>{});
+  };
+  f32 ? with_t(std::true_type{}) : with_t(std::false_type{});
+}
+
+DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const DraftShape &s, int d) {
+  DraftArgs a{};
+  a.c = c;
+  a.q = q;
+  a.rtiles = s.rtiles;
+  a.slots = s.slots;
+  a.pieces = s.pieces;
+  a.po = ar.take<float>((size_t)s.grid * 16 * s.nq * d);
+  a.pml = ar.take<float>((size_t)s.grid * 16 * s.nq * 2);
+  return a;
+}
+
+SelectArgs select_parts(Arena &ar, const CacheView &c, const DraftView &q, int nsel) {
+  SelectArgs s{};
+  s.c = c;
+  s.q = q;
+  s.nsel = nsel;
+  s.fcap = c.cap >> 6;
+  s.list = ar.take<int32_t>((size_t)q.nrows * c.hkv * nsel);
+  s.score = ar.take<double>((size_t)q.nrows * c.hkv * s.fcap);
+  return s;
+}
+
+template <bool SEL>
+rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipStream_t st) {
+  by_tiles(f32, d, s.nq, [&](auto x, auto dd, auto nn) {
+    constexpr bool F = decltype(x)::value;
+    constexpr int D = decltype(dd)::value, NQ = decltype(nn)::value;
+    if constexpr (SEL)
+      draft_kernel<F, D, NQ, true><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
+    else
+      draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
+    if (SEL ? s.pieces > 1 : a.c.cap > kGroup)
+      draft_join_kernel<D, NQ, SEL><<<dim3(a.q.nrows, a.q.hq), 256, 0, st>>>(a);
+  });
+  RS_HIP(hipGetLastError());
+  return RS_OK;
+}
+
+}  // namespace
+
+size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
+  Arena ar(nullptr, 0);
+  if (nsel) select_parts(ar, c, q, nsel);
+  draft_parts(ar, c, q, draft_shape(c, q, f32, nsel), d);
+  return ar.off + 256;
+}
+
+rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
+                       void *ws, size_t ws_bytes, hipStream_t st) {
+  const DraftShape s = draft_shape(c, q, f32, 0);
+  Arena ar(ws, ws_bytes);
+  DraftArgs a = draft_parts(ar, c, q, s, d);
+  if (!ws || !ar.ok())
+    return fail(RS_ERR_WORKSPACE, "draft attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, 0)));
+  a.o = (char *)o, a.so_t = so_t, a.so_h = so_h, a.lse = lse;
+  return attend<false>(a, s, f32, d, st);
+}
+
+rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int nsink, int nlocal, void *o,
+                        int64_t so_t, int64_t so_h, float *lse, int32_t *blocks, void *ws, size_t ws_bytes, hipStream_t st) {
+  const DraftShape s = draft_shape(c, q, f32, nsel);
+  Arena ar(ws, ws_bytes);
+  SelectArgs sel = select_parts(ar, c, q, nsel);
+  DraftArgs a = draft_parts(ar, c, q, s, d);
+  if (!ws || !ar.ok())
+    return fail(RS_ERR_WORKSPACE, "selected attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, nsel)));
+  if (blocks) sel.list = blocks;
+  sel.nsink = nsink, sel.nlocal = nlocal;
+  a.o = (char *)o, a.so_t = so_t, a.so_h = so_h, a.lse = lse;
+  a.list = sel.list, a.nsel = nsel;
+  if (sel.fcap > nsel) {
+    const dim3 grid(q.nrows, c.hkv, (sel.fcap + 63) / 64);
+    f32 ? (d == 128 ? score_kernel<true, 128><<<grid, 64, 0, st>>>(sel) : score_kernel<true, 64><<<grid, 64, 0, st>>>(sel))
+        : (d == 128 ? score_kernel<false, 128><<<grid, 64, 0, st>>>(sel) : score_kernel<false, 64><<<grid, 64, 0, st>>>(sel));
+  }
+  select_kernel<<<dim3(q.nrows, c.hkv), kSelThreads, 0, st>>>(sel);
+  return attend<true>(a, s, f32, d, st);
+}
+
+rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d, const float *lse, const float *row_w,
+                         const float *acc_in, float *acc_out, hipStream_t st) {
+  WeightArgs a{c, q, lse, row_w, acc_in, acc_out};
+  const int rows = (f32 ? 2 : 4) * kTile * kWaves;
+  const dim3 grid((c.cap + rows - 1) / rows, c.hkv, c.nseq);
+  f32 ? (d == 128 ? weights_kernel<true, 128><<<grid, 256, 0, st>>>(a) : weights_kernel<true, 64><<<grid, 256, 0, st>>>(a))
+      : (d == 128 ? weights_kernel<false, 128><<<grid, 256, 0, st>>>(a) : weights_kernel<false, 64><<<grid, 256, 0, st>>>(a));
+  RS_HIP(hipGetLastError());
+  return RS_OK;
+}
+
+}  // namespace rs
