@@ -207,9 +207,20 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(CacheView c, i
     const int bits = pass ? 10 : 12, sh = pass == 0 ? 20 : pass == 1 ? 10 : 0, bins = 1 << bits;
     for (int x = tid; x < bins; x += kPlanThreads) hist[x] = 0;
     __syncthreads();
-    for (int j = tid; j < n; j += kPlanThreads) {
-      const uint32_t key = evict_key(acc[j], pos[j], nsink, firm_from);
-      if ((key & have) == prefix) atomicAdd(&hist[(key >> sh) & (bins - 1)], 1);
+    for (int j0 = tid; j0 < n; j0 += kPlanThreads * kPer) {
+      float x[kPer];
+      int y[kPer];
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) {
+        const int j = j0 + u * kPlanThreads < n ? j0 + u * kPlanThreads : j0;
+        x[u] = acc[j];
+        y[u] = pos[j];
+      }
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) {
+        const uint32_t key = evict_key(x[u], y[u], nsink, firm_from);
+        if (j0 + u * kPlanThreads < n && (key & have) == prefix) atomicAdd(&hist[(key >> sh) & (bins - 1)], 1);
+      }
     }
     __syncthreads();
     // thread t counts the t-th highest group of bins; the one where the count reaches `need` picks

@@ -642,9 +642,12 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
 // ---- scores and selection of blocks ------------------------------------------------------------
 // score(c) = max over the heads h of g of q_h . mean_c, in fp64: products of bf16 means and bf16 (or fp32) q
 // are exact, and so are the sums as long as their terms lie within 2^37 of each other, so that the
-// selection does not depend on the order of a sum.  A wave holds 64 blocks, one per lane, their means
-// staged through LDS; q comes as LDS broadcasts.  fp64 FMAs run at half the fp32 rate: the means' bytes and
-// the launch bound this kernel, not its arithmetic.
+// selection does not depend on the order of a sum.  The products are v_mfma_f64_16x16x4: 16 rows of a
+// sequence (tokens and heads) against 16 blocks per wave, both operands straight from memory (a lane holds a
+// quarter of a row: the contraction may run in any order), the means converted once for all rows.  The
+// vector ALU has the same fp64 rate without padding rows to 16, but its q operands come through LDS: 80 rows x 8
+// heads over 36K rows of cache took 114 us so, 25 us with the matrix instructions; what is left is
+// latency.
 struct SelectArgs {
   CacheView c;
   DraftView q;
@@ -664,53 +667,94 @@ __device__ __forceinline__ int seq_of_row(const CacheView &c, const DraftView &q
   return -1;
 }
 
+// Rows of a 16-row tile: whole tokens of G heads, or 16 heads of one token.
+RS_HD int score_tokens(int G) { return G < 16 ? 16 / G : 1; }
+
 template <bool F32, int D>
-__global__ __launch_bounds__(64) void score_kernel(const SelectArgs a) {
-  constexpr int HB = 8, LPR = D / 8;  // heads at a time; lanes per mean
-  __shared__ uint32_t sm[64][D / 2 + 4];
-  __shared__ double sq[HB][D];
-  const int lane = threadIdx.x, r = blockIdx.x, g = blockIdx.y, c0 = blockIdx.z * 64;
-  const int b = seq_of_row(a.c, a.q, r, lane);
-  if (b < 0) return;
+__global__ __launch_bounds__(256, 2) void score_kernel(const SelectArgs a) {
+  constexpr int DL = D / 4, E = F32 ? 4 : 2;  // dimensions per lane: lane (m, h) holds [DL h, DL (h + 1)) of a row
+  __shared__ double ss[kWaves][16][17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, h = lane >> 4;
+  const int g = blockIdx.y, b = blockIdx.z, c0 = (blockIdx.x * kWaves + wave) * 16;
+  const RowRange rr = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
   const int F = cache_len(a.c, b) >> 6;
   if (c0 >= F || F <= a.nsel) return;  // (all blocks are taken: no scores)
-  const int G = a.q.hq / a.c.hkv;
-#pragma unroll 4
-  for (int x = lane / LPR; x < 64; x += 64 / LPR) {
-    const int blk = c0 + x < F ? c0 + x : F - 1, p = page_of(a.c, blk * 64), id = page_id(a.c, b, p);
-    u32x4 w{0, 0, 0, 0};
-    if (id >= 0) w = *(const u32x4 *)((const bf16 *)a.c.kmean + mean_offset(a.c, id, p, blk, g, D) + lane % LPR * 8);
-    *(u32x4 *)&sm[x][lane % LPR * 4] = w;
-  }
-  double best = -__builtin_inf();
-  for (int h0 = 0; h0 < G; h0 += HB) {
-    const int nh = G - h0 < HB ? G - h0 : HB;
-    __syncthreads();
-    for (int x = lane; x < nh * D; x += 64) {
-      const int64_t at = r * a.q.sq_t + (int64_t)(g * G + h0 + x / D) * a.q.sq_h + x % D;
-      sq[x / D][x % D] = F32 ? (double)((const float *)a.q.q)[at] : (double)(float)((const bf16 *)a.q.q)[at];
-    }
-    __syncthreads();
-    double s[HB] = {};
-    for (int d0 = 0; d0 < D; d0 += 8) {
-      const u32x4 w = *(const u32x4 *)&sm[lane][d0 / 2];
-      double k[8];
+  const int G = a.q.hq / a.c.hkv, tp = score_tokens(G), parts = (G + 15) >> 4;
+  // means of 16 blocks, lane m the m-th; blocks behind the last are read as the last
+  const int blk = c0 + m < F ? c0 + m : F - 1, p = page_of(a.c, blk * 64), id = page_id(a.c, b, p);
+  double km[DL];
+  {
+    const u32x4 *x = (const u32x4 *)((const bf16 *)a.c.kmean + mean_offset(a.c, id >= 0 ? id : 0, p, id >= 0 ? blk : p * (a.c.page >> 6), g, D) + DL * h);
+#pragma unroll
+    for (int i = 0; i < DL / 8; ++i) {
+      u32x4 w = x[i];
+      if (id < 0) w = u32x4{0, 0, 0, 0};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        k[2 * e] = (double)__builtin_bit_cast(float, w[e] << 16);
-        k[2 * e + 1] = (double)__builtin_bit_cast(float, w[e] & 0xffff0000u);
+        km[8 * i + 2 * e] = (double)__builtin_bit_cast(float, w[e] << 16);
+        km[8 * i + 2 * e + 1] = (double)__builtin_bit_cast(float, w[e] & 0xffff0000u);
       }
+    }
+  }
+  typedef double f64x4 __attribute__((ext_vector_type(4)));
+  for (int t0 = 0; t0 < rr.count; t0 += tp) {
+    double best[4] = {-__builtin_inf(), -__builtin_inf(), -__builtin_inf(), -__builtin_inf()};
+    for (int part = 0; part < parts; ++part) {
+      // the m-th row: head hh of token t; rows beyond the last are read as the last
+      int t = t0, hh = part * 16 + m;
+      if (parts == 1) {
+        t = t0 + m / G;
+        hh = m % G;
+        if (m >= tp * G || t >= rr.count) t = rr.count - 1;
+      }
+      hh = hh < G ? hh : G - 1;
+      const char *q = (const char *)a.q.q + ((rr.first + t) * a.q.sq_t + (g * G + hh) * a.q.sq_h + DL * h) * E;
+      f64x4 s{0., 0., 0., 0.};
 #pragma unroll
-      for (int h = 0; h < HB; ++h)
-        if (h < nh)
+      for (int i = 0; i < DL / 8; ++i) {
+        float f[8];
+        if constexpr (F32) {
+          const f32x4 x = *(const f32x4 *)(q + 32 * i), y = *(const f32x4 *)(q + 32 * i + 16);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s[h] = __builtin_fma(sq[h][d0 + e], k[e], s[h]);
+          for (int e = 0; e < 4; ++e) f[e] = x[e], f[4 + e] = y[e];
+        } else {
+          const u32x4 w = *(const u32x4 *)(q + 16 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+            f[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = __builtin_amdgcn_mfma_f64_16x16x4f64((double)f[e], km[8 * i + e], s, 0, 0, 0);
+      }
+      // lane (m, h) holds rows h, 4 + h, ... of block m; the maximum over a token's heads through LDS
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ss[wave][4 * e + h][m] = s[e];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const int nh = parts == 1 ? G : G - part * 16 < 16 ? G - part * 16 : 16;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // tokens h, h + 4, ...
+        const int tt = h + 4 * e;
+        if (tt < tp)
+          for (int x = 0; x < nh; ++x) {
+            const double v = ss[wave][tt * G + x][m];
+            best[e] = v > best[e] ? v : best[e];
+          }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
 #pragma unroll
-    for (int h = 0; h < HB; ++h)
-      if (h < nh && s[h] > best) best = s[h];
+    for (int e = 0; e < 4; ++e) {
+      const int tt = h + 4 * e;
+      if (tt < tp && t0 + tt < rr.count && c0 + m < F)
+        a.score[((int64_t)(rr.first + t0 + tt) * a.c.hkv + g) * a.fcap + c0 + m] = best[e];
+    }
   }
-  if (c0 + lane < F) a.score[((int64_t)r * a.c.hkv + g) * a.fcap + c0 + lane] = best;
 }
 
 // The selected blocks of a row and head, ascending: a radix selection over the scores as ordered 64-bit keys
@@ -795,10 +839,11 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
 }
 
 // ---- accumulated weights -------------------------------------------------------------------------
-// acc_j += sum over rows r of w_r exp(l_rj - lse_r): the S^T tiles of the attention again, without V, summed over
-// the 16 rows of a tile in the lanes that hold them.  K is read once, into registers (NT tiles of 32 rows per
-// wave), and the rows' Q tiles pass over it; a row of the cache belongs to one wave, so nothing is added in
-// an order that varies.
+// acc_j += sum over rows r of w_r exp(l_rj - lse_r).  K once, acc in and out once: memory bounds it while a head
+// has few rows.  The products are S = Q K^T here, Q as the first operand: lane (m, h) then holds row m of the
+// cache and 4 of the 16 rows of Q, so the sum over rows stays in one register per 16 cached rows until two
+// exchanges at the end (with S^T, as in the attention, 16 lanes hold each sum apart: 128 exchanges per 128 rows).
+// A row of the cache belongs to one wave, so nothing is added in an order that varies.
 struct WeightArgs {
   CacheView c;
   DraftView q;
@@ -806,51 +851,28 @@ struct WeightArgs {
   float *acc_out;
 };
 
-template <bool F32, int D>
+constexpr int kWeightRows = 1024, kRowsLds = 512;  // cached rows per workgroup; rows of Q whose factors LDS holds
+
+// NQ: 16-row tiles of Q kept in registers; 0: more rows than that, Q is read again for every 64 cached rows.
+template <bool F32, int D, int NQ>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
-  using T = Tile<F32, D>;
-  constexpr int KC = T::KC, E = F32 ? 4 : 2, NT = F32 ? 2 : 4;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int KC = D / 32, E = F32 ? 4 : 2, QP = F32 ? 2 : 1, NK = NQ ? NQ : 1;
+  constexpr int NU = F32 && D == 128 ? 2 : 4, RW = 16 * NU;  // 16-row pieces of K in a wave's step (registers)
+  __shared__ float sl[kRowsLds], sw[kRowsLds];
+  __shared__ int st[kRowsLds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4, g = blockIdx.y, b = blockIdx.z;
   const CacheView &c = a.c;
   const RowRange rr = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
   const int len = cache_len(c, b), total = len + rr.count < c.cap ? len + rr.count : c.cap;
-  const int j0 = (blockIdx.x * kWaves + wave) * NT * kTile;
-  if (j0 >= total || rr.count == 0) return;
+  const int first = blockIdx.x * kWeightRows;
+  if (first >= total || rr.count == 0) return;
   const int G = a.q.hq / c.hkv, nr = G * rr.count;
-  u32x4 k[NT][2][KC][T::CH];
-  bool ok[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    int j = j0 + n * kTile;
-    j = j < total ? j : j0;  // a tile behind the end: read as the first and not stored
-    const int p = page_of(c, j), id = page_id(c, b, p);
-    ok[n] = id >= 0;
-    const char *base = ok[n] ? c.k + k_offset(c, id, p, j, g) : c.k + g * c.sk_h;
-    int last = total - 1 - j < kTile - 1 ? total - 1 - j : kTile - 1;
-    if (!ok[n]) last = 0;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = 16 * u + m;
-      const char *q = base + (r < last ? r : last) * c.sk_t + h * (F32 ? 32 : 16);
-#pragma unroll
-      for (int x = 0; x < KC; ++x)
-#pragma unroll
-        for (int y = 0; y < T::CH; ++y) k[n][u][x][y] = *(const u32x4 *)(q + x * (F32 ? 128 : 64) + y * 16);
-    }
-  }
-  float sum[NT][8];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[n][e] = 0.f;
-  const bool edge = j0 + NT * kTile > len;
-  for (int r0 = 0; r0 < nr; r0 += 16) {
-    const bool mine = r0 + m < nr;
-    const int r = mine ? r0 + m : nr - 1, t = r / G, hh = g * G + r - t * G;
-    const int64_t row = rr.first + t;
-    const char *p = (const char *)a.q.q + (row * a.q.sq_t + hh * a.q.sq_h) * E + h * 8 * E;
-    u32x4 q[KC][F32 ? 2 : 1];
+  const int64_t at = ((int64_t)b * c.hkv + g) * c.cap;
+
+  auto load_q = [&](int r0, u32x4 (&q)[KC][QP]) {
+    const int r = r0 + m < nr ? r0 + m : nr - 1, t = r / G, hh = g * G + r - t * G;
+    const char *p = (const char *)a.q.q + ((rr.first + t) * a.q.sq_t + hh * a.q.sq_h) * E + h * 8 * E;
 #pragma unroll
     for (int x = 0; x < KC; ++x) {
       if constexpr (F32)
@@ -858,54 +880,121 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
       else
         q[x][0] = *(const u32x4 *)(p + x * 64);
     }
-    const float l2 = a.lse[(int64_t)hh * a.q.nrows + row] * kLog2e, w = mine ? (a.row_w ? a.row_w[row] : 1.f) : 0.f;
-    const bool on = w != 0.f && l2 != -__builtin_inff();
+  };
+  // 16 cached rows, lane m the m-th: rows behind the end are read as the last, without a page as row 0 of page 0
+  auto load_k = [&](int j0, u32x4 (&k)[KC][QP], bool &ok) {
+    const int p = page_of(c, j0), id = checked_page(c, c.table ? uload(c.table, (int64_t)b * c.max_pages + p) : b * c.max_pages + p);
+    ok = id >= 0;
+    const int r = j0 + m < total ? m : total - 1 - j0;
+    const char *x = (ok ? c.k + k_offset(c, id, p, j0, g) + r * c.sk_t : c.k + g * c.sk_h) + h * 8 * E;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      f32x4 s[2];
+    for (int i = 0; i < KC; ++i)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int y = 0; y < QP; ++y) k[i][y] = *(const u32x4 *)(x + i * 32 * E + 16 * y);
+  };
+
+  u32x4 q[NK][KC][QP];
+  if constexpr (NQ > 0)
 #pragma unroll
-        for (int x = 0; x < KC; ++x) {
-          if constexpr (F32) {
-            u32x4 kh, kl;
-            split8(__builtin_bit_cast(f32x4, k[n][u][x][0]), __builtin_bit_cast(f32x4, k[n][u][x][1]), kh, kl);
-            s[u] = mfma16(kl, q[x][0], s[u]);
-            s[u] = mfma16(kh, q[x][1], s[u]);
-            s[u] = mfma16(kh, q[x][0], s[u]);
-          } else {
-            s[u] = mfma16(k[n][u][x][0], q[x][0], s[u]);
-          }
+    for (int n = 0; n < NQ; ++n) load_q(16 * n, q[n]);
+
+  // one tile of 16 rows of Q (factors at r0 of LDS) against 16 cached rows; `plain`: every row counts and
+  // sees all of them
+  auto add = [&](const u32x4 (&qq)[KC][QP], const u32x4 (&kk)[KC][QP], int r0, int j0, float &sum) {
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < KC; ++x) {
+      if constexpr (F32) {
+        u32x4 kh, kl;
+        split8(__builtin_bit_cast(f32x4, kk[x][0]), __builtin_bit_cast(f32x4, kk[x][1]), kh, kl);
+        s = mfma16(qq[x][0], kl, s);
+        s = mfma16(qq[x][1], kh, s);
+        s = mfma16(qq[x][0], kh, s);
+      } else {
+        s = mfma16(qq[x][0], kk[x][0], s);
+      }
+    }
+    const f32x4 l2 = *(const f32x4 *)&sl[r0 + 4 * h], w = *(const f32x4 *)&sw[r0 + 4 * h];
+    const int i = j0 + m - len;  // drafted row, negative: a cached one
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bool see = w[e] != 0.f;
+      if (j0 + 16 > len) {
+        const int t = st[r0 + 4 * h + e];
+        if (i >= 0) {
+          bool v = i < rr.count && i <= t;
+          if (i < rr.count && a.q.mask) v = a.q.mask[(int64_t)(rr.first + t) * a.q.nwords + (i >> 5)] >> (i & 31) & 1;
+          see = see && v;
+        }
+      }
+      sum += see ? w[e] * exp2_fast(s[e] * a.q.c - l2[e]) : 0.f;
+    }
+  };
+
+  for (int base = 0; base < nr; base += kRowsLds) {  // (once, but for the widest groups of the most rows)
+    __syncthreads();
+    for (int x = tid; x < kRowsLds; x += 256) {
+      const int r = base + x, t = r < nr ? r / G : 0;
+      const float l = r < nr ? a.lse[(int64_t)(g * G + r - t * G) * a.q.nrows + rr.first + t] * kLog2e : 0.f;
+      const float w = r < nr ? (a.row_w ? a.row_w[rr.first + t] : 1.f) : 0.f;
+      sl[x] = l;
+      sw[x] = l == -__builtin_inff() ? 0.f : w;  // a row that sees nothing weighs nothing
+      st[x] = t;
+    }
+    __syncthreads();
+    const int rows = nr - base < kRowsLds ? nr - base : kRowsLds;
+    const int end = total - first < kWeightRows ? total : first + kWeightRows;
+    u32x4 k[NU][KC][QP], kn[NU][KC][QP];
+    bool ok[NU], okn[NU];
+    // RW cached rows per wave and step, the next in flight
+    auto fetch = [&](int j0, u32x4 (&x)[NU][KC][QP], bool (&o)[NU]) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) load_k(j0 + 16 * u < end ? j0 + 16 * u : j0, x[u], o[u]);
+    };
+    auto step = [&](int j0, const u32x4 (&x)[NU][KC][QP], const bool (&o)[NU]) {
+      float sum[NU] = {};
+      if constexpr (NQ > 0) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int u = 0; u < NU; ++u) add(q[n], x[u], 16 * n, j0 + 16 * u, sum[u]);
+      } else {
+        for (int r0 = 0; r0 < rows; r0 += 16) {
+          load_q(base + r0, q[0]);
+#pragma unroll
+          for (int u = 0; u < NU; ++u) add(q[0], x[u], r0, j0 + 16 * u, sum[u]);
         }
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        bool see = on;
-        if (edge) {
-          const int i = j0 + n * kTile + 16 * (e >> 2) + 4 * h + (e & 3) - len;
-          if (i >= 0) {
-            bool v = i < rr.count && i <= t;
-            if (i < rr.count && a.q.mask) v = a.q.mask[row * a.q.nwords + (i >> 5)] >> (i & 31) & 1;
-            see = see && v;
-          }
-        }
-        const float x = w * exp2_fast(s[e >> 2][e & 3] * a.q.c - l2);
-        sum[n][e] += see ? x : 0.f;
+      for (int u = 0; u < NU; ++u) sum[u] = sum4(sum[u]);
+      // lane (m, h) writes row 16 h + m
+      float x0 = sum[0];
+      bool has = o[0];
+#pragma unroll
+      for (int u = 1; u < NU; ++u) {
+        x0 = h == u ? sum[u] : x0;
+        has = h == u ? o[u] : has;
       }
+      const int j = j0 + lane;
+      if (lane < RW && j < end && has) {
+        const float in = base ? a.acc_out[at + j] : a.acc_in ? a.acc_in[at + j] : 0.f;
+        a.acc_out[at + j] = in + x0;
+      }
+    };
+    int j = first + wave * RW;
+    if (j >= end) continue;
+    fetch(j, k, ok);
+    while (true) {
+      if (j + 4 * RW < end) fetch(j + 4 * RW, kn, okn);
+      step(j, k, ok);
+      j += 4 * RW;
+      if (j >= end) break;
+      if (j + 4 * RW < end) fetch(j + 4 * RW, k, ok);
+      step(j, kn, okn);
+      j += 4 * RW;
+      if (j >= end) break;
     }
   }
-  const int64_t at = ((int64_t)b * c.hkv + g) * c.cap;
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = sum[n][e];
-#pragma unroll
-      for (int y = 1; y < 16; y <<= 1) x += __shfl_xor(x, y);
-      const int j = j0 + n * kTile + 16 * (e >> 2) + 4 * h + (e & 3);
-      if (m == (e & 15) && j < total && ok[n]) a.acc_out[at + j] = (a.acc_in ? a.acc_in[at + j] : 0.f) + x;
-    }
 }
 
 // ---- launches --------------------------------------------------------------------------------------
@@ -1032,9 +1121,9 @@ rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d,
   a.o = (char *)o, a.so_t = so_t, a.so_h = so_h, a.lse = lse;
   a.list = sel.list, a.nsel = nsel;
   if (sel.fcap > nsel) {
-    const dim3 grid(q.nrows, c.hkv, (sel.fcap + 63) / 64);
-    f32 ? (d == 128 ? score_kernel<true, 128><<<grid, 64, 0, st>>>(sel) : score_kernel<true, 64><<<grid, 64, 0, st>>>(sel))
-        : (d == 128 ? score_kernel<false, 128><<<grid, 64, 0, st>>>(sel) : score_kernel<false, 64><<<grid, 64, 0, st>>>(sel));
+    const dim3 grid((sel.fcap + 63) / 64, c.hkv, c.nseq);
+    f32 ? (d == 128 ? score_kernel<true, 128><<<grid, 256, 0, st>>>(sel) : score_kernel<true, 64><<<grid, 256, 0, st>>>(sel))
+        : (d == 128 ? score_kernel<false, 128><<<grid, 256, 0, st>>>(sel) : score_kernel<false, 64><<<grid, 256, 0, st>>>(sel));
   }
   select_kernel<<<dim3(q.nrows, c.hkv), kSelThreads, 0, st>>>(sel);
   return attend<true>(a, s, f32, d, st);
@@ -1042,11 +1131,21 @@ rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d,
 
 rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d, const float *lse, const float *row_w,
                          const float *acc_in, float *acc_out, hipStream_t st) {
-  WeightArgs a{c, q, lse, row_w, acc_in, acc_out};
-  const int rows = (f32 ? 2 : 4) * kTile * kWaves;
-  const dim3 grid((c.cap + rows - 1) / rows, c.hkv, c.nseq);
-  f32 ? (d == 128 ? weights_kernel<true, 128><<<grid, 256, 0, st>>>(a) : weights_kernel<true, 64><<<grid, 256, 0, st>>>(a))
-      : (d == 128 ? weights_kernel<false, 128><<<grid, 256, 0, st>>>(a) : weights_kernel<false, 64><<<grid, 256, 0, st>>>(a));
+  const WeightArgs a{c, q, lse, row_w, acc_in, acc_out};
+  const dim3 grid((c.cap + kWeightRows - 1) / kWeightRows, c.hkv, c.nseq);
+  const int rows = q.hq / c.hkv * q.max_rows;
+  auto run = [&](auto x, auto dd) {
+    constexpr bool F = decltype(x)::value;
+    constexpr int DD = decltype(dd)::value;
+    if (rows <= 16)
+      weights_kernel<F, DD, 1><<<grid, 256, 0, st>>>(a);
+    else if (rows > 32 || F)
+      weights_kernel<F, DD, 0><<<grid, 256, 0, st>>>(a);
+    else if constexpr (!F)
+      weights_kernel<F, DD, 2><<<grid, 256, 0, st>>>(a);
+  };
+  auto with_d = [&](auto x) { d == 128 ? run(x, std::integral_constant<int, 128>{}) : run(x, std::integral_constant<int, 64>{}); };
+  f32 ? with_d(std::true_type{}) : with_d(std::false_type{});
   RS_HIP(hipGetLastError());
   return RS_OK;
 }
