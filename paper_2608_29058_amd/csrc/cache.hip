@@ -167,9 +167,9 @@ __global__ void commit_len_kernel(CacheView c, const int32_t *naccept, int max_n
 }
 
 // ---- eviction ------------------------------------------------------------------------------
-// Plan, one workgroup per sequence and head: the `budget` first rows of the order (firm rows, then acc
-// descending, then row ascending) are found by a radix selection over 32-bit keys with the counts in LDS,
-// the rows read again from cache in each pass.  The first digit has 12 bits: weights lie in a few
+// Plan, one workgroup per sequence and head (or several, below): the `budget` first rows of the order (firm
+// rows, then acc descending, then row ascending) are found by a radix selection over 32-bit keys with the counts
+// in LDS, the rows read again from cache in each pass.  The first digit has 12 bits: weights lie in a few
 // octaves, and with 8 bits nearly all of a wave's counts would go to the same word.  One more pass lists,
 // in row order, the places before the budget whose row goes and the rows behind it that stay.
 struct EvictPlan {
@@ -186,100 +186,256 @@ __device__ __forceinline__ uint32_t evict_key(float a, int pos, int nsink, int f
   return pos < nsink || pos >= firm_from ? 0xffffffffu : float_key(a);
 }
 
+// The bin in which the count from the highest key down reaches `need`: pick = {bin, rows of it that still
+// stay, rows in it}.  Thread t counts the t-th highest group of bins.
+__device__ __forceinline__ void pick_bin(const int *hist, int bins, int need, int *sw, int *pick) {
+  const int per = bins / kPlanThreads, top = bins - 1 - (int)threadIdx.x * per;
+  int sum = 0, all;
+  for (int x = 0; x < per; ++x) sum += hist[top - x];
+  int before = block_scan<kPlanThreads>(sum, sw, &all);
+  if (before < need && before + sum >= need) {
+    int x = top;
+    while (before + hist[x] < need) before += hist[x--];
+    pick[0] = x;
+    pick[1] = need - before;
+    pick[2] = hist[x];
+  }
+  __syncthreads();
+}
+
+// Counts of the digit (key >> sh) & (bins - 1) of the rows [lo, hi) whose leading digits are `prefix`.
+__device__ __forceinline__ void count_digit(const float *acc, const int *pos, int lo, int hi, int nsink, int firm_from,
+                                            uint32_t prefix, uint32_t have, int sh, int bins, int *hist) {
+  constexpr int kPer = 8;
+  const int tid = threadIdx.x;
+  for (int x = tid; x < bins; x += kPlanThreads) hist[x] = 0;
+  __syncthreads();
+  for (int j0 = lo + tid; j0 < hi; j0 += kPlanThreads * kPer) {
+    float x[kPer];
+    int y[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int j = j0 + u * kPlanThreads < hi ? j0 + u * kPlanThreads : j0;
+      x[u] = acc[j];
+      y[u] = pos[j];
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const uint32_t key = evict_key(x[u], y[u], nsink, firm_from);
+      if (j0 + u * kPlanThreads < hi && (key & have) == prefix) atomicAdd(&hist[(key >> sh) & (bins - 1)], 1);
+    }
+  }
+  __syncthreads();
+}
+
+// What is known of the budget-th largest key: its digits (those under `have`), how many rows share them
+// and how many of these still stay.
+struct Border {
+  uint32_t prefix, have;
+  int need, equal;
+};
+constexpr int kBins = 4096;  // bins of a digit at most
+__device__ __forceinline__ int digit_bins(int pass) { return pass ? 1024 : 4096; }
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 20 : pass == 1 ? 10 : 0; }
+
+// Lists, in row order, the places of [lo, hi) before the budget whose row goes and the rows behind it that
+// stay.  Before lo: `ranked` rows equal to the border's, `holes` such places and `movers` such rows.
+__device__ void list_moves(const float *acc, const int *pos, int lo, int hi, int budget, int nsink, int firm_from,
+                           const Border &bd, int ranked, int &holes, int &movers, int *hole_out, int *mover_out, int *sw) {
+  constexpr int kPer = 8;  // pieces of 64 consecutive rows per wave and step
+  const bool ties = bd.need < bd.equal;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t below = (1ull << lane) - 1;
+  // x of the waves before this one, and of all
+  auto scan = [&](int x, int &all) {
+    if (lane == 0) sw[wave] = x;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanThreads / 64; ++k) {
+      const int y = sw[k];
+      before += k < wave ? y : 0;
+      all += y;
+    }
+    __syncthreads();
+    return before;
+  };
+  for (int j0 = lo; j0 < hi; j0 += kPlanThreads * kPer) {
+    const int jw = j0 + wave * 64 * kPer + lane;
+    float a[kPer];
+    int q[kPer], all;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int j = jw + 64 * x < hi ? jw + 64 * x : hi - 1;
+      a[x] = acc[j];
+      q[x] = pos[j];
+    }
+    uint32_t key[kPer];
+    uint64_t eq[kPer];
+    int e = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      key[x] = evict_key(a[x], q[x], nsink, firm_from) & bd.have;
+      eq[x] = __ballot(jw + 64 * x < hi && key[x] == bd.prefix);
+      e += __popcll(eq[x]);
+    }
+    int at = 0;
+    if (ties) {
+      at = ranked + scan(e, all);
+      ranked += all;
+    }
+    uint64_t hole[kPer], mover[kPer];
+    int hm = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int j = jw + 64 * x;
+      const bool same = key[x] == bd.prefix;
+      const bool stay = key[x] > bd.prefix || (same && (!ties || at + __popcll(eq[x] & below) < bd.need));
+      at += __popcll(eq[x]);
+      hole[x] = __ballot(j < hi && j < budget && !stay);
+      mover[x] = __ballot(j < hi && j >= budget && stay);
+      hm += __popcll(hole[x]) | __popcll(mover[x]) << 16;  // at most 8192 of each in a step
+    }
+    const int before = scan(hm, all);
+    int h = holes + (before & 0xffff), m = movers + (before >> 16);
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      if (hole[x] >> lane & 1) hole_out[h + __popcll(hole[x] & below)] = jw + 64 * x;
+      if (mover[x] >> lane & 1) mover_out[m + __popcll(mover[x] & below)] = jw + 64 * x;
+      h += __popcll(hole[x]);
+      m += __popcll(mover[x]);
+    }
+    holes += all & 0xffff;
+    movers += all >> 16;
+  }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(CacheView c, int budget, int nsink, int nrecent, EvictPlan pl) {
-  constexpr int kBins = 4096, kPer = 8;  // bins of a pass at most; consecutive rows per thread and step of the last
   __shared__ int hist[kBins], sw[kPlanThreads / 64], pick[3];
-  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.y, g = blockIdx.x;
   const int64_t item = (int64_t)b * c.hkv + g;
   const int n = cache_len(c, b);
   if (n <= budget) {
-    if (tid == 0) pl.count[item] = -1;
+    if (threadIdx.x == 0) pl.count[item] = -1;
     return;
   }
   const float *acc = c.acc + item * c.cap;
   const int *pos = c.pos + item * c.cap;
   const int seen = c.seen[b], firm_from = (seen > 0 ? seen : 0) - nrecent;
-  // the budget-th largest key: its digits found so far (those under `have`), how many rows share them,
-  // and how many of these still stay
-  uint32_t prefix = 0, have = 0;
-  int need = budget, equal = n, all;
-  for (int pass = 0; pass < 3 && need < equal; ++pass) {
-    const int bits = pass ? 10 : 12, sh = pass == 0 ? 20 : pass == 1 ? 10 : 0, bins = 1 << bits;
-    for (int x = tid; x < bins; x += kPlanThreads) hist[x] = 0;
-    __syncthreads();
-    for (int j0 = tid; j0 < n; j0 += kPlanThreads * kPer) {
-      float x[kPer];
-      int y[kPer];
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        const int j = j0 + u * kPlanThreads < n ? j0 + u * kPlanThreads : j0;
-        x[u] = acc[j];
-        y[u] = pos[j];
-      }
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        const uint32_t key = evict_key(x[u], y[u], nsink, firm_from);
-        if (j0 + u * kPlanThreads < n && (key & have) == prefix) atomicAdd(&hist[(key >> sh) & (bins - 1)], 1);
-      }
-    }
-    __syncthreads();
-    // thread t counts the t-th highest group of bins; the one where the count reaches `need` picks
-    const int per = bins / kPlanThreads, top = bins - 1 - tid * per;
-    int sum = 0;
-    for (int x = 0; x < per; ++x) sum += hist[top - x];
-    int before = block_scan<kPlanThreads>(sum, sw, &all);
-    if (before < need && before + sum >= need) {
-      int x = top;
-      while (before + hist[x] < need) before += hist[x--];
-      pick[0] = x;
-      pick[1] = need - before;
-      pick[2] = hist[x];
-    }
-    __syncthreads();
-    prefix |= (uint32_t)pick[0] << sh;
-    have |= (uint32_t)(bins - 1) << sh;
-    need = pick[1];
-    equal = pick[2];
+  Border bd{0, 0, budget, n};
+  for (int pass = 0; pass < 3 && bd.need < bd.equal; ++pass) {
+    const int bins = digit_bins(pass), sh = digit_shift(pass);
+    count_digit(acc, pos, 0, n, nsink, firm_from, bd.prefix, bd.have, sh, bins, hist);
+    pick_bin(hist, bins, bd.need, sw, pick);
+    bd = Border{bd.prefix | (uint32_t)pick[0] << sh, bd.have | (uint32_t)(bins - 1) << sh, pick[1], pick[2]};
     __syncthreads();
   }
-  // rows above `prefix` stay, and the first `need` of those that share it
-  const bool ties = need < equal;
-  int ranked = 0, holes = 0, movers = 0;
-  for (int j0 = 0; j0 < n; j0 += kPlanThreads * kPer) {
-    const int jt = j0 + tid * kPer;
-    uint32_t key[kPer];
-    int e = 0;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      key[x] = jt + x < n ? evict_key(acc[jt + x], pos[jt + x], nsink, firm_from) & have : 0;
-      e += jt + x < n && key[x] == prefix;
-    }
-    int at = 0;
-    if (ties) {
-      at = ranked + block_scan<kPlanThreads>(e, sw, &all);
-      ranked += all;
-    }
-    uint32_t hole = 0, mover = 0;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int j = jt + x;
-      const bool eq = key[x] == prefix;
-      const bool stay = j < n && (key[x] > prefix || (eq && (!ties || at < need)));
-      at += eq;
-      hole |= (uint32_t)(j < budget && !stay) << x;
-      mover |= (uint32_t)(j >= budget && stay) << x;
-    }
-    const int hm = block_scan<kPlanThreads>(__popc(hole) | (__popc(mover) << 16), sw, &all);  // at most 8192 of each in a step
-    int h = holes + (hm & 0xffff), m = movers + (hm >> 16);
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      if (hole >> x & 1) pl.hole[item * pl.most + h++] = jt + x;
-      if (mover >> x & 1) pl.mover[item * pl.most + m++] = jt + x;
-    }
-    holes += all & 0xffff;
-    movers += all >> 16;
+  int holes = 0, movers = 0;
+  list_moves(acc, pos, 0, n, budget, nsink, firm_from, bd, 0, holes, movers, pl.hole + item * pl.most, pl.mover + item * pl.most, sw);
+  if (threadIdx.x == 0) pl.count[item] = movers;
+}
+
+// The same with the rows of an item cut into slices, a workgroup each: one workgroup reads 8 bytes per row and
+// pass at the rate of one CU (two sequences of 128K rows and 8 heads: 197 us).  Slices do not cross the budget,
+// so that one has either places or movers.  A launch per digit: it adds up the slices' counts of the digit
+// before (every workgroup for itself), finds the border's next bin, notes how many of the rows above and in it
+// lie in earlier slices, and counts its own slice's next digit.  The last launch lists.
+struct EvictSlices {
+  uint16_t *hist;   // [item][slice][3 digits: 4096, 1024, 1024]
+  Border *border;   // [item][3], after each digit
+  int *above;       // [2][item][slice + 1][2] after the first and second digit: rows above the border so far, and
+                    // equal to it, in earlier slices; last those of all slices before the budget
+  int nslice, n1, rows;  // slices per item, those before the budget, rows of a slice
+};
+constexpr int kSliceBins = 4096 + 1024 + 1024;
+__device__ __forceinline__ int digit_first(int pass) { return pass == 0 ? 0 : pass == 1 ? 4096 : 5120; }
+
+// PASS 0, 1, 2: counts that digit; 3: lists.
+template <int PASS>
+__global__ __launch_bounds__(kPlanThreads) void evict_slice_kernel(CacheView c, int budget, int nsink, int nrecent, EvictPlan pl,
+                                                                   EvictSlices sl) {
+  __shared__ int hist[kBins], sw[kPlanThreads / 64], pick[3], part[4];
+  const int s = blockIdx.x, g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int64_t item = (int64_t)b * c.hkv + g;
+  const int n = cache_len(c, b);
+  if (n <= budget) {
+    if (PASS == 3 && s == 0 && tid == 0) pl.count[item] = -1;
+    return;
   }
-  if (tid == 0) pl.count[item] = movers;
+  const float *acc = c.acc + item * c.cap;
+  const int *pos = c.pos + item * c.cap;
+  const int seen = c.seen[b], firm_from = (seen > 0 ? seen : 0) - nrecent;
+  const int lo = s < sl.n1 ? s * sl.rows : budget + (s - sl.n1) * sl.rows;
+  int hi = lo + sl.rows;
+  hi = s < sl.n1 ? (hi < budget ? hi : budget) : (hi < n ? hi : n);
+  Border bd{0, 0, budget, n};
+  const int64_t items = (int64_t)c.nseq * c.hkv;
+  auto above_at = [&](int pass, int x) { return sl.above + ((pass * items + item) * (sl.nslice + 1) + x) * 2; };
+  int above[2] = {0, 0}, equal[2] = {0, 0};  // of earlier slices, and of all slices before the budget
+  if constexpr (PASS > 1) {
+    bd = sl.border[item * 3 + PASS - 2];
+    const int *w = above_at(PASS - 2, s), *w1 = above_at(PASS - 2, sl.nslice);
+    above[0] = w[0], equal[0] = w[1];
+    above[1] = w1[0], equal[1] = w1[1];
+  }
+  if constexpr (PASS > 0) {
+    if (PASS == 1 || bd.need < bd.equal) {
+      constexpr int bins = PASS == 1 ? 4096 : 1024, sh = PASS == 1 ? 20 : PASS == 2 ? 10 : 0, per = bins / kPlanThreads;
+      const uint16_t *h = sl.hist + item * sl.nslice * kSliceBins + digit_first(PASS - 1);
+      int before[4] = {0, 0, 0, 0}, first[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0};  // of bins tid, tid + 1024, ...
+#pragma unroll 6
+      for (int x = 0; x < sl.nslice; ++x)
+#pragma unroll
+        for (int u = 0; u < per; ++u) {
+          const int v = h[(int64_t)x * kSliceBins + tid + u * kPlanThreads];
+          all[u] += v;
+          before[u] += x < s ? v : 0;
+          first[u] += x < sl.n1 ? v : 0;
+        }
+      for (int u = 0; u < per; ++u) hist[tid + u * kPlanThreads] = all[u];
+      if (tid < 4) part[tid] = 0;
+      __syncthreads();
+      pick_bin(hist, bins, bd.need, sw, pick);
+      int p0 = 0, p1 = 0;
+      for (int u = 0; u < per; ++u) {
+        const int x = tid + u * kPlanThreads;
+        p0 += x > pick[0] ? before[u] : 0;
+        p1 += x > pick[0] ? first[u] : 0;
+        if (x == pick[0]) part[2] = before[u], part[3] = first[u];
+      }
+      if (p0) atomicAdd(&part[0], p0);
+      if (p1) atomicAdd(&part[1], p1);
+      __syncthreads();
+      bd = Border{bd.prefix | (uint32_t)pick[0] << sh, bd.have | (uint32_t)(bins - 1) << sh, pick[1], pick[2]};
+      for (int k = 0; k < 2; ++k) above[k] += part[k], equal[k] = part[2 + k];
+      __syncthreads();
+    }
+    if constexpr (PASS < 3)
+      if (tid == 0) {
+        int *w = above_at(PASS - 1, s);
+        w[0] = above[0], w[1] = equal[0];
+        if (s == 0) {
+          sl.border[item * 3 + PASS - 1] = bd;
+          w = above_at(PASS - 1, sl.nslice);
+          w[0] = above[1], w[1] = equal[1];
+        }
+      }
+  }
+  if constexpr (PASS < 3) {
+    if (PASS > 0 && bd.need == bd.equal) return;  // the border is known
+    const int bins = digit_bins(PASS), sh = digit_shift(PASS);
+    count_digit(acc, pos, lo, hi, nsink, firm_from, bd.prefix, bd.have, sh, bins, hist);
+    uint16_t *h = sl.hist + (item * sl.nslice + s) * kSliceBins + digit_first(PASS);
+    for (int x = tid; x < bins; x += kPlanThreads) h[x] = (uint16_t)hist[x];
+  } else {
+    const int kept = above[0] + (equal[0] < bd.need ? equal[0] : bd.need);    // rows that stay in earlier slices,
+    const int kept1 = above[1] + (equal[1] < bd.need ? equal[1] : bd.need);   // and before the budget
+    int holes = s < sl.n1 ? lo - kept : 0, movers = s < sl.n1 ? 0 : kept - kept1;
+    list_moves(acc, pos, lo, hi, budget, nsink, firm_from, bd, equal[0], holes, movers, pl.hole + item * pl.most,
+               pl.mover + item * pl.most, sw);
+    if (s == 0 && tid == 0) pl.count[item] = budget - kept1;
+  }
 }
 
 // The planned moves: places before the budget receive rows behind it, so nothing is read that is written.
@@ -338,6 +494,22 @@ EvictPlan plan_at(Arena &a, int64_t items, int budget, int cap) {
   return pl;
 }
 
+// Slices of 8K rows (their counts fit 16 bits) where a cache is long enough for more than two of them; 16 at most
+// to add up for the longest.
+constexpr int kSliceRows = 8192;
+EvictSlices slices_at(Arena &a, int64_t items, int budget, int cap) {
+  EvictSlices sl{};
+  if (cap <= 2 * kSliceRows) return sl;
+  const int r = (cap + 15) / 16;
+  sl.rows = r > kSliceRows ? r : kSliceRows;
+  sl.n1 = (budget + sl.rows - 1) / sl.rows;
+  sl.nslice = sl.n1 + (cap - budget + sl.rows - 1) / sl.rows;
+  sl.hist = a.take<uint16_t>((size_t)items * sl.nslice * kSliceBins);
+  sl.border = a.take<Border>((size_t)items * 3);
+  sl.above = a.take<int>((size_t)items * (sl.nslice + 1) * 4);
+  return sl;
+}
+
 int log2i(int x) { return 31 - __builtin_clz((unsigned)x); }
 
 template <typename F>
@@ -379,6 +551,7 @@ rs_status commit_launch(const CacheView &c, int dtype, int d, const int32_t *nac
 size_t evict_ws_bytes(int64_t items, int budget, int cap) {
   Arena a(nullptr, 0);
   plan_at(a, items, budget, cap);
+  if (budget < cap) slices_at(a, items, budget, cap);
   return a.off + 256;
 }
 
@@ -387,9 +560,18 @@ rs_status evict_launch(const CacheView &c, int dtype, int d, int budget, int nsi
   if (budget >= c.cap) return RS_OK;  // no sequence can hold more
   Arena a(ws, ws_bytes);
   const EvictPlan pl = plan_at(a, (int64_t)c.nseq * c.hkv, budget, c.cap);
+  const EvictSlices sl = slices_at(a, (int64_t)c.nseq * c.hkv, budget, c.cap);
   if (!ws || !a.ok())
     return fail(RS_ERR_WORKSPACE, "eviction workspace too small: need " + std::to_string(evict_ws_bytes((int64_t)c.nseq * c.hkv, budget, c.cap)));
-  evict_plan_kernel<<<dim3(c.hkv, c.nseq), kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+  if (sl.nslice) {
+    const dim3 grid(sl.nslice, c.hkv, c.nseq);
+    evict_slice_kernel<0><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
+    evict_slice_kernel<1><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
+    evict_slice_kernel<2><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
+    evict_slice_kernel<3><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
+  } else {
+    evict_plan_kernel<<<dim3(c.hkv, c.nseq), kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+  }
   const int e = dtype == RS_BF16 ? 2 : 4;
   evict_move_kernel<<<dim3((pl.most + kMoveRows - 1) / kMoveRows, c.hkv, c.nseq), 256, 0, st>>>(c, budget, pl, log2i(d * e / 16));
   if (c.kmean && budget >= 64)

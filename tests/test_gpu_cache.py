@@ -207,13 +207,26 @@ def test_evict_with_equal_weights(kind):
     check_evicted(s, bk, [5000, 700], 600, 3, 50)
 
 
-def test_long_cache_evicts_to_a_short_one():
+@pytest.mark.parametrize("lens,budget,nsink,nrecent,kind", [
+    ([70001, 8193], 8192, 100, 1000, "random"),
+    ([40000, 17000], 20001, 0, 7, "few"),        # ties across slices of rows, on both sides of the budget
+    ([33333], 33332, 5, 300, "tiny"),
+    ([20000, 100, 16500], 100, 4, 10, "equal"),
+    ([150000], 60000, 0, 0, "random"),           # slices longer than 8K rows
+])
+def test_long_caches(lens, budget, nsink, nrecent, kind):
     import torch
-    s = Setup(4, [70001], [0], hq=1, hkv=1, d=64, page=1024)
+    s = Setup(4, lens, [0] * len(lens), hq=1, hkv=1, d=64, page=1024)
     bk = Book(s, 3)
+    r = np.random.default_rng(9)
+    n = bk.acc.shape
+    if kind != "random":
+        bk.acc = {"equal": np.full(n, 0.25), "few": r.choice([0.5, 0.25, 3.0], n),
+                  "tiny": 1.0 + r.integers(0, 900, n) * 2.0 ** -23}[kind].astype(np.float32)
+        bk.dacc.copy_(torch.from_numpy(bk.acc))
     c = s.cache(**bk.args())
-    _rs.rs_cache_evict(c, 8192, 100, 1000, _rs.workspace(_rs.rs_cache_evict_workspace_size(c, 8192)))
-    check_evicted(s, bk, [70001], 8192, 100, 1000)
+    _rs.rs_cache_evict(c, budget, nsink, nrecent, _rs.workspace(_rs.rs_cache_evict_workspace_size(c, budget)))
+    check_evicted(s, bk, lens, budget, nsink, nrecent)
 
 
 def test_evict_skips_rows_without_a_page_and_replays():
