@@ -28,10 +28,20 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 }
 
 // Values of lanes i, i ^ 16, i ^ 32 and i ^ 48 joined, in all four.
+// (elements are copied out first: __builtin_bit_cast of a vector's element reads element 0)
+__device__ __forceinline__ void halves(u32x2 r, float &a, float &b) {
+  const uint32_t x = r[0], y = r[1];
+  a = __builtin_bit_cast(float, x);
+  b = __builtin_bit_cast(float, y);
+}
 template <typename F>
 __device__ __forceinline__ float join4(float x, F f) {
-  x = f(x, __shfl_xor(x, 16));
-  return f(x, __shfl_xor(x, 32));
+  float a, b;
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  halves(__builtin_amdgcn_permlane32_swap(u, u, false, false), a, b);
+  const uint32_t v = __builtin_bit_cast(uint32_t, f(a, b));
+  halves(__builtin_amdgcn_permlane16_swap(v, v, false, false), a, b);
+  return f(a, b);
 }
 __device__ __forceinline__ float max4(float x) { return join4(x, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float sum4(float x) { return join4(x, [](float a, float b) { return a + b; }); }
@@ -76,6 +86,19 @@ struct TileAt {
   bool ok;    // the table names a page
 };
 
+// The tile from row j of sequence b and head g, whose rows end before `total`.  Without a page: row 0 of page 0,
+// to be masked.
+__device__ __forceinline__ TileAt tile_at(const CacheView &c, int b, int g, int j, int total) {
+  const int p = page_of(c, j);
+  const int id = checked_page(c, c.table ? uload(c.table, (int64_t)b * c.max_pages + p) : b * c.max_pages + p);
+  TileAt at;
+  at.ok = id >= 0;
+  at.k = c.k + (at.ok ? k_offset(c, id, p, j, g) : g * c.sk_h);
+  at.v = c.v + (at.ok ? v_offset(c, id, p, j, g) : g * c.sv_h);
+  at.last = !at.ok ? 0 : total - 1 - j < kTile - 1 ? total - 1 - j : kTile - 1;
+  return at;
+}
+
 template <bool F32, int D>
 __device__ __forceinline__ void load_k(Tile<F32, D> &t, const TileAt &at, int64_t sk, int m, int h) {
 #pragma unroll
@@ -112,15 +135,168 @@ __device__ __forceinline__ void load_v(Tile<F32, D> &t, const TileAt &at, int64_
 
 // The operand V^T of output tile t: dimension DT * m + t of the lane's 8 rows (lo: fp32 only).
 template <bool F32, int D>
-__device__ __forceinline__ void v_operand(const Tile<F32, D> &T, int t, u32x4 &hi, u32x4 &lo) {
+__device__ __forceinline__ void v_operand(const uint32_t (&v)[8][Tile<F32, D>::VW], int t, u32x4 &hi, u32x4 &lo) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (F32) {
       uint32_t x, y;
-      split2(__builtin_bit_cast(float, T.v[2 * i][t]), __builtin_bit_cast(float, T.v[2 * i + 1][t]), x, y);
+      split2(__builtin_bit_cast(float, v[2 * i][t]), __builtin_bit_cast(float, v[2 * i + 1][t]), x, y);
       hi[i] = x, lo[i] = y;
     } else {
-      hi[i] = __builtin_amdgcn_perm(T.v[2 * i + 1][t / 2], T.v[2 * i][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
+      hi[i] = __builtin_amdgcn_perm(v[2 * i + 1][t / 2], v[2 * i][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
+    }
+  }
+}
+
+__device__ __forceinline__ bool page_ok(const CacheView &c, int b, int j) {
+  const int p = page_of(c, j);
+  return checked_page(c, c.table ? uload(c.table, (int64_t)b * c.max_pages + p) : b * c.max_pages + p) >= 0;
+}
+
+// Barrier after this wave's LDS accesses; loads from memory stay in flight.
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// What the drafted rows of an item are: its sequence's lengths and rows.
+struct RowsOf {
+  const DraftView *q;
+  int len, total, t, first;  // cached rows; with the drafted ones; new rows and the first of them
+};
+
+// The weights of a tile of 32 cached rows from row j for NQ x 16 rows of Q: raises the running maxima (and
+// rescales sums and O), adds to the sums, and leaves P as the operand of the product with V.  edge: a tile that
+// some row may not see in whole (its end, drafted rows, no page); pvis is then 1 for what a row sees.
+template <bool F32, int D, int NQ>
+__device__ __forceinline__ void weigh_tile(const u32x4 (&k)[2][D / 32][F32 ? 2 : 1], const u32x4 (&q)[NQ][D / 32][F32 ? 2 : 1],
+                                           const RowsOf &ro, const int (&tq)[NQ], int j, int h, bool ok, bool edge,
+                                           float (&mx)[NQ], float (&sum)[NQ], f32x4 (&oacc)[NQ][D / 16], u32x4 (&pb)[NQ],
+                                           u32x4 (&pvis)[NQ]) {
+  constexpr int KC = D / 32, DT = D / 16;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    f32x4 s[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        if constexpr (F32) {
+          u32x4 kh, kl;
+          split8(__builtin_bit_cast(f32x4, k[u][x][0]), __builtin_bit_cast(f32x4, k[u][x][1]), kh, kl);
+          s[u] = mfma16(kl, q[n][x][0], s[u]);
+          s[u] = mfma16(kh, q[n][x][1], s[u]);
+          s[u] = mfma16(kh, q[n][x][0], s[u]);
+        } else {
+          s[u] = mfma16(k[u][x][0], q[n][x][0], s[u]);
+        }
+      }
+    }
+    const float c = ro.q->c;
+    if (edge) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = j + 16 * u + 4 * h + e - ro.len;  // drafted row, negative: a cached one
+          bool see = i < 0 || (i < ro.t && i <= tq[n]);
+          if (i >= 0 && i < ro.t && ro.q->mask)
+            see = ro.q->mask[(int64_t)(ro.first + tq[n]) * ro.q->nwords + (i >> 5)] >> (i & 31) & 1;
+          see = see && ok && j + 16 * u + 4 * h + e < ro.total;
+          s[u][e] = see ? s[u][e] : -__builtin_inff();
+        }
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        pvis[n][w] = (s[w >> 1][2 * (w & 1)] == -__builtin_inff() ? 0u : 0x3f80u) |
+                     (s[w >> 1][2 * (w & 1) + 1] == -__builtin_inff() ? 0u : 0x3f800000u);
+    }
+    // maxima and exponents in units of 2^x: c = scale log2(e) > 0 goes into the exponent's one FMA
+    float tm = -__builtin_inff();
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tm = fmaxf(tm, s[u][e]);
+    tm = fmaxf(max4(tm) * c, mx[n]);
+    if (__any(tm > mx[n])) {
+      const float al = tm == -__builtin_inff() ? 1.f : exp2_fast(mx[n] - tm);
+      mx[n] = tm;
+      sum[n] *= al;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) oacc[n][t] *= al;
+    }
+    const float base = mx[n] == -__builtin_inff() ? 0.f : mx[n];
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = exp2_fast(__builtin_fmaf(s[e >> 2][e & 3], c, -base));
+      sum[n] += p[e];
+    }
+    // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-8 of
+    // sum p |v| at most); its sum is taken before
+#pragma unroll
+    for (int w = 0; w < 4; ++w) pb[n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
+  }
+}
+
+// Whether a tile of V holds infinities or NaN: values that a zero weight does not silence.
+template <bool F32, int D>
+__device__ __forceinline__ bool any_special(const uint32_t (&v)[8][Tile<F32, D>::VW]) {
+  int bad = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int w = 0; w < Tile<F32, D>::VW; ++w) {
+      if constexpr (F32)
+        bad |= (v[i][w] & 0x7f800000u) == 0x7f800000u;
+      else
+        bad |= (v[i][w] & 0x7f80u) == 0x7f80u || (v[i][w] & 0x7f800000u) == 0x7f800000u;
+    }
+  return __any(bad);
+}
+
+// O^T += V^T P^T over a tile.  special: infinities and NaN count only where they are seen: finite values go
+// through the product, the others through products of 0 and 1 that tell which rows see one.
+template <bool F32, int D, int NQ>
+__device__ __forceinline__ void add_values(const uint32_t (&v)[8][Tile<F32, D>::VW], bool special, const u32x4 (&pb)[NQ],
+                                           const u32x4 (&pvis)[NQ], f32x4 (&oacc)[NQ][D / 16]) {
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {
+    u32x4 vh, vl;
+    v_operand<F32, D>(v, t, vh, vl);
+    if (special) {
+#pragma unroll
+      for (int kind = 0; kind < 3; ++kind) {
+        u32x4 one, clean = vh;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t o2 = 0, c2 = 0;
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const uint32_t x = vh[w] >> (16 * z) & 0xffffu;
+            const bool hit = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
+            o2 |= (hit ? 0x3f80u : 0u) << (16 * z);
+            c2 |= ((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) << (16 * z);
+          }
+          one[w] = o2;
+          clean[w] &= c2;
+          if (F32 && kind == 2) vl[w] &= c2;
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const f32x4 cnt = mfma16(one, pvis[n], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (cnt[e] > 0.f) oacc[n][t][e] += kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
+        }
+        if (kind == 2) vh = clean;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      if constexpr (F32) oacc[n][t] = mfma16(vl, pb[n], oacc[n][t]);
+      oacc[n][t] = mfma16(vh, pb[n], oacc[n][t]);
     }
   }
 }
@@ -139,7 +315,7 @@ struct DraftArgs {
   int64_t so_t, so_h;
   float *lse;
   float *po, *pml;   // pieces: O (unnormalised), then (max, sum) of every row
-  int rtiles;        // row tiles of a sequence with max_rows rows
+  int rtiles, trows; // row tiles of a sequence with max_rows rows, rows of one
   int slots;         // pieces that all items together may have beyond one each
   const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
   int nsel, pieces;  // with a list: pieces per item
@@ -212,14 +388,72 @@ __device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
   return false;
 }
 
+// ---- the end of a piece ---------------------------------------------------------------------------
+template <int D>
+constexpr int kLd = D + 4;  // a row of O in LDS, padded
+
+// A wave's O, maximum and sum of 16 rows into LDS (so: rows of kLd, sml: max and sum per row).
+template <int D>
+__device__ __forceinline__ void store_wave(float *so, float *sml, int m, int h, float mx, float sum, const f32x4 (&oacc)[D / 16]) {
+  const float z = sum4(sum);
+  if (h == 0) {
+    sml[2 * m] = mx;
+    sml[2 * m + 1] = z;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) so[m * kLd<D> + h * (D / 4) + e * (D / 16) + t] = oacc[t][e];
+}
+
+// Joins KW parts of `rows` rows each (part k at so + k rows kLd) and writes them: as the result where the item
+// has one piece, else as the piece `slot`.
+template <int D, int KW, int NT, bool SEL>
+__device__ __forceinline__ void join_waves(const DraftArgs &a, const Item &it, const float *so, const float *sml, int rows, int r0,
+                                           int nr, int G, int row_t0, int slot) {
+  for (int x = threadIdx.x; x < rows * (D / 4); x += NT) {
+    const int r = x / (D / 4), o4 = x % (D / 4) * 4;
+    if (r0 + r >= nr) continue;
+    float M = -__builtin_inff(), z = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) M = fmaxf(M, sml[(k * rows + r) * 2]);
+    const float base = M == -__builtin_inff() ? 0.f : M;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const float m = sml[(k * rows + r) * 2], w = exp2_fast(m - base);
+      z += w * sml[(k * rows + r) * 2 + 1];
+      const f32x4 p = *(const f32x4 *)&so[(k * rows + r) * kLd<D> + o4];
+      if (m != -__builtin_inff())
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w * p[e];
+    }
+    if (it.npieces == 1) {
+      const int t = SEL ? row_t0 : (r0 + r) / G, hh = it.g * G + (SEL ? r0 + r : r0 + r - t * G);
+      const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
+      u32x2 w2;
+      w2[0] = pack_bf16x2(v[0] * inv, v[1] * inv);
+      w2[1] = pack_bf16x2(v[2] * inv, v[3] * inv);
+      *(u32x2 *)(a.o + ((it.first + t) * a.so_t + hh * a.so_h + o4) * 2) = w2;
+      if (a.lse && o4 == 0)
+        a.lse[(int64_t)hh * a.q.nrows + it.first + t] = z == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(z)) * kLn2;
+    } else {
+      *(f32x4 *)(a.po + ((int64_t)slot * a.trows + r) * D + o4) = v;
+      if (o4 == 0) {
+        float *ml = a.pml + ((int64_t)slot * a.trows + r) * 2;
+        ml[0] = M;
+        ml[1] = z;
+      }
+    }
+  }
+}
+
 // NQ: 16-row tiles of Q per wave.
 template <bool F32, int D, int NQ, bool SEL>
 __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const DraftArgs a) {
   using T = Tile<F32, D>;
   constexpr int KC = T::KC, DT = T::DT, E = F32 ? 4 : 2, QP = F32 ? 2 : 1;
-  constexpr int LD = D + 4;  // row of O in LDS, padded
-  __shared__ float so[kWaves][16 * NQ][LD];
-  __shared__ float sml[kWaves][16 * NQ][2];
+  __shared__ float so[kWaves * 16 * NQ * kLd<D>], sml[kWaves * 16 * NQ * 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4;
   Item it;
@@ -309,150 +543,15 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
   };
   auto place = [&](int s, int &j) {
     j = __builtin_amdgcn_readfirstlane(row_of(s));
-    const int p = page_of(c, j);
-    const int raw = c.table ? uload(c.table, (int64_t)it.b * c.max_pages + p) : it.b * c.max_pages + p;
-    int id = checked_page(c, raw);
-    TileAt at;
-    at.ok = id >= 0;
-    id = at.ok ? id : 0;
-    at.k = c.k + k_offset(c, id, p, j, it.g);
-    at.v = c.v + v_offset(c, id, p, j, it.g);
-    at.last = total - 1 - j < kTile - 1 ? total - 1 - j : kTile - 1;
-    if (!at.ok) at.last = 0;  // page 0 has a row 0 ... and its rows are masked
-    if (!at.ok) {
-      at.k = c.k + it.g * c.sk_h;
-      at.v = c.v + it.g * c.sv_h;
-    }
-    return at;
+    return tile_at(c, it.b, it.g, j, total);
   };
 
+  const RowsOf ro{&a.q, len, total, it.t, it.first};
   auto compute = [&](T &kv, const TileAt &at, int j) {
-    // a tile that any row may not see in whole: its end, drafted rows, no page
     const bool edge = j + kTile > len || !at.ok;
     u32x4 pb[NQ], pvis[NQ];
-    bool odd = false;  // values that a zero weight does not silence, in an edge tile
-    if (edge) {
-      int bad = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int w = 0; w < T::VW; ++w) {
-          const uint32_t x = kv.v[i][w];
-          if constexpr (F32)
-            bad |= (x & 0x7f800000u) == 0x7f800000u;
-          else
-            bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-        }
-      odd = __any(bad);
-    }
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      f32x4 s[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < KC; ++x) {
-          if constexpr (F32) {
-            u32x4 kh, kl;
-            split8(__builtin_bit_cast(f32x4, kv.k[u][x][0]), __builtin_bit_cast(f32x4, kv.k[u][x][1]), kh, kl);
-            s[u] = mfma16(kl, q[n][x][0], s[u]);
-            s[u] = mfma16(kh, q[n][x][1], s[u]);
-            s[u] = mfma16(kh, q[n][x][0], s[u]);
-          } else {
-            s[u] = mfma16(kv.k[u][x][0], q[n][x][0], s[u]);
-          }
-        }
-      }
-      float tm = -__builtin_inff();
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[u][e] *= a.q.c;
-      if (edge) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = j + 16 * u + 4 * h + e - len;  // drafted row, negative: a cached one
-            bool see = i < 0 || (i < it.t && i <= tq[n]);
-            if (i >= 0 && i < it.t && a.q.mask)
-              see = a.q.mask[(int64_t)(it.first + tq[n]) * a.q.nwords + (i >> 5)] >> (i & 31) & 1;
-            see = see && at.ok && j + 16 * u + 4 * h + e < total;
-            s[u][e] = see ? s[u][e] : -__builtin_inff();
-          }
-        if (odd) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            pvis[n][w] = (s[w >> 1][2 * (w & 1)] == -__builtin_inff() ? 0u : 0x3f80u) |
-                         (s[w >> 1][2 * (w & 1) + 1] == -__builtin_inff() ? 0u : 0x3f800000u);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) tm = fmaxf(tm, s[u][e]);
-      tm = fmaxf(max4(tm), mx[n]);
-      if (__any(tm > mx[n])) {
-        const float al = tm == -__builtin_inff() ? 1.f : exp2_fast(mx[n] - tm);
-        mx[n] = tm;
-        sum[n] *= al;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) oacc[n][t] *= al;
-      }
-      const float base = mx[n] == -__builtin_inff() ? 0.f : mx[n];
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = exp2_fast(s[e >> 2][e & 3] - base);
-        sum[n] += p[e];
-      }
-      // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-9
-      // of the output at most); its sum is taken before
-#pragma unroll
-      for (int w = 0; w < 4; ++w) pb[n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
-    }
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      u32x4 vh, vl;
-      v_operand<F32, D>(kv, t, vh, vl);
-      if (odd) {
-        // infinities and NaN count only where they are seen: finite values go through the product, the
-        // others through products of 0 and 1 that tell which rows see one
-#pragma unroll
-        for (int kind = 0; kind < 3; ++kind) {
-          u32x4 one, clean = vh;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t o2 = 0, c2 = 0;
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const uint32_t x = vh[w] >> (16 * z) & 0xffffu;
-              const bool hit = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
-              o2 |= (hit ? 0x3f80u : 0u) << (16 * z);
-              c2 |= ((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) << (16 * z);
-            }
-            one[w] = o2;
-            clean[w] &= c2;
-            if (F32 && kind == 2) vl[w] &= c2;
-          }
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            const f32x4 cnt = mfma16(one, pvis[n], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (cnt[e] > 0.f)
-                oacc[n][t][e] += kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
-          }
-          if (kind == 2) vh = clean;
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        if constexpr (F32) oacc[n][t] = mfma16(vl, pb[n], oacc[n][t]);
-        oacc[n][t] = mfma16(vh, pb[n], oacc[n][t]);
-      }
-    }
+    weigh_tile<F32, D, NQ>(kv.k, q, ro, tq, j, h, at.ok, edge, mx, sum, oacc, pb, pvis);
+    add_values<F32, D, NQ>(kv.v, edge && any_special<F32, D>(kv.v), pb, pvis, oacc);
   };
 
   // two tiles take turns: one is in flight while the other is used
@@ -488,60 +587,162 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
 
   // join the waves: lane (m, h) holds dimensions [D / 4 h, D / 4 (h + 1)) of row m
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const float z = sum4(sum[n]);
-    if (h == 0) {
-      sml[wave][16 * n + m][0] = mx[n];
-      sml[wave][16 * n + m][1] = z;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int t = 0; t < DT; ++t) so[wave][16 * n + m][h * (D / 4) + e * DT + t] = oacc[n][t][e];
-  }
+  for (int n = 0; n < NQ; ++n)
+    store_wave<D>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
   __syncthreads();
-  const bool whole = it.npieces == 1;
   const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
-  for (int x = tid; x < 16 * NQ * (D / 4); x += 256) {
-    const int r = x / (D / 4), o4 = x % (D / 4) * 4;
-    if (r0 + r >= nr) continue;
-    float M = -__builtin_inff(), w[kWaves], z = 0.f;
+  join_waves<D, kWaves, 256, SEL>(a, it, so, sml, 16 * NQ, r0, nr, G, row_t0, slot);
+}
+
+// Many rows (a tree: more than 32 per head).  Streaming K and V into each wave's registers would read them once
+// per 32 rows; here 8 waves share a stage of 32 KW rows in LDS: 8 / KW groups of 32 rows of Q, KW parts of the stage
+// (64, 128 or 256 rows per workgroup).  Matrix and vector instructions are about even at 256 rows (per wave and 32
+// cached rows 512 cycles of v_mfma, about 600 of exponents, maxima and packing), and two waves per SIMD overlap
+// them.  A stage travels through registers (64 KB in flight per CU whatever KW, ahead by 4 / KW stages), is
+// written to one of two buffers and read after one barrier.  The 16-byte chunks of a row are permuted (an XOR with
+// the row) so that 16 rows' equal chunks lie in different banks.
+template <int D>
+__device__ __forceinline__ int chunk_xor(int r) {
+  return D == 128 ? r & 15 : (r >> 1) & 7;
+}
+
+template <int D, int KW>
+__global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
+  constexpr int NQ = 2, NW = 8, RW = NW / KW, SR = 32 * KW, PD = 4 / KW;  // SR: rows of a stage; PD: stages ahead
+  constexpr int KC = D / 32, DT = D / 16, VW = Tile<false, D>::VW, CPR = D / 8, RPI = 64 / CPR;
+  constexpr int NI = 2 * SR / RPI / NW;  // 16-byte loads per lane and stage, K before V
+  constexpr int kStage = SR * D * 2;     // bytes of K (or V) of a stage
+  constexpr int kJoin = NW * 16 * NQ * (kLd<D> + 2) * 4, kLds = 4 * kStage > kJoin ? 4 * kStage : kJoin;
+  __shared__ __align__(16) char lds[kLds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m = lane & 15, h = lane >> 4, wk = wave % KW, wr = wave / KW;
+  Item it;
+  if (!find_item(a, blockIdx.x, lane, it)) return;
+  {
+    const RowRange x = new_rows(a.q.start, it.b, a.q.nrows, a.q.max_rows);
+    it.first = x.first;
+    it.t = x.count;
+  }
+  it.b = __builtin_amdgcn_readfirstlane(it.b);
+  it.g = __builtin_amdgcn_readfirstlane(it.g);
+  it.first = __builtin_amdgcn_readfirstlane(it.first);
+  it.t = __builtin_amdgcn_readfirstlane(it.t);
+  const CacheView &c = a.c;
+  const int len = __builtin_amdgcn_readfirstlane(cache_len(c, it.b));
+  const int G = a.q.hq / c.hkv, nr = G * it.t, r0 = it.rt * 32 * RW;
+  if (r0 >= nr) return;
+  const int total = walk_len(a, len, it.t), ngroups = (total + kGroup - 1) / kGroup;
+  const int g0 = (int)((long long)ngroups * it.piece / it.npieces), g1 = (int)((long long)ngroups * (it.piece + 1) / it.npieces);
+  const int j0 = g0 * kGroup, j1 = g1 * kGroup < total ? g1 * kGroup : total;
+  const int nst = (j1 - j0 + SR - 1) / SR;
+
+  u32x4 q[NQ][KC][1];
+  int tq[NQ];
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sml[k][r][0]);
-    const float base = M == -__builtin_inff() ? 0.f : M;
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < NQ; ++n) {
+    int r = r0 + 32 * wr + 16 * n + m;
+    r = r < nr ? r : nr - 1;
+    tq[n] = r / G;
+    const char *p = (const char *)a.q.q + ((it.first + tq[n]) * a.q.sq_t + (it.g * G + r - tq[n] * G) * a.q.sq_h) * 2 + h * 16;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      w[k] = exp2_fast(sml[k][r][0] - base);
-      z += w[k] * sml[k][r][1];
-      const float *p = &so[k][r][o4];
-      if (sml[k][r][0] != -__builtin_inff())
+    for (int x = 0; x < KC; ++x) q[n][x][0] = *(const u32x4 *)(p + x * 64);
+  }
+  f32x4 oacc[NQ][DT];
+  float mx[NQ], sum[NQ];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += w[k] * p[e];
+  for (int n = 0; n < NQ; ++n) {
+    mx[n] = -__builtin_inff();
+    sum[n] = 0.f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) oacc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const bool idle = r0 + 32 * wr >= nr;  // a wave without rows only carries its part of the stages
+
+  // load i of a stage: RPI rows of K (i < NI / 2) or V, all of one 32-row tile; rows behind the end are read as
+  // the last
+  const int lr = lane / CPR, lc = lane % CPR;
+  u32x4 st[PD][NI];
+  auto fetch = [&](int stage, u32x4 (&x)[NI]) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI);  // piece of RPI rows; K or V
+      const int j = __builtin_amdgcn_readfirstlane(j0 + stage * SR + w * RPI / 32 * 32);
+      const TileAt at = tile_at(c, it.b, it.g, j < total ? j : total - 1, total);
+      int r = w * RPI % 32 + lr;
+      r = j < total ? (r < at.last ? r : at.last) : 0;
+      x[i] = *(const u32x4 *)((isv ? at.v + r * c.sv_t : at.k + r * c.sk_t) + 16 * lc);
     }
-    if (whole) {
-      const int t = SEL ? row_t0 : (r0 + r) / G, hh = it.g * G + (SEL ? r0 + r : r0 + r - t * G);
-      const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
-      u32x2 w2;
-      w2[0] = pack_bf16x2(v[0] * inv, v[1] * inv);
-      w2[1] = pack_bf16x2(v[2] * inv, v[3] * inv);
-      *(u32x2 *)(a.o + ((it.first + t) * a.so_t + hh * a.so_h + o4) * 2) = w2;
-      if (a.lse && o4 == 0)
-        a.lse[(int64_t)hh * a.q.nrows + it.first + t] = z == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(z)) * kLn2;
-    } else {
-      *(f32x4 *)(a.po + ((int64_t)slot * 16 * NQ + r) * D + o4) = v;
-      if (o4 == 0) {
-        float *ml = a.pml + ((int64_t)slot * 16 * NQ + r) * 2;
-        ml[0] = M;
-        ml[1] = z;
+  };
+  auto put = [&](char *buf, const u32x4 (&x)[NI]) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), r = w * RPI + lr;
+      *(u32x4 *)(buf + isv * kStage + r * (D * 2) + ((lc ^ chunk_xor<D>(r)) << 4)) = x[i];
+    }
+  };
+  const RowsOf ro{&a.q, len, total, it.t, it.first};
+  auto compute = [&](const char *buf, int stage) {
+    const int j = j0 + stage * SR + wk * 32;
+    if (idle || j >= j1) return;
+    const char *kb = buf + wk * 32 * (D * 2), *vb = kb + kStage;
+    u32x4 k[2][KC][1];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        const int r = 16 * u + m;
+        k[u][x][0] = *(const u32x4 *)(kb + r * (D * 2) + (((4 * x + h) ^ chunk_xor<D>(r)) << 4));
+      }
+    const bool edge = j + kTile > len || !page_ok(c, it.b, j);
+    u32x4 pb[NQ], pvis[NQ];
+    weigh_tile<false, D, NQ>(k, q, ro, tq, j, h, !edge || page_ok(c, it.b, j), edge, mx, sum, oacc, pb, pvis);
+    uint32_t v[8][VW];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = (i < 4 ? i : 12 + i) + 4 * h, f = chunk_xor<D>(r);
+      const char *x = vb + r * (D * 2) + (D == 128 ? (m ^ f) << 4 : (((m >> 1) ^ f) << 4) + ((m & 1) << 3));
+      if constexpr (D == 128) {
+        const u32x4 y = *(const u32x4 *)x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = y[e];
+      } else {
+        const u32x2 y = *(const u32x2 *)x;
+        v[i][0] = y[0], v[i][1] = y[1];
+      }
+    }
+    add_values<false, D, NQ>(v, edge && any_special<false, D>(v), pb, pvis, oacc);
+  };
+
+#pragma unroll
+  for (int x = 0; x < PD; ++x) fetch(x < nst ? x : 0, st[x]);
+  for (int s0 = 0; s0 < nst; s0 += PD) {
+#pragma unroll
+    for (int x = 0; x < PD; ++x) {
+      const int s = s0 + x;
+      if (s < nst) {
+        char *buf = lds + (s & 1) * 2 * kStage;
+        put(buf, st[x]);
+        if (s + PD < nst) fetch(s + PD, st[x]);
+        stage_barrier();
+        compute(buf, s);
       }
     }
   }
+  __syncthreads();  // the buffers become the parts' results: part wk of row group wr at rows 32 wr
+  float *so = (float *)lds, *sml = so + NW * 16 * NQ * kLd<D>;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int at = wk * 32 * RW + 32 * wr + 16 * n;
+    store_wave<D>(so + at * kLd<D>, sml + at * 2, m, h, mx[n], sum[n], oacc[n]);
+  }
+  __syncthreads();
+  join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0,
+                                it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g);
 }
 
 // Joins the pieces of every item: a workgroup per new row and head; its waves take pieces in turn, lanes
 // the dimensions, and LDS joins the waves.
-template <int D, int NQ, bool SEL>
+template <int D, bool SEL>
 __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   __shared__ float so[kWaves][D];
   __shared__ float sml[kWaves][2];
@@ -550,8 +751,8 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = blockIdx.y, g = hh / G;
   int slot, np, stride, row;
   if constexpr (SEL) {
-    const int rr = hh - g * G, rt = rr / (16 * NQ);
-    row = rr - rt * 16 * NQ;
+    const int rr = hh - g * G, rt = rr / a.trows;
+    row = rr - rt * a.trows;
     slot = ((r * a.rtiles + rt) * c.hkv + g) * a.pieces;
     np = a.pieces;
     stride = 1;
@@ -589,8 +790,8 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
       }
     }
     if (b < 0) return;
-    const int rr = (r - first) * G + hh - g * G, rt = rr / (16 * NQ);
-    row = rr - rt * 16 * NQ;
+    const int rr = (r - first) * G + hh - g * G, rt = rr / a.trows;
+    row = rr - rt * a.trows;
     slot = base + rt * c.hkv + g;
     stride = per;
   }
@@ -600,7 +801,7 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   for (int e = 0; e < D / 64; ++e) v[e] = 0.f;
 #pragma unroll 4
   for (int k = wave; k < np; k += kWaves) {
-    const int64_t at = (int64_t)(slot + k * stride) * 16 * NQ + row;
+    const int64_t at = (int64_t)(slot + k * stride) * a.trows + row;
     const float pm = a.pml[at * 2], pz = a.pml[at * 2 + 1];
     const float *p = a.po + at * D + lane * (D / 64);
     const float m2 = fmaxf(M, pm), base = m2 == -__builtin_inff() ? 0.f : m2;
@@ -998,21 +1199,23 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 }
 
 // ---- launches --------------------------------------------------------------------------------------
-// Row tiles of Q per wave: as few as hold the rows of one item, so that K and V are read once; more rows
-// than 64 (32 in fp32, whose tiles take twice the registers) become row tiles of their own.
-int row_tiles(bool f32, int rows) { return rows <= 16 ? 1 : rows <= 32 || f32 ? 2 : 4; }
+// Rows of an item: up to 32 are held by every wave (16 or 32); more of them in bf16 share stages (64, 128 or 256 per
+// workgroup), in fp32, whose tiles take twice the registers, they become row tiles of 32.
+int tile_rows(bool f32, bool sel, int rows) {
+  return rows <= 16 ? 16 : rows <= 32 || f32 || sel ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
 
 struct DraftShape {
-  int nq, rtiles, slots, grid, pieces;
+  int trows, rtiles, slots, grid, pieces;
 };
 
-// Workgroups that the chip holds at once: two per CU with one row tile of bf16, else one.
 DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int nsel) {
   DraftShape s{};
   const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
-  s.nq = row_tiles(f32, rows);
-  s.rtiles = (rows + 16 * s.nq - 1) / (16 * s.nq);
-  const int resident = !f32 && s.nq == 1 ? 512 : 256;
+  s.trows = tile_rows(f32, nsel > 0, rows);
+  s.rtiles = (rows + s.trows - 1) / s.trows;
+  // workgroups that the chip holds at once: two per CU with 16 rows of bf16, else one
+  const int resident = !f32 && s.trows == 16 ? 512 : 256;
   if (nsel) {
     const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
     const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
@@ -1031,22 +1234,24 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int nse
 }
 
 template <typename F>
-void by_tiles(bool f32, int d, int nq, F f) {
-  auto with_d = [&](auto x, auto dd) {
-    using N1 = std::integral_constant<int, 1>;
-    using N2 = std::integral_constant<int, 2>;
-    using N4 = std::integral_constant<int, 4>;
-    if (nq == 1)
-      f(x, dd, N1{});
-    else if (nq == 2)
-      f(x, dd, N2{});
-    else if constexpr (!decltype(x)::value)
-      f(x, dd, N4{});
-  };
+void by_tiles(bool f32, int d, int trows, F f) {
+  using N1 = std::integral_constant<int, 1>;
+  using N2 = std::integral_constant<int, 2>;
+  auto with_d = [&](auto x, auto dd) { trows == 16 ? f(x, dd, N1{}) : f(x, dd, N2{}); };
   auto with_t = [&](auto x) {
     d == 128 ? with_d(x, std::integral_constant<int, 128>{}) : with_d(x, std::integral_constant<int, 64>{});
   };
   f32 ? with_t(std::true_type{}) : with_t(std::false_type{});
+}
+
+template <int D>
+void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
+  if (s.trows == 64)
+    draft_wide_kernel<D, 4><<<s.grid, 512, 0, st>>>(a);
+  else if (s.trows == 128)
+    draft_wide_kernel<D, 2><<<s.grid, 512, 0, st>>>(a);
+  else
+    draft_wide_kernel<D, 1><<<s.grid, 512, 0, st>>>(a);
 }
 
 DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const DraftShape &s, int d) {
@@ -1054,10 +1259,11 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   a.c = c;
   a.q = q;
   a.rtiles = s.rtiles;
+  a.trows = s.trows;
   a.slots = s.slots;
   a.pieces = s.pieces;
-  a.po = ar.take<float>((size_t)s.grid * 16 * s.nq * d);
-  a.pml = ar.take<float>((size_t)s.grid * 16 * s.nq * 2);
+  a.po = ar.take<float>((size_t)s.grid * s.trows * d);
+  a.pml = ar.take<float>((size_t)s.grid * s.trows * 2);
   return a;
 }
 
@@ -1074,16 +1280,21 @@ SelectArgs select_parts(Arena &ar, const CacheView &c, const DraftView &q, int n
 
 template <bool SEL>
 rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipStream_t st) {
-  by_tiles(f32, d, s.nq, [&](auto x, auto dd, auto nn) {
-    constexpr bool F = decltype(x)::value;
-    constexpr int D = decltype(dd)::value, NQ = decltype(nn)::value;
-    if constexpr (SEL)
-      draft_kernel<F, D, NQ, true><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
-    else
-      draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
-    if (SEL ? s.pieces > 1 : a.c.cap > kGroup)
-      draft_join_kernel<D, NQ, SEL><<<dim3(a.q.nrows, a.q.hq), 256, 0, st>>>(a);
-  });
+  if (s.trows > 32)
+    d == 128 ? wide_launch<128>(a, s, st) : wide_launch<64>(a, s, st);
+  else
+    by_tiles(f32, d, s.trows, [&](auto x, auto dd, auto nn) {
+      constexpr bool F = decltype(x)::value;
+      constexpr int D = decltype(dd)::value, NQ = decltype(nn)::value;
+      if constexpr (SEL)
+        draft_kernel<F, D, NQ, true><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
+      else
+        draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
+    });
+  if (SEL ? s.pieces > 1 : a.c.cap > kGroup) {
+    const dim3 grid(a.q.nrows, a.q.hq);
+    d == 128 ? draft_join_kernel<128, SEL><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL><<<grid, 256, 0, st>>>(a);
+  }
   RS_HIP(hipGetLastError());
   return RS_OK;
 }
