@@ -20,7 +20,8 @@ struct CacheView {
   int64_t sk_p, sk_h, sk_t, sv_p, sv_h, sv_t;
   const int32_t *table;
   int32_t *len;
-  int32_t nseq, hkv, page, shift;  // shift: log2(page), or -1
+  int32_t nseq, hkv, page;
+  uint32_t pmul;                   // ceil(2^31 / (page / 64)), 0 where a sequence has one page: see page_of
   int32_t npages, max_pages, cap, kblocks;  // kblocks: blocks of 64 rows per page (the last may be partial)
   void *kmean;
   float *acc;
@@ -32,7 +33,12 @@ RS_HD int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; 
 // Rows that sequence b holds.
 RS_HD int cache_len(const CacheView &c, int b) { return clampi(c.len[b], 0, c.cap); }
 
-RS_HD int page_of(const CacheView &c, int j) { return c.shift >= 0 ? j >> c.shift : j / c.page; }
+// j / page by a multiplication: with B = page / 64 and M = ceil(2^31 / B), 2 (j / 64) M / 2^32 lies above
+// (j / 64) / B by less than (j / 64) B / (2^31 B) < 2^-19 < 1 / B, since j / 64 and B are at most 2^12.
+RS_HD int page_of(const CacheView &c, int j) { return (int)(((uint64_t)((uint32_t)(j >> 6) * 2u) * c.pmul) >> 32); }
+RS_HD uint32_t page_mul(int page, int max_pages) {
+  return max_pages == 1 ? 0u : (uint32_t)(((1ull << 31) + (uint64_t)(page / 64) - 1) / (uint64_t)(page / 64));
+}
 
 // The page that `entry` of the table names; -1: none.
 RS_HD int checked_page(const CacheView &c, int entry) { return entry >= 0 && entry < c.npages ? entry : -1; }

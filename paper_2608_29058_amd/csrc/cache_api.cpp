@@ -53,7 +53,7 @@ static rs_status check_cache(const rs_cache *x, CacheView *c) {
   c->table = x->table;
   c->len = x->len;
   c->nseq = x->nseq, c->hkv = x->hkv, c->page = x->page;
-  c->shift = (x->page & (x->page - 1)) ? -1 : __builtin_ctz((unsigned)x->page);
+  c->pmul = page_mul(x->page, x->max_pages);
   c->npages = x->npages, c->max_pages = x->max_pages, c->cap = x->page * x->max_pages;
   c->kblocks = (x->page + 63) / 64;
   c->kmean = x->kmean, c->acc = x->acc, c->pos = x->pos, c->seen = x->seen;

@@ -79,6 +79,9 @@ struct Tile {
   uint32_t v[8][VW];
 };
 
+template <bool F32, int D>
+using VTile = uint32_t[8][Tile<F32, D>::VW];
+
 // The rows of a tile: page and first row in it; rows behind `last` are read as the last (and masked).
 struct TileAt {
   const char *k, *v;
@@ -135,7 +138,7 @@ __device__ __forceinline__ void load_v(Tile<F32, D> &t, const TileAt &at, int64_
 
 // The operand V^T of output tile t: dimension DT * m + t of the lane's 8 rows (lo: fp32 only).
 template <bool F32, int D>
-__device__ __forceinline__ void v_operand(const uint32_t (&v)[8][Tile<F32, D>::VW], int t, u32x4 &hi, u32x4 &lo) {
+__device__ __forceinline__ void v_operand(const VTile<F32, D> &v, int t, u32x4 &hi, u32x4 &lo) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (F32) {
@@ -146,11 +149,6 @@ __device__ __forceinline__ void v_operand(const uint32_t (&v)[8][Tile<F32, D>::V
       hi[i] = __builtin_amdgcn_perm(v[2 * i + 1][t / 2], v[2 * i][t / 2], t % 2 ? 0x07060302u : 0x05040100u);
     }
   }
-}
-
-__device__ __forceinline__ bool page_ok(const CacheView &c, int b, int j) {
-  const int p = page_of(c, j);
-  return checked_page(c, c.table ? uload(c.table, (int64_t)b * c.max_pages + p) : b * c.max_pages + p) >= 0;
 }
 
 // Barrier after this wave's LDS accesses; loads from memory stay in flight.
@@ -166,133 +164,138 @@ struct RowsOf {
   int len, total, t, first;  // cached rows; with the drafted ones; new rows and the first of them
 };
 
-// The weights of a tile of 32 cached rows from row j for NQ x 16 rows of Q: raises the running maxima (and
-// rescales sums and O), adds to the sums, and leaves P as the operand of the product with V.  edge: a tile that
-// some row may not see in whole (its end, drafted rows, no page); pvis is then 1 for what a row sees.
+// S^T of 16 cached rows (operand k) and NQ x 16 rows of Q.
 template <bool F32, int D, int NQ>
-__device__ __forceinline__ void weigh_tile(const u32x4 (&k)[2][D / 32][F32 ? 2 : 1], const u32x4 (&q)[NQ][D / 32][F32 ? 2 : 1],
-                                           const RowsOf &ro, const int (&tq)[NQ], int j, int h, bool ok, bool edge,
-                                           float (&mx)[NQ], float (&sum)[NQ], f32x4 (&oacc)[NQ][D / 16], u32x4 (&pb)[NQ],
-                                           u32x4 (&pvis)[NQ]) {
-  constexpr int KC = D / 32, DT = D / 16;
+__device__ __forceinline__ void score_rows(const u32x4 (&k)[D / 32][F32 ? 2 : 1], const u32x4 (&q)[NQ][D / 32][F32 ? 2 : 1], f32x4 (&s)[NQ]) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    f32x4 s[2];
+  for (int n = 0; n < NQ; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < D / 32; ++x) {
+    if constexpr (F32) {
+      u32x4 kh, kl;
+      split8(__builtin_bit_cast(f32x4, k[x][0]), __builtin_bit_cast(f32x4, k[x][1]), kh, kl);
 #pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        if constexpr (F32) {
-          u32x4 kh, kl;
-          split8(__builtin_bit_cast(f32x4, k[u][x][0]), __builtin_bit_cast(f32x4, k[u][x][1]), kh, kl);
-          s[u] = mfma16(kl, q[n][x][0], s[u]);
-          s[u] = mfma16(kh, q[n][x][1], s[u]);
-          s[u] = mfma16(kh, q[n][x][0], s[u]);
-        } else {
-          s[u] = mfma16(k[u][x][0], q[n][x][0], s[u]);
-        }
+      for (int n = 0; n < NQ; ++n) {
+        s[n] = mfma16(kl, q[n][x][0], s[n]);
+        s[n] = mfma16(kh, q[n][x][1], s[n]);
+        s[n] = mfma16(kh, q[n][x][0], s[n]);
       }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n] = mfma16(k[x][0], q[n][x][0], s[n]);
     }
-    const float c = ro.q->c;
-    if (edge) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = j + 16 * u + 4 * h + e - ro.len;  // drafted row, negative: a cached one
-          bool see = i < 0 || (i < ro.t && i <= tq[n]);
-          if (i >= 0 && i < ro.t && ro.q->mask)
-            see = ro.q->mask[(int64_t)(ro.first + tq[n]) * ro.q->nwords + (i >> 5)] >> (i & 31) & 1;
-          see = see && ok && j + 16 * u + 4 * h + e < ro.total;
-          s[u][e] = see ? s[u][e] : -__builtin_inff();
-        }
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        pvis[n][w] = (s[w >> 1][2 * (w & 1)] == -__builtin_inff() ? 0u : 0x3f80u) |
-                     (s[w >> 1][2 * (w & 1) + 1] == -__builtin_inff() ? 0u : 0x3f800000u);
-    }
-    // maxima and exponents in units of 2^x: c = scale log2(e) > 0 goes into the exponent's one FMA
-    float tm = -__builtin_inff();
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) tm = fmaxf(tm, s[u][e]);
-    tm = fmaxf(max4(tm) * c, mx[n]);
-    if (__any(tm > mx[n])) {
-      const float al = tm == -__builtin_inff() ? 1.f : exp2_fast(mx[n] - tm);
-      mx[n] = tm;
-      sum[n] *= al;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) oacc[n][t] *= al;
-    }
-    const float base = mx[n] == -__builtin_inff() ? 0.f : mx[n];
-    float p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = exp2_fast(__builtin_fmaf(s[e >> 2][e & 3], c, -base));
-      sum[n] += p[e];
-    }
-    // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-8 of
-    // sum p |v| at most); its sum is taken before
-#pragma unroll
-    for (int w = 0; w < 4; ++w) pb[n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
   }
 }
 
-// Whether a tile of V holds infinities or NaN: values that a zero weight does not silence.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
+// Which of the rows j .. j + 31 of its cache the i-th new row of the sequence sees, as bits: the cached ones,
+// and of the drafted ones those of its mask row, or up to itself.
+__device__ __forceinline__ uint32_t seen_rows(const RowsOf &ro, int i, int j) {
+  const int x = j - ro.len;  // drafted row of bit 0, negative: a cached one
+  uint32_t drafts = low_bits(i - x + 1);
+  if (ro.q->mask) {
+    const uint32_t *row = ro.q->mask + (int64_t)(ro.first + i) * ro.q->nwords;
+    const int w = x >> 5;
+    const uint32_t lo = w >= 0 && w < ro.q->nwords ? row[w] : 0u, hi = w + 1 >= 0 && w + 1 < ro.q->nwords ? row[w + 1] : 0u;
+    drafts = (uint32_t)(((uint64_t)hi << 32 | lo) >> (x & 31));
+  }
+  return low_bits(-x) | (drafts & low_bits(ro.total - j));
+}
+
+// An edge: a tile of 32 rows from row j that some row of Q may not see in whole (drafted rows, the end).  Scores
+// of rows that are not seen become minus infinity.
+template <int NQ>
+__device__ __forceinline__ void mask_scores(const RowsOf &ro, const int (&tq)[NQ], int j, int h, f32x4 (&s)[2][NQ]) {
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const uint32_t see = seen_rows(ro, tq[n], j) >> (4 * h);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[u][n][e] = see >> (16 * u + e) & 1 ? s[u][n][e] : -__builtin_inff();
+  }
+}
+
+// The weights of NT tiles of 32 rows from their scores: raises the running maxima (and rescales sums and O), adds
+// to the sums, and leaves P as the operands of the products with V.
+template <int D, int NQ, int NT>
+__device__ __forceinline__ void weigh(const f32x4 (&s)[2 * NT][NQ], float c, float (&mx)[NQ], float (&sum)[NQ],
+                                      f32x4 (&oacc)[NQ][D / 16], u32x4 (&pb)[NT][NQ]) {
+  const float inf = __builtin_inff();
+  // maxima and exponents in units of 2^x: c = scale log2(e) > 0 goes into the exponent's one FMA
+  float tm[NQ];
+  bool raise = false;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    tm[n] = -inf;
+#pragma unroll
+    for (int u = 0; u < 2 * NT; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tm[n] = fmaxf(tm[n], s[u][n][e]);
+    tm[n] = fmaxf(max4(tm[n]) * c, mx[n]);
+    raise = raise || tm[n] > mx[n];
+  }
+  if (__any(raise)) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const float al = tm[n] == -inf ? 1.f : exp2_fast(mx[n] - tm[n]);
+      mx[n] = tm[n];
+      sum[n] *= al;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) oacc[n][t] *= al;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const float base = mx[n] == -inf ? 0.f : mx[n];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = exp2_fast(__builtin_fmaf(s[2 * i + (e >> 2)][n][e & 3], c, -base));
+        sum[n] += p[e];
+      }
+      // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-8 of
+      // sum p |v| at most); its sum is taken before
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pb[i][n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
+    }
+  }
+}
+
+// A value whose bf16 part is infinite or NaN: a zero weight does not silence it.
+__device__ __forceinline__ bool is_special(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
+
+// Takes infinities and NaN out of an edge's V; whether there were any.
 template <bool F32, int D>
-__device__ __forceinline__ bool any_special(const uint32_t (&v)[8][Tile<F32, D>::VW]) {
-  int bad = 0;
+__device__ __forceinline__ bool clean_values(VTile<F32, D> &v) {
+  bool bad = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int w = 0; w < Tile<F32, D>::VW; ++w) {
-      if constexpr (F32)
-        bad |= (v[i][w] & 0x7f800000u) == 0x7f800000u;
-      else
-        bad |= (v[i][w] & 0x7f80u) == 0x7f80u || (v[i][w] & 0x7f800000u) == 0x7f800000u;
+      if constexpr (F32) {
+        const bool x = is_special(pack_bf16x2(__builtin_bit_cast(float, v[i][w]), 0.f));
+        bad = bad || x;
+        v[i][w] = x ? 0u : v[i][w];
+      } else {
+        const bool x = is_special(v[i][w]), y = is_special(v[i][w] >> 16);
+        bad = bad || x || y;
+        v[i][w] &= (x ? 0u : 0xffffu) | (y ? 0u : 0xffff0000u);
+      }
     }
   return __any(bad);
 }
 
-// O^T += V^T P^T over a tile.  special: infinities and NaN count only where they are seen: finite values go
-// through the product, the others through products of 0 and 1 that tell which rows see one.
+// O^T += V^T P^T over a tile.
 template <bool F32, int D, int NQ>
-__device__ __forceinline__ void add_values(const uint32_t (&v)[8][Tile<F32, D>::VW], bool special, const u32x4 (&pb)[NQ],
-                                           const u32x4 (&pvis)[NQ], f32x4 (&oacc)[NQ][D / 16]) {
+__device__ __forceinline__ void add_values(const VTile<F32, D> &v, const u32x4 (&pb)[NQ], f32x4 (&oacc)[NQ][D / 16]) {
 #pragma unroll
   for (int t = 0; t < D / 16; ++t) {
     u32x4 vh, vl;
     v_operand<F32, D>(v, t, vh, vl);
-    if (special) {
-#pragma unroll
-      for (int kind = 0; kind < 3; ++kind) {
-        u32x4 one, clean = vh;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t o2 = 0, c2 = 0;
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const uint32_t x = vh[w] >> (16 * z) & 0xffffu;
-            const bool hit = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
-            o2 |= (hit ? 0x3f80u : 0u) << (16 * z);
-            c2 |= ((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) << (16 * z);
-          }
-          one[w] = o2;
-          clean[w] &= c2;
-          if (F32 && kind == 2) vl[w] &= c2;
-        }
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          const f32x4 cnt = mfma16(one, pvis[n], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (cnt[e] > 0.f) oacc[n][t][e] += kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
-        }
-        if (kind == 2) vh = clean;
-      }
-    }
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       if constexpr (F32) oacc[n][t] = mfma16(vl, pb[n], oacc[n][t]);
@@ -331,6 +334,13 @@ struct Item {
   int b, g, rt, piece, npieces, slot0;  // slot0: the item's first slot of pieces
   int len, t, first;                    // rows held, new rows and the first of them
 };
+
+// (what lanes agree on, said so: scalar registers, scalar branches)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Item uniform(const Item &x) {
+  return Item{uniform(x.b), uniform(x.g), uniform(x.rt), uniform(x.piece), uniform(x.npieces), uniform(x.slot0),
+              uniform(x.len), uniform(x.t), uniform(x.first)};
+}
 
 // Groups per piece: the same from the lengths alone in every workgroup and in the joining kernel.
 __device__ int plan_groups(const DraftArgs &a, int lane) {
@@ -404,6 +414,25 @@ __device__ __forceinline__ void store_wave(float *so, float *sml, int m, int h, 
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) so[m * kLd<D> + h * (D / 4) + e * (D / 16) + t] = oacc[t][e];
+}
+
+// Infinities and NaN of V count only where they are seen: those that clean_values took out of the edge from row j
+// are added, one by one, to the wave's O in LDS (so: `rows` rows of Q from row r0 of the item's nr).
+template <bool F32, int D, bool SEL>
+__device__ __forceinline__ void add_special(const CacheView &c, const Item &it, const RowsOf &ro, int j, float *so, int rows, int r0,
+                                            int nr, int G, int row_t0, int lane) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  const TileAt at = tile_at(c, it.b, it.g, j, ro.total);
+  for (int x = 0; x <= at.last; ++x)
+    for (int d = lane; d < D; d += 64) {
+      const float v = F32 ? ((const float *)(at.v + x * c.sv_t))[d] : (float)((const bf16 *)(at.v + x * c.sv_t))[d];
+      const uint32_t hi = pack_bf16x2(v, 0.f);
+      if (!is_special(hi)) continue;
+      for (int r = 0; r < rows && r0 + r < nr; ++r)
+        if (seen_rows(ro, SEL ? row_t0 : (r0 + r) / G, j) >> x & 1) so[r * kLd<D> + d] += __builtin_bit_cast(float, hi << 16);
+    }
 }
 
 // Joins KW parts of `rows` rows each (part k at so + k rows kLd) and writes them: as the result where the item
@@ -486,12 +515,11 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
     it.first = x.first;
     it.t = x.count;
   }
-  it.b = __builtin_amdgcn_readfirstlane(it.b);
-  it.g = __builtin_amdgcn_readfirstlane(it.g);
-  it.first = __builtin_amdgcn_readfirstlane(it.first);
-  it.t = __builtin_amdgcn_readfirstlane(it.t);
+  it.len = cache_len(a.c, it.b);
+  it = uniform(it);
+  row_t0 = uniform(row_t0);
   const CacheView &c = a.c;
-  const int len = __builtin_amdgcn_readfirstlane(cache_len(c, it.b));
+  const int len = it.len;
   const int G = a.q.hq / c.hkv, nr = SEL ? G : G * it.t;  // rows of this sequence (and token) and head
   const int r0 = it.rt * 16 * NQ;
   if (r0 >= nr) return;
@@ -547,11 +575,19 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
   };
 
   const RowsOf ro{&a.q, len, total, it.t, it.first};
+  bool special = false;  // an edge held infinities or NaN
   auto compute = [&](T &kv, const TileAt &at, int j) {
-    const bool edge = j + kTile > len || !at.ok;
-    u32x4 pb[NQ], pvis[NQ];
-    weigh_tile<F32, D, NQ>(kv.k, q, ro, tq, j, h, at.ok, edge, mx, sum, oacc, pb, pvis);
-    add_values<F32, D, NQ>(kv.v, edge && any_special<F32, D>(kv.v), pb, pvis, oacc);
+    if (!at.ok) return;  // no page: nobody sees these rows
+    f32x4 sc[2][NQ];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) score_rows<F32, D, NQ>(kv.k[u], q, sc[u]);
+    if (j + kTile > len) {
+      mask_scores<NQ>(ro, tq, j, h, sc);
+      special = clean_values<F32, D>(kv.v) || special;
+    }
+    u32x4 pb[1][NQ];
+    weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
+    add_values<F32, D, NQ>(kv.v, pb[0], oacc);
   };
 
   // two tiles take turns: one is in flight while the other is used
@@ -589,6 +625,12 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
     store_wave<D>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
+  if (special)
+    for (s = g0 * kGroup + wave * kTile; s < s_end; s += kGroup) {
+      const int j = uniform(row_of(s));
+      if (j + kTile > len && tile_at(c, it.b, it.g, j, total).ok)
+        add_special<F32, D, SEL>(c, it, ro, j, &so[wave * NQ * 16 * kLd<D>], 16 * NQ, r0, nr, G, row_t0, lane);
+    }
   __syncthreads();
   const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
   join_waves<D, kWaves, 256, SEL>(a, it, so, sml, 16 * NQ, r0, nr, G, row_t0, slot);
@@ -608,7 +650,8 @@ __device__ __forceinline__ int chunk_xor(int r) {
 
 template <int D, int KW>
 __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
-  constexpr int NQ = 2, NW = 8, RW = NW / KW, SR = 32 * KW, PD = 4 / KW;  // SR: rows of a stage; PD: stages ahead
+  constexpr int NT = KW == 4 ? 1 : 2;                            // tiles of 32 rows per wave and stage
+  constexpr int NQ = 2, NW = 8, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
   constexpr int KC = D / 32, DT = D / 16, VW = Tile<false, D>::VW, CPR = D / 8, RPI = 64 / CPR;
   constexpr int NI = 2 * SR / RPI / NW;  // 16-byte loads per lane and stage, K before V
   constexpr int kStage = SR * D * 2;     // bytes of K (or V) of a stage
@@ -623,12 +666,10 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     it.first = x.first;
     it.t = x.count;
   }
-  it.b = __builtin_amdgcn_readfirstlane(it.b);
-  it.g = __builtin_amdgcn_readfirstlane(it.g);
-  it.first = __builtin_amdgcn_readfirstlane(it.first);
-  it.t = __builtin_amdgcn_readfirstlane(it.t);
+  it.len = cache_len(a.c, it.b);
+  it = uniform(it);
   const CacheView &c = a.c;
-  const int len = __builtin_amdgcn_readfirstlane(cache_len(c, it.b));
+  const int len = it.len;
   const int G = a.q.hq / c.hkv, nr = G * it.t, r0 = it.rt * 32 * RW;
   if (r0 >= nr) return;
   const int total = walk_len(a, len, it.t), ngroups = (total + kGroup - 1) / kGroup;
@@ -658,19 +699,58 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   }
   const bool idle = r0 + 32 * wr >= nr;  // a wave without rows only carries its part of the stages
 
-  // load i of a stage: RPI rows of K (i < NI / 2) or V, all of one 32-row tile; rows behind the end are read as
-  // the last
+  // Load i of a stage: RPI rows of K or V.  64 rows of a stage lie in one page; the table's entries are read a
+  // stage ahead of their use.
+  constexpr int NP = SR > 64 ? SR / 64 : 1;
   const int lr = lane / CPR, lc = lane % CPR;
-  u32x4 st[PD][NI];
-  auto fetch = [&](int stage, u32x4 (&x)[NI]) {
+  u32x4 st[NI];
+  bool okst[NP];
+  int entry[NP];
+  auto look = [&](int stage) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI);  // piece of RPI rows; K or V
-      const int j = __builtin_amdgcn_readfirstlane(j0 + stage * SR + w * RPI / 32 * 32);
-      const TileAt at = tile_at(c, it.b, it.g, j < total ? j : total - 1, total);
-      int r = w * RPI % 32 + lr;
-      r = j < total ? (r < at.last ? r : at.last) : 0;
-      x[i] = *(const u32x4 *)((isv ? at.v + r * c.sv_t : at.k + r * c.sk_t) + 16 * lc);
+    for (int x = 0; x < NP; ++x) {
+      int j = j0 + stage * SR + 64 * x;
+      j = __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
+      const int p = page_of(c, j);
+      entry[x] = c.table ? uload(c.table, (int64_t)it.b * c.max_pages + p) : it.b * c.max_pages + p;
+    }
+  };
+  int off[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI);
+    off[i] = (w * RPI % 64 + lr) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc;
+  }
+  const char *kg = c.k + it.g * c.sk_h, *vg = c.v + it.g * c.sv_h;
+  auto fetch = [&](int stage, u32x4 (&x)[NI], bool (&ok)[NP]) {
+    const int js = j0 + stage * SR;
+    bool whole = js + SR <= total;
+    const char *kb[NP], *vb[NP];
+    int left[NP];  // last row that may be read
+#pragma unroll
+    for (int y = 0; y < NP; ++y) {
+      int j = js + 64 * y;
+      j = __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
+      const int id = checked_page(c, entry[y]), in = j - page_of(c, j) * c.page;
+      ok[y] = id >= 0;
+      kb[y] = kg + (ok[y] ? id * c.sk_p + in * c.sk_t : 0);
+      vb[y] = vg + (ok[y] ? id * c.sv_p + in * c.sv_t : 0);
+      left[y] = ok[y] ? total - 1 - j : 0;
+      whole = whole && ok[y];
+    }
+    look(stage + 1);
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64;
+        x[i] = *(const u32x4 *)((isv ? vb[y] : kb[y]) + off[i]);
+      }
+    } else {  // rows behind the end are read as the last, all without a page as its row 0
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64, r = w * RPI % 64 + lr;
+        x[i] = *(const u32x4 *)((isv ? vb[y] : kb[y]) + (r < left[y] ? r : left[y]) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc);
+      }
     }
   };
   auto put = [&](char *buf, const u32x4 (&x)[NI]) {
@@ -681,26 +761,16 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     }
   };
   const RowsOf ro{&a.q, len, total, it.t, it.first};
-  auto compute = [&](const char *buf, int stage) {
-    const int j = j0 + stage * SR + wk * 32;
-    if (idle || j >= j1) return;
-    const char *kb = buf + wk * 32 * (D * 2), *vb = kb + kStage;
-    u32x4 k[2][KC][1];
+  auto read_k = [&](const char *buf, int r, u32x4 (&k)[KC][1]) {  // 16 rows from row r
+    r += m;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int x = 0; x < KC; ++x) {
-        const int r = 16 * u + m;
-        k[u][x][0] = *(const u32x4 *)(kb + r * (D * 2) + (((4 * x + h) ^ chunk_xor<D>(r)) << 4));
-      }
-    const bool edge = j + kTile > len || !page_ok(c, it.b, j);
-    u32x4 pb[NQ], pvis[NQ];
-    weigh_tile<false, D, NQ>(k, q, ro, tq, j, h, !edge || page_ok(c, it.b, j), edge, mx, sum, oacc, pb, pvis);
-    uint32_t v[8][VW];
+    for (int x = 0; x < KC; ++x) k[x][0] = *(const u32x4 *)(buf + r * (D * 2) + (((4 * x + h) ^ chunk_xor<D>(m)) << 4));
+  };
+  auto read_v = [&](const char *buf, int r0, VTile<false, D> &v) {  // 32 rows
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int r = (i < 4 ? i : 12 + i) + 4 * h, f = chunk_xor<D>(r);
-      const char *x = vb + r * (D * 2) + (D == 128 ? (m ^ f) << 4 : (((m >> 1) ^ f) << 4) + ((m & 1) << 3));
+      const char *x = buf + kStage + (r0 + r) * (D * 2) + (D == 128 ? (m ^ f) << 4 : (((m >> 1) ^ f) << 4) + ((m & 1) << 3));
       if constexpr (D == 128) {
         const u32x4 y = *(const u32x4 *)x;
 #pragma unroll
@@ -710,22 +780,66 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
         v[i][0] = y[0], v[i][1] = y[1];
       }
     }
-    add_values<false, D, NQ>(v, edge && any_special<false, D>(v), pb, pvis, oacc);
   };
 
+  // stages of cached rows alone, which every row sees (and none what has no page)
+  const int nplain = len < j1 ? (len > j0 ? (len - j0) / SR : 0) : (j1 - j0) / SR, wr0 = wk * NT * 32;
+  const int page_of_wave = wr0 / 64 < NP ? wr0 / 64 : 0;
+  look(0);
+  fetch(0, st, okst);
+  for (int s = 0; s < nplain; ++s) {
+    char *buf = lds + (s & 1) * 2 * kStage;
+    put(buf, st);
+    bool ok = okst[0];
 #pragma unroll
-  for (int x = 0; x < PD; ++x) fetch(x < nst ? x : 0, st[x]);
-  for (int s0 = 0; s0 < nst; s0 += PD) {
+    for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
+    fetch(s + 1, st, okst);  // (behind the last: its last row)
+    stage_barrier();
+    if (idle || !ok) continue;
+    f32x4 sc[2 * NT][NQ];
+    u32x4 pb[NT][NQ];
 #pragma unroll
-    for (int x = 0; x < PD; ++x) {
-      const int s = s0 + x;
-      if (s < nst) {
-        char *buf = lds + (s & 1) * 2 * kStage;
-        put(buf, st[x]);
-        if (s + PD < nst) fetch(s + PD, st[x]);
-        stage_barrier();
-        compute(buf, s);
+    for (int u = 0; u < 2 * NT; ++u) {
+      u32x4 k[KC][1];
+      read_k(buf, wr0 + 16 * u, k);
+      score_rows<false, D, NQ>(k, q, sc[u]);
+    }
+    weigh<D, NQ, NT>(sc, a.q.c, mx, sum, oacc, pb);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      VTile<false, D> v;
+      read_v(buf, wr0 + 32 * i, v);
+      add_values<false, D, NQ>(v, pb[i], oacc);
+    }
+  }
+  // the few stages of drafted rows and the end
+  bool special = false;
+  for (int s = nplain; s < nst; ++s) {
+    __syncthreads();
+    put(lds, st);
+    bool ok = okst[0];
+#pragma unroll
+    for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
+    fetch(s + 1, st, okst);
+    stage_barrier();
+    if (idle || !ok) continue;
+    for (int i = 0; i < NT; ++i) {
+      const int r = wr0 + 32 * i, j = j0 + s * SR + r;
+      if (j >= j1) break;
+      f32x4 sc[2][NQ];
+      u32x4 pb[1][NQ];
+      VTile<false, D> v;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4 k[KC][1];
+        read_k(lds, r + 16 * u, k);
+        score_rows<false, D, NQ>(k, q, sc[u]);
       }
+      mask_scores<NQ>(ro, tq, j, h, sc);
+      weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
+      read_v(lds, r, v);
+      special = clean_values<false, D>(v) || special;
+      add_values<false, D, NQ>(v, pb[0], oacc);
     }
   }
   __syncthreads();  // the buffers become the parts' results: part wk of row group wr at rows 32 wr
@@ -735,6 +849,13 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     const int at = wk * 32 * RW + 32 * wr + 16 * n;
     store_wave<D>(so + at * kLd<D>, sml + at * 2, m, h, mx[n], sum[n], oacc[n]);
   }
+  if (special)
+    for (int s = nplain; s < nst; ++s)
+      for (int i = 0; i < NT; ++i) {
+        const int j = j0 + s * SR + wr0 + 32 * i;
+        if (j < j1 && tile_at(c, it.b, it.g, j, total).ok)
+          add_special<false, D, false>(c, it, ro, j, so + (wk * 32 * RW + 32 * wr) * kLd<D>, 32, r0 + 32 * wr, nr, G, 0, lane);
+      }
   __syncthreads();
   join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0,
                                 it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g);

@@ -114,13 +114,18 @@ def test_addresses_stay_in_bounds_whatever_the_device_arrays_hold(tmp_path):
 using namespace rs;
 static int bad(const char *what) { printf("%s\n", what); return 1; }
 int main() {
+  for (int blocks = 1; blocks <= 4096; ++blocks) {  // page numbers of every row block, for every page size
+    CacheView c{};
+    c.page = 64 * blocks; c.pmul = page_mul(c.page, 2);
+    for (int j = 0; j < 4096; ++j) if (page_of(c, j * 64 + j % 64) != j / blocks) return bad("page_of");
+  }
   const int odd[] = {0, 1, -1, 5, 6, 7, INT_MAX, INT_MIN, 64, 63, 255, 256, 257, 1 << 20};
   const int N = sizeof(odd) / sizeof(odd[0]);
   for (int page : {64, 128, 192, 100}) for (int with_table = 0; with_table < 2; ++with_table) {
     CacheView c{};
     int table[12], len[3], start[4];
-    c.nseq = 3; c.hkv = 2; c.page = page; c.shift = page == 64 ? 6 : page == 128 ? 7 : -1;
-    c.max_pages = page == 100 ? 1 : 4; c.npages = 3 * c.max_pages; c.cap = page * c.max_pages; c.kblocks = (page + 63) / 64;
+    c.nseq = 3; c.hkv = 2; c.page = page;     c.max_pages = page == 100 ? 1 : 4; c.npages = 3 * c.max_pages; c.cap = page * c.max_pages; c.kblocks = (page + 63) / 64;
+    c.pmul = page_mul(page, c.max_pages);
     c.sk_t = 256; c.sk_h = page * 256; c.sk_p = 2 * c.sk_h; c.sv_t = 512; c.sv_h = page * 512; c.sv_p = 2 * c.sv_h;
     c.table = with_table ? table : nullptr; c.len = len;
     for (int a = 0; a < N; ++a) for (int b = 0; b < N; ++b) {
