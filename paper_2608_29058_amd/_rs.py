@@ -582,6 +582,11 @@ class Draft:
         self.ref = C.byref(self.c)
 
 
+def _like(t, dtype, shape, device):
+    """t (or None) is a contiguous tensor of this dtype, shape and device."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous())
+
+
 def _check_pair(cache, draft):
     _want(draft.q.dtype == cache.dtype and draft.d == cache.d and draft.device == cache.device,
           "q must have the dtype, head dimension and device of the cache")
@@ -591,32 +596,37 @@ def _check_pair(cache, draft):
 def _check_rows_out(cache, draft, o, lse):
     import torch
     _check_pair(cache, draft)
-    _want(o.dtype == torch.bfloat16 and o.shape == draft.q.shape and (o.stride(2) == 1 or not o.numel()) and o.device == cache.device,
+    _want(o.dtype is torch.bfloat16 and o.shape == draft.q.shape and (o.stride(2) == 1 or not o.numel()) and o.device == cache.device,
           "o must be bf16 [nrows, hq, d] with a contiguous last dimension")
-    _want(lse is None or (lse.dtype == torch.float32 and lse.shape == (draft.hq, draft.nrows) and lse.is_contiguous()
-                          and lse.device == cache.device), "lse must be contiguous float32 [hq, nrows]")
+    _want(_like(lse, torch.float32, (draft.hq, draft.nrows), cache.device), "lse must be contiguous float32 [hq, nrows]")
+
+
+def _ws(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def rs_cache_append(cache, k_new, v_new, max_rows=1, start=None, stream=None):
     """k_new, v_new: [nrows, hkv, d] of the cache's dtype (last dim contiguous)."""
     import torch
-    _want(k_new.dim() == 3 and k_new.shape == v_new.shape and tuple(k_new.shape[1:]) == (cache.hkv, cache.d)
-          and k_new.dtype == cache.dtype == v_new.dtype and (k_new.stride(2) == v_new.stride(2) == 1 or not k_new.numel())
+    _want(k_new.dim() == 3 and k_new.shape == v_new.shape and k_new.shape[1] == cache.hkv and k_new.shape[2] == cache.d
+          and k_new.dtype is cache.dtype is v_new.dtype and (k_new.stride(2) == v_new.stride(2) == 1 or not k_new.numel())
           and k_new.device == cache.device == v_new.device, "k_new and v_new must be [nrows, hkv, d] like the cache")
-    _want(start is None or (start.dtype == torch.int32 and start.numel() == cache.nseq + 1 and start.is_contiguous()
-                            and start.device == cache.device), "start must be int32 with nseq + 1 entries")
+    _want(_like(start, torch.int32, (cache.nseq + 1,), cache.device), "start must be contiguous int32 [nseq + 1]")
     return _on_device(lib().rs_cache_append, cache.device, stream,
-                      (cache.ref, _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), v_new.stride(0),
-                       v_new.stride(1), _ptr(start), k_new.shape[0], max_rows))
+                      (cache.ref, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), v_new.stride(0),
+                       v_new.stride(1), _at(start), k_new.shape[0], max_rows))
 
 
 def rs_cache_commit(cache, naccept, max_new, path=None, stream=None):
     """naccept: int32 [nseq]; path: int32 [nseq, max_new] or None."""
     import torch
-    for name, t, shape in (("naccept", naccept, (cache.nseq,)), ("path", path, (cache.nseq, max_new))):
-        _want(t is None or (t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == cache.device),
-              f"{name} must be contiguous int32 {shape}")
-    return _on_device(lib().rs_cache_commit, cache.device, stream, (cache.ref, _ptr(naccept), _ptr(path), max_new))
+    _want(_like(naccept, torch.int32, (cache.nseq,), cache.device), "naccept must be contiguous int32 [nseq]")
+    _want(_like(path, torch.int32, (cache.nseq, max_new), cache.device), "path must be contiguous int32 [nseq, max_new]")
+    return _on_device(lib().rs_cache_commit, cache.device, stream, (cache.ref, naccept.data_ptr(), _at(path), max_new))
 
 
 def rs_draft_attn_workspace_size(cache, draft):
@@ -627,8 +637,7 @@ def rs_draft_attn(cache, draft, o, lse, ws, stream=None):
     """o: bf16 [nrows, hq, d]; lse: float32 [hq, nrows] or None."""
     _check_rows_out(cache, draft, o, lse)
     return _on_device(lib().rs_draft_attn, cache.device, stream,
-                      (cache.ref, draft.ref, _ptr(o), o.stride(0), o.stride(1), _ptr(lse), _ptr(ws),
-                       ws.numel() if ws is not None else 0))
+                      (cache.ref, draft.ref, o.data_ptr(), o.stride(0), o.stride(1), _at(lse), *_ws(ws)))
 
 
 def rs_select_attn_workspace_size(cache, draft, nsel):
@@ -639,25 +648,23 @@ def rs_select_attn(cache, draft, nsel, nsink, nlocal, o, lse, ws, blocks=None, s
     """As rs_draft_attn over nsel selected blocks per row and key/value head; blocks: int32 [nrows, hkv, nsel] or None."""
     import torch
     _check_rows_out(cache, draft, o, lse)
-    _want(blocks is None or (blocks.dtype == torch.int32 and tuple(blocks.shape) == (draft.nrows, cache.hkv, nsel)
-                             and blocks.is_contiguous() and blocks.device == cache.device),
-          "blocks must be contiguous int32 [nrows, hkv, nsel]")
+    _want(_like(blocks, torch.int32, (draft.nrows, cache.hkv, nsel), cache.device), "blocks must be contiguous int32 [nrows, hkv, nsel]")
     return _on_device(lib().rs_select_attn, cache.device, stream,
-                      (cache.ref, draft.ref, nsel, nsink, nlocal, _ptr(o), o.stride(0), o.stride(1), _ptr(lse),
-                       _ptr(blocks), _ptr(ws), ws.numel() if ws is not None else 0))
+                      (cache.ref, draft.ref, nsel, nsink, nlocal, o.data_ptr(), o.stride(0), o.stride(1), _at(lse),
+                       _at(blocks), *_ws(ws)))
 
 
 def rs_attn_weights(cache, draft, lse, acc_in, acc_out, row_w=None, stream=None):
     """lse: float32 [hq, nrows]; row_w: float32 [nrows] or None; acc_in (or None), acc_out: float32 [nseq, hkv, cap]."""
     import torch
     _check_pair(cache, draft)
-    for name, t, shape in (("lse", lse, (draft.hq, draft.nrows)), ("row_w", row_w, (draft.nrows,)),
-                           ("acc_in", acc_in, (cache.nseq, cache.hkv, cache.cap)),
-                           ("acc_out", acc_out, (cache.nseq, cache.hkv, cache.cap))):
-        _want(t is None or (t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous()
-                            and t.device == cache.device), f"{name} must be contiguous float32 {shape}")
+    f, acc = torch.float32, (cache.nseq, cache.hkv, cache.cap)
+    _want(lse is not None and _like(lse, f, (draft.hq, draft.nrows), cache.device), "lse must be contiguous float32 [hq, nrows]")
+    _want(_like(row_w, f, (draft.nrows,), cache.device), "row_w must be contiguous float32 [nrows]")
+    _want(acc_out is not None and _like(acc_in, f, acc, cache.device) and _like(acc_out, f, acc, cache.device),
+          "acc_in and acc_out must be contiguous float32 [nseq, hkv, cap]")
     return _on_device(lib().rs_attn_weights, cache.device, stream,
-                      (cache.ref, draft.ref, _ptr(lse), _ptr(row_w), _ptr(acc_in), _ptr(acc_out)))
+                      (cache.ref, draft.ref, lse.data_ptr(), _at(row_w), _at(acc_in), acc_out.data_ptr()))
 
 
 def rs_cache_evict_workspace_size(cache, budget):
@@ -665,5 +672,4 @@ def rs_cache_evict_workspace_size(cache, budget):
 
 
 def rs_cache_evict(cache, budget, nsink, nrecent, ws, stream=None):
-    return _on_device(lib().rs_cache_evict, cache.device, stream,
-                      (cache.ref, budget, nsink, nrecent, _ptr(ws), ws.numel() if ws is not None else 0))
+    return _on_device(lib().rs_cache_evict, cache.device, stream, (cache.ref, budget, nsink, nrecent, *_ws(ws)))

@@ -83,16 +83,28 @@ struct DraftView {
 };
 
 #if defined(__HIPCC__)
+// Inclusive prefix sum over the wave: DPP row shifts, then the rows' last lanes broadcast (six adds; __shfl_up
+// goes through LDS, 100 cycles a step).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_0(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x += dpp_or_0<0x111, 0xf>(x);
+  x += dpp_or_0<0x112, 0xf>(x);
+  x += dpp_or_0<0x114, 0xf>(x);
+  x += dpp_or_0<0x118, 0xf>(x);
+  x += dpp_or_0<0x142, 0xa>(x);
+  x += dpp_or_0<0x143, 0xc>(x);
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+
 // Exclusive prefix sum of x over the NT threads of a workgroup, and the total; sw: NT / 64 words of LDS.
 template <int NT>
 __device__ __forceinline__ int block_scan(int x, int *sw, int *total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int y = __shfl_up(s, m);
-    if (lane >= m) s += y;
-  }
+  const int s = wave_scan(x);
   if (lane == 63) sw[w] = s;
   __syncthreads();
   int before = 0, all = 0;

@@ -169,7 +169,7 @@ __global__ void commit_len_kernel(CacheView c, const int32_t *naccept, int max_n
 // ---- eviction ------------------------------------------------------------------------------
 // Plan, one workgroup per sequence and head (or several, below): the `budget` first rows of the order (firm
 // rows, then acc descending, then row ascending) are found by a radix selection over 32-bit keys with the counts
-// in LDS, the rows read again from cache in each pass.  The first digit has 12 bits: weights lie in a few
+// in LDS.  The first digit has 12 bits: weights lie in a few
 // octaves, and with 8 bits nearly all of a wave's counts would go to the same word.  One more pass lists,
 // in row order, the places before the budget whose row goes and the rows behind it that stay.
 struct EvictPlan {
@@ -238,13 +238,31 @@ constexpr int kBins = 4096;  // bins of a digit at most
 __device__ __forceinline__ int digit_bins(int pass) { return pass ? 1024 : 4096; }
 __device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 20 : pass == 1 ? 10 : 0; }
 
-// Lists, in row order, the places of [lo, hi) before the budget whose row goes and the rows behind it that
-// stay.  Before lo: `ranked` rows equal to the border's, `holes` such places and `movers` such rows.
-__device__ void list_moves(const float *acc, const int *pos, int lo, int hi, int budget, int nsink, int firm_from,
-                           const Border &bd, int ranked, int &holes, int &movers, int *hole_out, int *mover_out, int *sw) {
-  constexpr int kPer = 8;  // pieces of 64 consecutive rows per wave and step
+// Rows of a step: `PER` pieces of 64 consecutive rows per wave, the waves one after the other; thread (wave, lane)
+// holds rows j0 + wave 64 PER + 64 x + lane.
+template <int PER>
+__device__ __forceinline__ void load_keys(const float *acc, const int *pos, int j0, int hi, int nsink, int firm_from, uint32_t (&key)[PER]) {
+  const int jw = j0 + (threadIdx.x >> 6) * 64 * PER + (threadIdx.x & 63);
+  float a[PER];
+  int q[PER];
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int j = jw + 64 * x < hi ? jw + 64 * x : hi - 1;
+    a[x] = acc[j];
+    q[x] = pos[j];
+  }
+#pragma unroll
+  for (int x = 0; x < PER; ++x) key[x] = evict_key(a[x], q[x], nsink, firm_from);
+}
+
+// Lists, in row order, the places before the budget whose row goes and the rows behind it that stay, of a step
+// from row j0 of [.., hi).  Before it: `ranked` rows equal to the border's, `holes` such places and `movers` such
+// rows.
+template <int PER>
+__device__ __forceinline__ void list_moves(const uint32_t (&key)[PER], int j0, int hi, int budget, const Border &bd, int &ranked,
+                                           int &holes, int &movers, int *hole_out, int *mover_out, int *sw) {
   const bool ties = bd.need < bd.equal;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, jw = j0 + wave * 64 * PER + lane;
   const uint64_t below = (1ull << lane) - 1;
   // x of the waves before this one, and of all
   auto scan = [&](int x, int &all) {
@@ -261,56 +279,45 @@ __device__ void list_moves(const float *acc, const int *pos, int lo, int hi, int
     __syncthreads();
     return before;
   };
-  for (int j0 = lo; j0 < hi; j0 += kPlanThreads * kPer) {
-    const int jw = j0 + wave * 64 * kPer + lane;
-    float a[kPer];
-    int q[kPer], all;
+  int all, at = 0;
+  uint64_t eq[PER];
+  int e = 0;
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int j = jw + 64 * x < hi ? jw + 64 * x : hi - 1;
-      a[x] = acc[j];
-      q[x] = pos[j];
-    }
-    uint32_t key[kPer];
-    uint64_t eq[kPer];
-    int e = 0;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      key[x] = evict_key(a[x], q[x], nsink, firm_from) & bd.have;
-      eq[x] = __ballot(jw + 64 * x < hi && key[x] == bd.prefix);
-      e += __popcll(eq[x]);
-    }
-    int at = 0;
-    if (ties) {
-      at = ranked + scan(e, all);
-      ranked += all;
-    }
-    uint64_t hole[kPer], mover[kPer];
-    int hm = 0;
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int j = jw + 64 * x;
-      const bool same = key[x] == bd.prefix;
-      const bool stay = key[x] > bd.prefix || (same && (!ties || at + __popcll(eq[x] & below) < bd.need));
-      at += __popcll(eq[x]);
-      hole[x] = __ballot(j < hi && j < budget && !stay);
-      mover[x] = __ballot(j < hi && j >= budget && stay);
-      hm += __popcll(hole[x]) | __popcll(mover[x]) << 16;  // at most 8192 of each in a step
-    }
-    const int before = scan(hm, all);
-    int h = holes + (before & 0xffff), m = movers + (before >> 16);
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      if (hole[x] >> lane & 1) hole_out[h + __popcll(hole[x] & below)] = jw + 64 * x;
-      if (mover[x] >> lane & 1) mover_out[m + __popcll(mover[x] & below)] = jw + 64 * x;
-      h += __popcll(hole[x]);
-      m += __popcll(mover[x]);
-    }
-    holes += all & 0xffff;
-    movers += all >> 16;
+  for (int x = 0; x < PER; ++x) {
+    eq[x] = __ballot(jw + 64 * x < hi && (key[x] & bd.have) == bd.prefix);
+    e += __popcll(eq[x]);
   }
+  if (ties) {
+    at = ranked + scan(e, all);
+    ranked += all;
+  }
+  uint64_t hole[PER], mover[PER];
+  int hm = 0;
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int j = jw + 64 * x;
+    const uint32_t k = key[x] & bd.have;
+    const bool stay = k > bd.prefix || (k == bd.prefix && (!ties || at + __popcll(eq[x] & below) < bd.need));
+    at += __popcll(eq[x]);
+    hole[x] = __ballot(j < hi && j < budget && !stay);
+    mover[x] = __ballot(j < hi && j >= budget && stay);
+    hm += __popcll(hole[x]) | __popcll(mover[x]) << 16;  // at most 1024 PER of each in a step
+  }
+  const int before = scan(hm, all);
+  int h = holes + (before & 0xffff), m = movers + (before >> 16);
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    if (hole[x] >> lane & 1) hole_out[h + __popcll(hole[x] & below)] = jw + 64 * x;
+    if (mover[x] >> lane & 1) mover_out[m + __popcll(mover[x] & below)] = jw + 64 * x;
+    h += __popcll(hole[x]);
+    m += __popcll(mover[x]);
+  }
+  holes += all & 0xffff;
+  movers += all >> 16;
 }
 
+// Caches of up to 1024 PER rows: read once, their keys in registers.
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(CacheView c, int budget, int nsink, int nrecent, EvictPlan pl) {
   __shared__ int hist[kBins], sw[kPlanThreads / 64], pick[3];
   const int b = blockIdx.y, g = blockIdx.x;
@@ -323,16 +330,24 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(CacheView c, i
   const float *acc = c.acc + item * c.cap;
   const int *pos = c.pos + item * c.cap;
   const int seen = c.seen[b], firm_from = (seen > 0 ? seen : 0) - nrecent;
+  uint32_t key[PER];
+  load_keys<PER>(acc, pos, 0, n, nsink, firm_from, key);
+  const int jw = (threadIdx.x >> 6) * 64 * PER + (threadIdx.x & 63);
   Border bd{0, 0, budget, n};
   for (int pass = 0; pass < 3 && bd.need < bd.equal; ++pass) {
     const int bins = digit_bins(pass), sh = digit_shift(pass);
-    count_digit(acc, pos, 0, n, nsink, firm_from, bd.prefix, bd.have, sh, bins, hist);
+    for (int x = threadIdx.x; x < bins; x += kPlanThreads) hist[x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+      if (jw + 64 * x < n && (key[x] & bd.have) == bd.prefix) atomicAdd(&hist[(key[x] >> sh) & (bins - 1)], 1);
+    __syncthreads();
     pick_bin(hist, bins, bd.need, sw, pick);
     bd = Border{bd.prefix | (uint32_t)pick[0] << sh, bd.have | (uint32_t)(bins - 1) << sh, pick[1], pick[2]};
     __syncthreads();
   }
-  int holes = 0, movers = 0;
-  list_moves(acc, pos, 0, n, budget, nsink, firm_from, bd, 0, holes, movers, pl.hole + item * pl.most, pl.mover + item * pl.most, sw);
+  int ranked = 0, holes = 0, movers = 0;
+  list_moves<PER>(key, 0, n, budget, bd, ranked, holes, movers, pl.hole + item * pl.most, pl.mover + item * pl.most, sw);
   if (threadIdx.x == 0) pl.count[item] = movers;
 }
 
@@ -432,8 +447,12 @@ __global__ __launch_bounds__(kPlanThreads) void evict_slice_kernel(CacheView c, 
     const int kept = above[0] + (equal[0] < bd.need ? equal[0] : bd.need);    // rows that stay in earlier slices,
     const int kept1 = above[1] + (equal[1] < bd.need ? equal[1] : bd.need);   // and before the budget
     int holes = s < sl.n1 ? lo - kept : 0, movers = s < sl.n1 ? 0 : kept - kept1;
-    list_moves(acc, pos, lo, hi, budget, nsink, firm_from, bd, equal[0], holes, movers, pl.hole + item * pl.most,
-               pl.mover + item * pl.most, sw);
+    int ranked = equal[0];
+    for (int j0 = lo; j0 < hi; j0 += kPlanThreads * 8) {
+      uint32_t key[8];
+      load_keys<8>(acc, pos, j0, hi, nsink, firm_from, key);
+      list_moves<8>(key, j0, hi, budget, bd, ranked, holes, movers, pl.hole + item * pl.most, pl.mover + item * pl.most, sw);
+    }
     if (s == 0 && tid == 0) pl.count[item] = budget - kept1;
   }
 }
@@ -570,7 +589,11 @@ rs_status evict_launch(const CacheView &c, int dtype, int d, int budget, int nsi
     evict_slice_kernel<2><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
     evict_slice_kernel<3><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl, sl);
   } else {
-    evict_plan_kernel<<<dim3(c.hkv, c.nseq), kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+    const dim3 grid(c.hkv, c.nseq);
+    if (c.cap <= 4 * kPlanThreads)
+      evict_plan_kernel<4><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+    else
+      evict_plan_kernel<16><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
   }
   const int e = dtype == RS_BF16 ? 2 : 4;
   evict_move_kernel<<<dim3((pl.most + kMoveRows - 1) / kMoveRows, c.hkv, c.nseq), 256, 0, st>>>(c, budget, pl, log2i(d * e / 16));

@@ -46,6 +46,28 @@ __device__ __forceinline__ float join4(float x, F f) {
 __device__ __forceinline__ float max4(float x) { return join4(x, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float sum4(float x) { return join4(x, [](float a, float b) { return a + b; }); }
 
+// Maximum and sum over the wave.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or(float other, float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other), __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float wave_fold(float x, float none, F f) {
+  x = f(x, dpp_or<0x111, 0xf>(none, x));
+  x = f(x, dpp_or<0x112, 0xf>(none, x));
+  x = f(x, dpp_or<0x114, 0xf>(none, x));
+  x = f(x, dpp_or<0x118, 0xf>(none, x));
+  x = f(x, dpp_or<0x142, 0xa>(none, x));
+  x = f(x, dpp_or<0x143, 0xc>(none, x));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return wave_fold(x, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_total(float x) {
+  return wave_fold(x, 0.f, [](float a, float b) { return a + b; });
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // x as hi + lo, both bf16 (8 + 8 bits of its 24)
@@ -268,7 +290,20 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[2 * NT][NQ], float c, flo
 // A value whose bf16 part is infinite or NaN: a zero weight does not silence it.
 __device__ __forceinline__ bool is_special(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
 
-// Takes infinities and NaN out of an edge's V; whether there were any.
+// Takes infinities and NaN out of bf16 values of an edge; whether the lane held any.
+template <typename V>
+__device__ __forceinline__ bool clean_words(V &v) {
+  bool bad = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const bool x = is_special(v[w]), y = is_special(v[w] >> 16);
+    bad = bad || x || y;
+    v[w] &= (x ? 0u : 0xffffu) | (y ? 0u : 0xffff0000u);
+  }
+  return bad;
+}
+
+// The same of a tile of V; whether the wave held any.
 template <bool F32, int D>
 __device__ __forceinline__ bool clean_values(VTile<F32, D> &v) {
   bool bad = false;
@@ -342,51 +377,63 @@ __device__ __forceinline__ Item uniform(const Item &x) {
               uniform(x.len), uniform(x.t), uniform(x.first)};
 }
 
-// Groups per piece: the same from the lengths alone in every workgroup and in the joining kernel.
-__device__ int plan_groups(const DraftArgs &a, int lane) {
-  long long work = 0;
-  for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
-    const int b = b0 + lane;
-    if (b < a.c.nseq) {
-      const RowRange r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
-      if (r.count > 0) work += (walk_len(a, cache_len(a.c, b), r.count) + kGroup - 1) / kGroup;
-    }
+// Sequence of new row r, by the wave; -1: none.
+__device__ __forceinline__ int seq_of_row(const CacheView &c, const DraftView &q, int r, int lane) {
+  for (int b0 = 0; b0 < c.nseq; b0 += 64) {
+    RowRange x{0, 0};
+    if (b0 + lane < c.nseq) x = new_rows(q.start, b0 + lane, q.nrows, q.max_rows);
+    const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+    if (hit) return b0 + __builtin_ctzll(hit);
   }
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) work += __shfl_xor(work, m);
-  const long long per = (long long)a.c.hkv * a.rtiles, total = work * per;
+  return -1;
+}
+
+// What a lane knows of sequence b = b0 + lane; without new rows it has no items.
+struct Seq {
+  RowRange r;
+  int len, groups;
+};
+__device__ __forceinline__ Seq seq_at(const DraftArgs &a, int b) {
+  Seq s{RowRange{0, 0}, 0, 0};
+  if (b < a.c.nseq) {
+    s.r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+    s.len = cache_len(a.c, b);
+    if (s.r.count > 0) s.groups = (walk_len(a, s.len, s.r.count) + kGroup - 1) / kGroup;
+  }
+  return s;
+}
+
+// Groups per piece: the same from the lengths alone in every workgroup and in the joining kernel.  first: the
+// sequences of the first round of lanes.
+__device__ __forceinline__ int plan_groups(const DraftArgs &a, const Seq &first, int lane) {
+  if (a.slots == 0) return kMaxN;  // one piece each
+  int work = first.groups;  // (at most 65535 sequences of 2048 groups)
+  for (int b0 = 64; b0 < a.c.nseq; b0 += 64) work += seq_at(a, b0 + lane).groups;
+  work = wave_sum(work);
   // with pieces of at most C = ceil(total / slots) groups an item of n groups has less than n / C + 1 of them:
   // all together at most slots + the number of items, which is what the host counts
-  const long long groups = (total + a.slots - 1) / a.slots;
+  const long long total = (long long)work * a.c.hkv * a.rtiles, groups = (total + a.slots - 1) / a.slots;
   return groups > 0 ? (int)groups : 1;
 }
 
-// The piece-th piece overall; false: there are fewer.
+// The id-th piece overall; false: there are fewer.
 __device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
-  const int groups = plan_groups(a, lane);
-  const int per = a.c.hkv * a.rtiles;
+  Seq q = seq_at(a, lane);
+  const int groups = plan_groups(a, q, lane), per = a.c.hkv * a.rtiles;
   int base = 0;
   for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
-    const int b = b0 + lane;
-    int np = 0;
-    if (b < a.c.nseq) {
-      const RowRange r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
-      if (r.count > 0) np = pieces_of((walk_len(a, cache_len(a.c, b), r.count) + kGroup - 1) / kGroup, groups);
-    }
-    int s = np * per;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int y = __shfl_up(s, m);
-      if (lane >= m) s += y;
-    }
-    const int all = __shfl(s, 63);
+    if (b0) q = seq_at(a, b0 + lane);
+    const int np = q.r.count > 0 ? pieces_of(q.groups, groups) : 0;
+    const int s = wave_scan(np * per), all = __builtin_amdgcn_readlane(s, 63);
     if (id < base + all) {
-      const unsigned long long hit = __ballot(id < base + s);
-      const int l = __builtin_ctzll(hit);
+      const int l = __builtin_ctzll(__ballot(id < base + s));
       it.b = b0 + l;
-      it.npieces = __shfl(np, l);
-      const int x = id - (base + __shfl(s, l) - it.npieces * per);  // piece-major: all heads' row tiles of a piece adjacent
-      it.slot0 = base + __shfl(s, l) - it.npieces * per;
+      it.npieces = __builtin_amdgcn_readlane(np, l);
+      it.first = __builtin_amdgcn_readlane(q.r.first, l);
+      it.t = __builtin_amdgcn_readlane(q.r.count, l);
+      it.len = __builtin_amdgcn_readlane(q.len, l);
+      it.slot0 = base + __builtin_amdgcn_readlane(s, l) - it.npieces * per;
+      const int x = id - it.slot0;  // piece-major: all heads' row tiles of a piece adjacent
       it.piece = x / per;
       const int y = x - it.piece * per;
       it.rt = y / a.c.hkv;
@@ -402,8 +449,9 @@ __device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
 template <int D>
 constexpr int kLd = D + 4;  // a row of O in LDS, padded
 
-// A wave's O, maximum and sum of 16 rows into LDS (so: rows of kLd, sml: max and sum per row).
-template <int D>
+// A wave's O, maximum and sum of 16 rows into LDS (so: rows of kLd, sml: max and sum per row).  Lane (m, h) holds
+// dimension 16t + 4h + e (TR: V read transposed) or D / 4 h + D / 16 e + t of row m.
+template <int D, bool TR>
 __device__ __forceinline__ void store_wave(float *so, float *sml, int m, int h, float mx, float sum, const f32x4 (&oacc)[D / 16]) {
   const float z = sum4(sum);
   if (h == 0) {
@@ -413,7 +461,7 @@ __device__ __forceinline__ void store_wave(float *so, float *sml, int m, int h, 
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) so[m * kLd<D> + h * (D / 4) + e * (D / 16) + t] = oacc[t][e];
+    for (int t = 0; t < D / 16; ++t) so[m * kLd<D> + (TR ? 16 * t + 4 * h + e : h * (D / 4) + e * (D / 16) + t)] = oacc[t][e];
 }
 
 // Infinities and NaN of V count only where they are seen: those that clean_values took out of the edge from row j
@@ -479,7 +527,7 @@ __device__ __forceinline__ void join_waves(const DraftArgs &a, const Item &it, c
 
 // NQ: 16-row tiles of Q per wave.
 template <bool F32, int D, int NQ, bool SEL>
-__global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const DraftArgs a) {
+__global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draft_kernel(const DraftArgs a) {
   using T = Tile<F32, D>;
   constexpr int KC = T::KC, DT = T::DT, E = F32 ? 4 : 2, QP = F32 ? 2 : 1;
   __shared__ float so[kWaves * 16 * NQ * kLd<D>], sml[kWaves * 16 * NQ * 2];
@@ -495,15 +543,14 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
     it.npieces = a.pieces;
     it.b = -1;
     for (int b0 = 0; b0 < a.c.nseq && it.b < 0; b0 += 64) {
-      const int b = b0 + lane;
-      RowRange x{0, 0};
-      if (b < a.c.nseq) x = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
-      const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+      const Seq q = seq_at(a, b0 + lane);
+      const unsigned long long hit = __ballot(r >= q.r.first && r < q.r.first + q.r.count);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         it.b = b0 + l;
-        it.first = __shfl(x.first, l);
-        it.t = __shfl(x.count, l);
+        it.first = __builtin_amdgcn_readlane(q.r.first, l);
+        it.t = __builtin_amdgcn_readlane(q.r.count, l);
+        it.len = __builtin_amdgcn_readlane(q.len, l);
       }
     }
     if (it.b < 0) return;  // a row of no sequence
@@ -511,11 +558,7 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
     it.slot0 = ((r * a.rtiles + it.rt) * a.c.hkv + it.g) * a.pieces;
   } else {
     if (!find_item(a, blockIdx.x, lane, it)) return;
-    const RowRange x = new_rows(a.q.start, it.b, a.q.nrows, a.q.max_rows);
-    it.first = x.first;
-    it.t = x.count;
   }
-  it.len = cache_len(a.c, it.b);
   it = uniform(it);
   row_t0 = uniform(row_t0);
   const CacheView &c = a.c;
@@ -624,7 +667,7 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
   // join the waves: lane (m, h) holds dimensions [D / 4 h, D / 4 (h + 1)) of row m
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
-    store_wave<D>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
+    store_wave<D, false>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
   if (special)
     for (s = g0 * kGroup + wave * kTile; s < s_end; s += kGroup) {
       const int j = uniform(row_of(s));
@@ -637,15 +680,19 @@ __global__ __launch_bounds__(256, F32 || NQ > 1 ? 1 : 2) void draft_kernel(const
 }
 
 // Many rows (a tree: more than 32 per head).  Streaming K and V into each wave's registers would read them once
-// per 32 rows; here 8 waves share a stage of 32 KW rows in LDS: 8 / KW groups of 32 rows of Q, KW parts of the stage
-// (64, 128 or 256 rows per workgroup).  Matrix and vector instructions are about even at 256 rows (per wave and 32
-// cached rows 512 cycles of v_mfma, about 600 of exponents, maxima and packing), and two waves per SIMD overlap
-// them.  A stage travels through registers (64 KB in flight per CU whatever KW, ahead by 4 / KW stages), is
-// written to one of two buffers and read after one barrier.  The 16-byte chunks of a row are permuted (an XOR with
-// the row) so that 16 rows' equal chunks lie in different banks.
+// per 32 rows; here 8 waves share a stage in LDS: 8 / KW groups of 32 rows of Q, KW parts of the stage (64, 128 or
+// 256 rows per workgroup), one or two tiles of 32 rows per wave and stage.  A stage travels through registers (the
+// next one is in flight meanwhile), is written to one of two buffers and read after one barrier.  The 16-byte
+// chunks of a row are permuted by an XOR with the row, so that the reads spread over all banks; V is read
+// transposed (ds_read_b64_tr_b16).  At 256 rows, per wave and 64 rows of the cache: 64 v_mfma of 16 cycles, 32
+// v_exp of 16 and about 190 other vector instructions of 4; LDS passes 32 KB to each wave.  61 rows x 4 heads per
+// group over 128K rows: 195 us, 0.67 of 1.22 PFLOP/s; what is left over the matrix instructions is their lockstep
+// with the exponents (one barrier per stage).  64 rows per wave halve the LDS traffic, but O then lives in
+// accumulation registers and is copied at every rescale test: 418 us.
+// Chunks of K: 16 rows' equal chunks in different banks; of V: the chunk pairs 2t, 2t + 1 of 8 rows.
 template <int D>
 __device__ __forceinline__ int chunk_xor(int r) {
-  return D == 128 ? r & 15 : (r >> 1) & 7;
+  return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1);
 }
 
 template <int D, int KW>
@@ -661,12 +708,6 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   const int m = lane & 15, h = lane >> 4, wk = wave % KW, wr = wave / KW;
   Item it;
   if (!find_item(a, blockIdx.x, lane, it)) return;
-  {
-    const RowRange x = new_rows(a.q.start, it.b, a.q.nrows, a.q.max_rows);
-    it.first = x.first;
-    it.t = x.count;
-  }
-  it.len = cache_len(a.c, it.b);
   it = uniform(it);
   const CacheView &c = a.c;
   const int len = it.len;
@@ -766,19 +807,23 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
 #pragma unroll
     for (int x = 0; x < KC; ++x) k[x][0] = *(const u32x4 *)(buf + r * (D * 2) + (((4 * x + h) ^ chunk_xor<D>(m)) << 4));
   };
-  auto read_v = [&](const char *buf, int r0, VTile<false, D> &v) {  // 32 rows
+  // O^T += V^T P^T over 32 rows: lane (m, h) of a transposing read passes 4 dimensions of row 4h + m / 4 and gets
+  // dimension m of rows 4h .. 4h + 3; two of them are the operand of output tile t (dimensions 16t ..)
+  typedef short v4i16 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4i16 lds4;
+  const int vr = 4 * h + (m >> 2), vf = chunk_xor<D>(vr), vf1 = chunk_xor<D>(vr + 16);
+  bool special = false;  // an edge held infinities or NaN
+  auto values = [&](auto edge, const char *buf, int r0, const u32x4 (&p)[NQ]) {
+    const char *x0 = buf + kStage + (r0 + vr) * (D * 2) + (m & 1) * 8, *x1 = x0 + 16 * (D * 2);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = (i < 4 ? i : 12 + i) + 4 * h, f = chunk_xor<D>(r);
-      const char *x = buf + kStage + (r0 + r) * (D * 2) + (D == 128 ? (m ^ f) << 4 : (((m >> 1) ^ f) << 4) + ((m & 1) << 3));
-      if constexpr (D == 128) {
-        const u32x4 y = *(const u32x4 *)x;
+    for (int t = 0; t < DT; ++t) {
+      const int c2 = 2 * t + (m >> 1 & 1);
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x0 + ((c2 ^ vf) << 4))));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x1 + ((c2 ^ vf1) << 4))));
+      u32x4 v{lo[0], lo[1], hi[0], hi[1]};
+      if constexpr (decltype(edge)::value) special = clean_words(v) || special;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[i][e] = y[e];
-      } else {
-        const u32x2 y = *(const u32x2 *)x;
-        v[i][0] = y[0], v[i][1] = y[1];
-      }
+      for (int n = 0; n < NQ; ++n) oacc[n][t] = mfma16(v, p[n], oacc[n][t]);
     }
   };
 
@@ -797,6 +842,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     stage_barrier();
     if (idle || !ok) continue;
     f32x4 sc[2 * NT][NQ];
+    __builtin_amdgcn_s_setprio(1);  // matrix instructions first: the other wave's exponents fill their gaps (206 -> 198 us)
     u32x4 pb[NT][NQ];
 #pragma unroll
     for (int u = 0; u < 2 * NT; ++u) {
@@ -804,16 +850,14 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       read_k(buf, wr0 + 16 * u, k);
       score_rows<false, D, NQ>(k, q, sc[u]);
     }
+    __builtin_amdgcn_s_setprio(0);
     weigh<D, NQ, NT>(sc, a.q.c, mx, sum, oacc, pb);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      VTile<false, D> v;
-      read_v(buf, wr0 + 32 * i, v);
-      add_values<false, D, NQ>(v, pb[i], oacc);
-    }
+    for (int i = 0; i < NT; ++i) values(std::false_type{}, buf, wr0 + 32 * i, pb[i]);
+    __builtin_amdgcn_s_setprio(0);
   }
   // the few stages of drafted rows and the end
-  bool special = false;
   for (int s = nplain; s < nst; ++s) {
     __syncthreads();
     put(lds, st);
@@ -828,7 +872,6 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       if (j >= j1) break;
       f32x4 sc[2][NQ];
       u32x4 pb[1][NQ];
-      VTile<false, D> v;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         u32x4 k[KC][1];
@@ -837,9 +880,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       }
       mask_scores<NQ>(ro, tq, j, h, sc);
       weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
-      read_v(lds, r, v);
-      special = clean_values<false, D>(v) || special;
-      add_values<false, D, NQ>(v, pb[0], oacc);
+      values(std::true_type{}, lds, r, pb[0]);
     }
   }
   __syncthreads();  // the buffers become the parts' results: part wk of row group wr at rows 32 wr
@@ -847,9 +888,9 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int at = wk * 32 * RW + 32 * wr + 16 * n;
-    store_wave<D>(so + at * kLd<D>, sml + at * 2, m, h, mx[n], sum[n], oacc[n]);
+    store_wave<D, true>(so + at * kLd<D>, sml + at * 2, m, h, mx[n], sum[n], oacc[n]);
   }
-  if (special)
+  if (__any(special))
     for (int s = nplain; s < nst; ++s)
       for (int i = 0; i < NT; ++i) {
         const int j = j0 + s * SR + wr0 + 32 * i;
@@ -861,99 +902,89 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
                                 it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g);
 }
 
-// Joins the pieces of every item: a workgroup per new row and head; its waves take pieces in turn, lanes
-// the dimensions, and LDS joins the waves.
+// Joins the pieces of every item: a workgroup per new row and head.  Every wave reads all maxima and sums (a
+// lane per piece), so that each knows its weights before its share of the O parts arrives; LDS joins the waves.
 template <int D, bool SEL>
 __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   __shared__ float so[kWaves][D];
-  __shared__ float sml[kWaves][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int PL = D / 64;  // dimensions per lane
+  typedef float fv __attribute__((ext_vector_type(PL)));
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const CacheView &c = a.c;
   const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = blockIdx.y, g = hh / G;
   int slot, np, stride, row;
+  bool mine = true;
   if constexpr (SEL) {
     const int rr = hh - g * G, rt = rr / a.trows;
     row = rr - rt * a.trows;
     slot = ((r * a.rtiles + rt) * c.hkv + g) * a.pieces;
     np = a.pieces;
     stride = 1;
-    bool any = false;
-    for (int b0 = 0; b0 < c.nseq && !any; b0 += 64) {
-      RowRange x{0, 0};
-      if (b0 + lane < c.nseq) x = new_rows(a.q.start, b0 + lane, a.q.nrows, a.q.max_rows);
-      any = __any(r >= x.first && r < x.first + x.count);
-    }
-    if (!any) return;
   } else {
-    const int groups = plan_groups(a, lane), per = c.hkv * a.rtiles;
+    Seq q = seq_at(a, lane);
+    const int groups = plan_groups(a, q, lane), per = c.hkv * a.rtiles;
     int base = 0, b = -1, first = 0;
     np = 0;
     for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
-      RowRange x{0, 0};
-      int k = 0;
-      if (b0 + lane < c.nseq) x = new_rows(a.q.start, b0 + lane, a.q.nrows, a.q.max_rows);
-      if (x.count > 0) k = pieces_of((walk_len(a, cache_len(c, b0 + lane), x.count) + kGroup - 1) / kGroup, groups);
-      int s = k * per;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const int y = __shfl_up(s, m);
-        if (lane >= m) s += y;
-      }
-      const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
+      if (b0) q = seq_at(a, b0 + lane);
+      const int k = q.r.count > 0 ? pieces_of(q.groups, groups) : 0;
+      const int s = wave_scan(k * per);
+      const unsigned long long hit = __ballot(r >= q.r.first && r < q.r.first + q.r.count);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         b = b0 + l;
-        first = __shfl(x.first, l);
-        np = __shfl(k, l);
-        base += __shfl(s, l) - np * per;
+        first = __builtin_amdgcn_readlane(q.r.first, l);
+        np = __builtin_amdgcn_readlane(k, l);
+        base += __builtin_amdgcn_readlane(s, l) - np * per;
       } else {
-        base += __shfl(s, 63);
+        base += __builtin_amdgcn_readlane(s, 63);
       }
     }
-    if (b < 0) return;
+    if (b < 0 || np <= 1) return;
     const int rr = (r - first) * G + hh - g * G, rt = rr / a.trows;
     row = rr - rt * a.trows;
     slot = base + rt * c.hkv + g;
     stride = per;
   }
-  if (np <= 1) return;
-  float M = -__builtin_inff(), z = 0.f, v[D / 64];
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) v[e] = 0.f;
-#pragma unroll 4
-  for (int k = wave; k < np; k += kWaves) {
-    const int64_t at = (int64_t)(slot + k * stride) * a.trows + row;
-    const float pm = a.pml[at * 2], pz = a.pml[at * 2 + 1];
-    const float *p = a.po + at * D + lane * (D / 64);
-    const float m2 = fmaxf(M, pm), base = m2 == -__builtin_inff() ? 0.f : m2;
-    const float wo = exp2_fast(M - base), wn = exp2_fast(pm - base);
-    z = z * wo + pz * wn;
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) v[e] = v[e] * wo + (pm == -__builtin_inff() ? 0.f : p[e] * wn);
+  slot = uniform(slot), np = uniform(np), row = uniform(row);
+  const float *po = a.po + ((int64_t)slot * a.trows + row) * D + lane * PL, *pml = a.pml + ((int64_t)slot * a.trows + row) * 2;
+  const int64_t step = (int64_t)stride * a.trows;
+  float M = -__builtin_inff(), z = 0.f;
+  for (int k0 = 0; k0 < np; k0 += 64) {
+    const int k = k0 + lane;
+    float m = -__builtin_inff(), s = 0.f;
+    if (k < np) m = pml[k * step * 2], s = pml[k * step * 2 + 1];
+    const float m2 = wave_max(fmaxf(M, m));
+    const float base = m2 == -__builtin_inff() ? 0.f : m2;
+    s = wave_total(k < np ? s * exp2_fast(m - base) : 0.f);
+    z = (z == 0.f ? 0.f : z * exp2_fast(M - base)) + s;
     M = m2;
   }
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) so[wave][lane * (D / 64) + e] = v[e];
-  if (lane == 0) {
-    sml[wave][0] = M;
-    sml[wave][1] = z;
-  }
-  __syncthreads();
-  if (tid >= D / 2) return;
-  M = -__builtin_inff();
-#pragma unroll
-  for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sml[k][0]);
   const float base = M == -__builtin_inff() ? 0.f : M;
+  fv v{};
+  constexpr int kAhead = 8;
+  for (int k0 = wave; k0 < np; k0 += kWaves * kAhead) {
+    fv p[kAhead];
+    float m[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int k = k0 + x * kWaves < np ? k0 + x * kWaves : k0;
+      p[x] = *(const fv *)(po + k * step * D);
+      m[x] = pml[k * step * 2];
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x)
+      if (k0 + x * kWaves < np && m[x] != -__builtin_inff()) v += p[x] * exp2_fast(m[x] - base);
+  }
+  *(fv *)&so[wave][lane * PL] = v;
+  if constexpr (SEL) mine = seq_of_row(c, a.q, r, lane) >= 0;
+  __syncthreads();
+  if (tid >= D / 2 || !mine) return;
   float x = 0.f, y = 0.f;
-  z = 0.f;
 #pragma unroll
   for (int k = 0; k < kWaves; ++k) {
-    const float w = exp2_fast(sml[k][0] - base);
-    z += w * sml[k][1];
-    if (sml[k][0] != -__builtin_inff()) {
-      x += w * so[k][2 * tid];
-      y += w * so[k][2 * tid + 1];
-    }
+    x += so[k][2 * tid];
+    y += so[k][2 * tid + 1];
   }
   const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
   *(uint32_t *)(a.o + (r * a.so_t + hh * a.so_h + 2 * tid) * 2) = pack_bf16x2(x * inv, y * inv);
@@ -977,17 +1008,6 @@ struct SelectArgs {
   int32_t *list;  // [nrows * hkv][nsel]
   int fcap, nsel, nsink, nlocal;
 };
-
-// Sequence of new row r, by the wave; -1: none.
-__device__ __forceinline__ int seq_of_row(const CacheView &c, const DraftView &q, int r, int lane) {
-  for (int b0 = 0; b0 < c.nseq; b0 += 64) {
-    RowRange x{0, 0};
-    if (b0 + lane < c.nseq) x = new_rows(q.start, b0 + lane, q.nrows, q.max_rows);
-    const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
-    if (hit) return b0 + __builtin_ctzll(hit);
-  }
-  return -1;
-}
 
 // Rows of a 16-row tile: whole tokens of G heads, or 16 heads of one token.
 RS_HD int score_tokens(int G) { return G < 16 ? 16 / G : 1; }
@@ -1092,9 +1112,19 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
   constexpr int kBins = 2048;
   __shared__ int hist[kBins], sw[kSelThreads / 64], pick[3];
   const int tid = threadIdx.x, r = blockIdx.x, g = blockIdx.y;
-  const int b = seq_of_row(a.c, a.q, r, tid & 63);
-  if (b < 0) return;
-  const int F = cache_len(a.c, b) >> 6;
+  int F = -1;
+  for (int b0 = 0; b0 < a.c.nseq && F < 0; b0 += 64) {
+    const int b = b0 + (tid & 63);
+    RowRange q{0, 0};
+    int len = 0;
+    if (b < a.c.nseq) {
+      q = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
+      len = cache_len(a.c, b);
+    }
+    const unsigned long long hit = __ballot(r >= q.first && r < q.first + q.count);
+    if (hit) F = __builtin_amdgcn_readlane(len, __builtin_ctzll(hit)) >> 6;
+  }
+  if (F < 0) return;  // a row of no sequence
   const int64_t item = (int64_t)r * a.c.hkv + g;
   int32_t *list = a.list + item * a.nsel;
   const int nb = a.nsel < F ? a.nsel : F;
@@ -1171,9 +1201,10 @@ struct WeightArgs {
   DraftView q;
   const float *lse, *row_w, *acc_in;
   float *acc_out;
+  int rows;  // cached rows per workgroup
 };
 
-constexpr int kWeightRows = 1024, kRowsLds = 512;  // cached rows per workgroup; rows of Q whose factors LDS holds
+constexpr int kRowsLds = 512;  // rows of Q whose factors LDS holds
 
 // NQ: 16-row tiles of Q kept in registers; 0: more rows than that, Q is read again for every 64 cached rows.
 template <bool F32, int D, int NQ>
@@ -1187,7 +1218,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
   const CacheView &c = a.c;
   const RowRange rr = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
   const int len = cache_len(c, b), total = len + rr.count < c.cap ? len + rr.count : c.cap;
-  const int first = blockIdx.x * kWeightRows;
+  const int first = blockIdx.x * a.rows;
   if (first >= total || rr.count == 0) return;
   const int G = a.q.hq / c.hkv, nr = G * rr.count;
   const int64_t at = ((int64_t)b * c.hkv + g) * c.cap;
@@ -1265,7 +1296,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
     }
     __syncthreads();
     const int rows = nr - base < kRowsLds ? nr - base : kRowsLds;
-    const int end = total - first < kWeightRows ? total : first + kWeightRows;
+    const int end = total - first < a.rows ? total : first + a.rows;
     u32x4 k[NU][KC][QP], kn[NU][KC][QP];
     bool ok[NU], okn[NU];
     // RW cached rows per wave and step, the next in flight
@@ -1330,13 +1361,15 @@ struct DraftShape {
   int trows, rtiles, slots, grid, pieces;
 };
 
-DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int nsel) {
+constexpr int kShort = 256;
+
+DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
   DraftShape s{};
   const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
   s.trows = tile_rows(f32, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
-  // workgroups that the chip holds at once: two per CU with 16 rows of bf16, else one
-  const int resident = !f32 && s.trows == 16 ? 512 : 256;
+  // workgroups that the chip holds at once: two per CU with d = 64 or 16 rows of bf16, else one
+  const int resident = s.trows <= 32 && (d == 64 || (!f32 && s.trows == 16)) ? 512 : 256;
   if (nsel) {
     const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
     const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
@@ -1347,7 +1380,14 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int nse
     return s;
   }
   const int64_t items = (int64_t)c.nseq * c.hkv * s.rtiles, most = items * ((c.cap + kGroup - 1) / kGroup);
-  // few items: one round of workgroups; many: pieces of a quarter of a round, so that the last round is short
+  // A cache of up to kShort rows stays in one piece and needs no joining launch (4 us).  Longer ones gain from pieces
+  // (one token over 1001 rows, 8 heads: 16 us in one piece, 13 with the launch): few items make one round of
+  // workgroups; many, pieces of a quarter of a round, so that the last round is short.
+  if (c.cap <= kShort) {
+    s.slots = 0;
+    s.grid = (int)items;
+    return s;
+  }
   s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
   const int64_t grid = items + s.slots;
   s.grid = (int)(grid < most ? grid : most);
@@ -1412,7 +1452,7 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
       else
         draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
     });
-  if (SEL ? s.pieces > 1 : a.c.cap > kGroup) {
+  if (SEL ? s.pieces > 1 : s.slots > 0) {
     const dim3 grid(a.q.nrows, a.q.hq);
     d == 128 ? draft_join_kernel<128, SEL><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL><<<grid, 256, 0, st>>>(a);
   }
@@ -1425,13 +1465,13 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
 size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
   Arena ar(nullptr, 0);
   if (nsel) select_parts(ar, c, q, nsel);
-  draft_parts(ar, c, q, draft_shape(c, q, f32, nsel), d);
+  draft_parts(ar, c, q, draft_shape(c, q, f32, d, nsel), d);
   return ar.off + 256;
 }
 
 rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
                        void *ws, size_t ws_bytes, hipStream_t st) {
-  const DraftShape s = draft_shape(c, q, f32, 0);
+  const DraftShape s = draft_shape(c, q, f32, d, 0);
   Arena ar(ws, ws_bytes);
   DraftArgs a = draft_parts(ar, c, q, s, d);
   if (!ws || !ar.ok())
@@ -1442,7 +1482,7 @@ rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, 
 
 rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int nsink, int nlocal, void *o,
                         int64_t so_t, int64_t so_h, float *lse, int32_t *blocks, void *ws, size_t ws_bytes, hipStream_t st) {
-  const DraftShape s = draft_shape(c, q, f32, nsel);
+  const DraftShape s = draft_shape(c, q, f32, d, nsel);
   Arena ar(ws, ws_bytes);
   SelectArgs sel = select_parts(ar, c, q, nsel);
   DraftArgs a = draft_parts(ar, c, q, s, d);
@@ -1457,14 +1497,17 @@ rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d,
     f32 ? (d == 128 ? score_kernel<true, 128><<<grid, 256, 0, st>>>(sel) : score_kernel<true, 64><<<grid, 256, 0, st>>>(sel))
         : (d == 128 ? score_kernel<false, 128><<<grid, 256, 0, st>>>(sel) : score_kernel<false, 64><<<grid, 256, 0, st>>>(sel));
   }
-  select_kernel<<<dim3(q.nrows, c.hkv), kSelThreads, 0, st>>>(sel);
+  const dim3 rows(q.nrows, c.hkv);
+  select_kernel<<<rows, kSelThreads, 0, st>>>(sel);
   return attend<true>(a, s, f32, d, st);
 }
 
 rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d, const float *lse, const float *row_w,
                          const float *acc_in, float *acc_out, hipStream_t st) {
-  const WeightArgs a{c, q, lse, row_w, acc_in, acc_out};
-  const dim3 grid((c.cap + kWeightRows - 1) / kWeightRows, c.hkv, c.nseq);
+  // four steps of every wave, so that loads run ahead; one where that would leave CUs idle
+  const int per = (int64_t)((c.cap + 1023) / 1024) * c.hkv * c.nseq >= 512 ? 1024 : 256;
+  const WeightArgs a{c, q, lse, row_w, acc_in, acc_out, per};
+  const dim3 grid((c.cap + per - 1) / per, c.hkv, c.nseq);
   const int rows = q.hq / c.hkv * q.max_rows;
   auto run = [&](auto x, auto dd) {
     constexpr bool F = decltype(x)::value;
