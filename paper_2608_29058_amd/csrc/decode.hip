@@ -354,7 +354,7 @@ struct DraftArgs {
   float *lse;
   float *po, *pml;   // pieces: O (unnormalised), then (max, sum) of every row
   int rtiles, trows; // row tiles of a sequence with max_rows rows, rows of one
-  int slots;         // pieces that all items together may have beyond one each
+  int slots, least;  // pieces that all items together may have beyond one each; groups of a piece at least
   const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
   int nsel, pieces;  // with a list: pieces per item
 };
@@ -413,7 +413,7 @@ __device__ __forceinline__ int plan_groups(const DraftArgs &a, const Seq &first,
   // with pieces of at most C = ceil(total / slots) groups an item of n groups has less than n / C + 1 of them:
   // all together at most slots + the number of items, which is what the host counts
   const long long total = (long long)work * a.c.hkv * a.rtiles, groups = (total + a.slots - 1) / a.slots;
-  return groups > 0 ? (int)groups : 1;
+  return groups > a.least ? (int)groups : a.least;
 }
 
 // The id-th piece overall; false: there are fewer.
@@ -695,14 +695,16 @@ __device__ __forceinline__ int chunk_xor(int r) {
   return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1);
 }
 
-template <int D, int KW>
+// F32: values are split into their bf16 parts as they enter LDS, a plane each.
+template <bool F32, int D, int KW>
 __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
-  constexpr int NT = KW == 4 ? 1 : 2;                            // tiles of 32 rows per wave and stage
+  constexpr int NT = KW == 4 || F32 ? 1 : 2;                     // tiles of 32 rows per wave and stage
   constexpr int NQ = 2, NW = 8, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
-  constexpr int KC = D / 32, DT = D / 16, VW = Tile<false, D>::VW, CPR = D / 8, RPI = 64 / CPR;
+  constexpr int E = F32 ? 4 : 2, QP = F32 ? 2 : 1;                // bytes of a value; bf16 parts of it
+  constexpr int KC = D / 32, DT = D / 16, CPR = D * E / 16, RPI = 64 / CPR;
   constexpr int NI = 2 * SR / RPI / NW;  // 16-byte loads per lane and stage, K before V
-  constexpr int kStage = SR * D * 2;     // bytes of K (or V) of a stage
-  constexpr int kJoin = NW * 16 * NQ * (kLd<D> + 2) * 4, kLds = 4 * kStage > kJoin ? 4 * kStage : kJoin;
+  constexpr int kPlane = SR * D * 2, kBuf = 2 * QP * kPlane;  // a bf16 part of K or V of a stage; all of them
+  constexpr int kJoin = NW * 16 * NQ * (kLd<D> + 2) * 4, kLds = 2 * kBuf > kJoin ? 2 * kBuf : kJoin;
   __shared__ __align__(16) char lds[kLds];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4, wk = wave % KW, wr = wave / KW;
@@ -718,16 +720,21 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   const int j0 = g0 * kGroup, j1 = g1 * kGroup < total ? g1 * kGroup : total;
   const int nst = (j1 - j0 + SR - 1) / SR;
 
-  u32x4 q[NQ][KC][1];
+  u32x4 q[NQ][KC][QP];
   int tq[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     int r = r0 + 32 * wr + 16 * n + m;
     r = r < nr ? r : nr - 1;
     tq[n] = r / G;
-    const char *p = (const char *)a.q.q + ((it.first + tq[n]) * a.q.sq_t + (it.g * G + r - tq[n] * G) * a.q.sq_h) * 2 + h * 16;
+    const char *p = (const char *)a.q.q + ((it.first + tq[n]) * a.q.sq_t + (it.g * G + r - tq[n] * G) * a.q.sq_h) * E + h * 8 * E;
 #pragma unroll
-    for (int x = 0; x < KC; ++x) q[n][x][0] = *(const u32x4 *)(p + x * 64);
+    for (int x = 0; x < KC; ++x) {
+      if constexpr (F32)
+        split8(*(const f32x4 *)(p + x * 128), *(const f32x4 *)(p + x * 128 + 16), q[n][x][0], q[n][x][1]);
+      else
+        q[n][x][0] = *(const u32x4 *)(p + x * 64);
+    }
   }
   f32x4 oacc[NQ][DT];
   float mx[NQ], sum[NQ];
@@ -798,14 +805,43 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), r = w * RPI + lr;
-      *(u32x4 *)(buf + isv * kStage + r * (D * 2) + ((lc ^ chunk_xor<D>(r)) << 4)) = x[i];
+      char *row = buf + isv * QP * kPlane + r * (D * 2);
+      if constexpr (F32) {
+        const f32x4 f = __builtin_bit_cast(f32x4, x[i]);
+        uint32_t h0, l0, h1, l1;
+        split2(f[0], f[1], h0, l0);
+        split2(f[2], f[3], h1, l1);
+        row += ((lc >> 1 ^ chunk_xor<D>(r)) << 4) + (lc & 1) * 8;
+        *(u32x2 *)row = u32x2{h0, h1};
+        *(u32x2 *)(row + kPlane) = u32x2{l0, l1};
+      } else {
+        *(u32x4 *)(row + ((lc ^ chunk_xor<D>(r)) << 4)) = x[i];
+      }
     }
   };
   const RowsOf ro{&a.q, len, total, it.t, it.first};
-  auto read_k = [&](const char *buf, int r, u32x4 (&k)[KC][1]) {  // 16 rows from row r
-    r += m;
+  // S^T of 16 rows from row r0 of the stage
+  auto scores = [&](const char *buf, int r0, f32x4 (&s)[NQ]) {
+    const char *row = buf + (r0 + m) * (D * 2);
+    u32x4 k[KC][QP];
 #pragma unroll
-    for (int x = 0; x < KC; ++x) k[x][0] = *(const u32x4 *)(buf + r * (D * 2) + (((4 * x + h) ^ chunk_xor<D>(m)) << 4));
+    for (int x = 0; x < KC; ++x)
+#pragma unroll
+      for (int y = 0; y < QP; ++y) k[x][y] = *(const u32x4 *)(row + y * kPlane + (((4 * x + h) ^ chunk_xor<D>(m)) << 4));
+    if constexpr (F32) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KC; ++x)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          s[n] = mfma16(k[x][1], q[n][x][0], s[n]);
+          s[n] = mfma16(k[x][0], q[n][x][1], s[n]);
+          s[n] = mfma16(k[x][0], q[n][x][0], s[n]);
+        }
+    } else {
+      score_rows<false, D, NQ>(k, q, s);
+    }
   };
   // O^T += V^T P^T over 32 rows: lane (m, h) of a transposing read passes 4 dimensions of row 4h + m / 4 and gets
   // dimension m of rows 4h .. 4h + 3; two of them are the operand of output tile t (dimensions 16t ..)
@@ -814,16 +850,23 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   const int vr = 4 * h + (m >> 2), vf = chunk_xor<D>(vr), vf1 = chunk_xor<D>(vr + 16);
   bool special = false;  // an edge held infinities or NaN
   auto values = [&](auto edge, const char *buf, int r0, const u32x4 (&p)[NQ]) {
-    const char *x0 = buf + kStage + (r0 + vr) * (D * 2) + (m & 1) * 8, *x1 = x0 + 16 * (D * 2);
+    const char *x0 = buf + QP * kPlane + (r0 + vr) * (D * 2) + (m & 1) * 8, *x1 = x0 + 16 * (D * 2);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
       const int c2 = 2 * t + (m >> 1 & 1);
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x0 + ((c2 ^ vf) << 4))));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x1 + ((c2 ^ vf1) << 4))));
-      u32x4 v{lo[0], lo[1], hi[0], hi[1]};
-      if constexpr (decltype(edge)::value) special = clean_words(v) || special;
+      u32x4 v[QP];
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) oacc[n][t] = mfma16(v, p[n], oacc[n][t]);
+      for (int y = 0; y < QP; ++y) {
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x0 + y * kPlane + ((c2 ^ vf) << 4))));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x1 + y * kPlane + ((c2 ^ vf1) << 4))));
+        v[y] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        if constexpr (decltype(edge)::value) special = clean_words(v[y]) || special;
+      }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if constexpr (F32) oacc[n][t] = mfma16(v[QP - 1], p[n], oacc[n][t]);
+        oacc[n][t] = mfma16(v[0], p[n], oacc[n][t]);
+      }
     }
   };
 
@@ -833,7 +876,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   look(0);
   fetch(0, st, okst);
   for (int s = 0; s < nplain; ++s) {
-    char *buf = lds + (s & 1) * 2 * kStage;
+    char *buf = lds + (s & 1) * kBuf;
     put(buf, st);
     bool ok = okst[0];
 #pragma unroll
@@ -845,11 +888,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     __builtin_amdgcn_s_setprio(1);  // matrix instructions first: the other wave's exponents fill their gaps (206 -> 198 us)
     u32x4 pb[NT][NQ];
 #pragma unroll
-    for (int u = 0; u < 2 * NT; ++u) {
-      u32x4 k[KC][1];
-      read_k(buf, wr0 + 16 * u, k);
-      score_rows<false, D, NQ>(k, q, sc[u]);
-    }
+    for (int u = 0; u < 2 * NT; ++u) scores(buf, wr0 + 16 * u, sc[u]);
     __builtin_amdgcn_s_setprio(0);
     weigh<D, NQ, NT>(sc, a.q.c, mx, sum, oacc, pb);
     __builtin_amdgcn_s_setprio(1);
@@ -873,11 +912,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       f32x4 sc[2][NQ];
       u32x4 pb[1][NQ];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 k[KC][1];
-        read_k(lds, r + 16 * u, k);
-        score_rows<false, D, NQ>(k, q, sc[u]);
-      }
+      for (int u = 0; u < 2; ++u) scores(lds, r + 16 * u, sc[u]);
       mask_scores<NQ>(ro, tq, j, h, sc);
       weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
       values(std::true_type{}, lds, r, pb[0]);
@@ -895,7 +930,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       for (int i = 0; i < NT; ++i) {
         const int j = j0 + s * SR + wr0 + 32 * i;
         if (j < j1 && tile_at(c, it.b, it.g, j, total).ok)
-          add_special<false, D, false>(c, it, ro, j, so + (wk * 32 * RW + 32 * wr) * kLd<D>, 32, r0 + 32 * wr, nr, G, 0, lane);
+          add_special<F32, D, false>(c, it, ro, j, so + (wk * 32 * RW + 32 * wr) * kLd<D>, 32, r0 + 32 * wr, nr, G, 0, lane);
       }
   __syncthreads();
   join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0,
@@ -1351,14 +1386,15 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 }
 
 // ---- launches --------------------------------------------------------------------------------------
-// Rows of an item: up to 32 are held by every wave (16 or 32); more of them in bf16 share stages (64, 128 or 256 per
-// workgroup), in fp32, whose tiles take twice the registers, they become row tiles of 32.
+// Rows of an item: up to 32 are held by every wave (16 or 32); more of them share stages (64, 128 or 256 per
+// workgroup; fp32 stages are twice as large and serve 128 or 256).  Selections belong to one token, whose heads rarely
+// are that many: row tiles of 32.
 int tile_rows(bool f32, bool sel, int rows) {
-  return rows <= 16 ? 16 : rows <= 32 || f32 || sel ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  return rows <= 16 ? 16 : rows <= 32 || sel ? 32 : rows <= 64 && !f32 ? 64 : rows <= 128 ? 128 : 256;
 }
 
 struct DraftShape {
-  int trows, rtiles, slots, grid, pieces;
+  int trows, rtiles, slots, least, grid, pieces;
 };
 
 constexpr int kShort = 256;
@@ -1388,7 +1424,11 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
     s.grid = (int)items;
     return s;
   }
+  // A piece of many rows writes, and the join reads, as much as 2 trows rows of fp32: where the items alone fill
+  // the chip, it walks so many groups that this stays small beside K and V (49 sequences of 0 to 433 rows, 448 rows
+  // of Q per head: 215 us in pieces of one group, NEW4 us so).
   s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
+  s.least = items <= resident / 2 ? 1 : s.trows / 16;
   const int64_t grid = items + s.slots;
   s.grid = (int)(grid < most ? grid : most);
   return s;
@@ -1405,14 +1445,14 @@ void by_tiles(bool f32, int d, int trows, F f) {
   f32 ? with_t(std::true_type{}) : with_t(std::false_type{});
 }
 
-template <int D>
+template <bool F32, int D>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
-  if (s.trows == 64)
-    draft_wide_kernel<D, 4><<<s.grid, 512, 0, st>>>(a);
+  if (s.trows == 256)
+    draft_wide_kernel<F32, D, 1><<<s.grid, 512, 0, st>>>(a);
   else if (s.trows == 128)
-    draft_wide_kernel<D, 2><<<s.grid, 512, 0, st>>>(a);
-  else
-    draft_wide_kernel<D, 1><<<s.grid, 512, 0, st>>>(a);
+    draft_wide_kernel<F32, D, 2><<<s.grid, 512, 0, st>>>(a);
+  else if constexpr (!F32)
+    draft_wide_kernel<F32, D, 4><<<s.grid, 512, 0, st>>>(a);
 }
 
 DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const DraftShape &s, int d) {
@@ -1422,6 +1462,7 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   a.rtiles = s.rtiles;
   a.trows = s.trows;
   a.slots = s.slots;
+  a.least = s.least;
   a.pieces = s.pieces;
   a.po = ar.take<float>((size_t)s.grid * s.trows * d);
   a.pml = ar.take<float>((size_t)s.grid * s.trows * 2);
@@ -1442,7 +1483,8 @@ SelectArgs select_parts(Arena &ar, const CacheView &c, const DraftView &q, int n
 template <bool SEL>
 rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipStream_t st) {
   if (s.trows > 32)
-    d == 128 ? wide_launch<128>(a, s, st) : wide_launch<64>(a, s, st);
+    f32 ? (d == 128 ? wide_launch<true, 128>(a, s, st) : wide_launch<true, 64>(a, s, st))
+        : (d == 128 ? wide_launch<false, 128>(a, s, st) : wide_launch<false, 64>(a, s, st));
   else
     by_tiles(f32, d, s.trows, [&](auto x, auto dd, auto nn) {
       constexpr bool F = decltype(x)::value;

@@ -43,6 +43,11 @@ def test_one_token_per_sequence(hq, hkv, d, dtype, page, layout):
     (28, 4, 64, "f32", [0, 61, 130], [13, 5, 13], "tree"),
     (4, 4, 128, "f32", [0, 100], [7, 70], "random"),
     (8, 2, 128, "bf16", [40, 3], [256, 100], "tree"),       # the most rows
+    (8, 2, 64, "f32", [300, 45], [70, 256], "tree"),
+    (14, 2, 128, "f32", [700, 0, 64], [10, 16, 1], None),   # 70 to 112 rows
+    (8, 2, 128, "f32", [1000, 0], [200, 60], "random"),
+    (12, 1, 128, "bf16", [333, 20], [5, 3], None),          # 36 to 60 rows
+    (20, 2, 64, "bf16", [1200], [12], "tree"),              # 120 rows
     (8, 2, 64, "bf16", [63, 500], [2, 0], None),            # a sequence without new rows
 ])
 def test_drafted_rows(hq, hkv, d, dtype, lens, rows, kind):
@@ -61,6 +66,7 @@ def test_drafted_rows(hq, hkv, d, dtype, lens, rows, kind):
     ([20011], [1], 8, 2, None),                 # one item per head, many pieces
     ([9000, 1, 0, 4097], [16, 1, 1, 3], 4, 1, "tree"),
     ([3000] * 5 + [17] * 90, [1] * 95, 4, 2, None),   # more sequences than a wave has lanes
+    ([500, 0, 2100] * 20, [40, 7, 64] * 20, 8, 2, "tree"),   # items that fill the chip, of many rows
 ])
 def test_split_sequences(lens, rows, hq, hkv, kind):
     s = Setup(7, lens, rows, hq=hq, hkv=hkv, d=128, page=128, kind=kind, spread=3.0)
@@ -125,11 +131,11 @@ def test_rows_without_a_page_are_not_seen(dtype, bad):
     check_rows(s, ref, o, l)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_values_that_nobody_sees_do_no_harm(dtype):
+@pytest.mark.parametrize("dtype,hq", [("bf16", 8), ("f32", 8), ("bf16", 24), ("f32", 24), ("bf16", 40), ("bf16", 80), ("f32", 80)])
+def test_values_that_nobody_sees_do_no_harm(dtype, hq):
     """Drafted rows of other branches, and whatever lies behind a sequence, hold infinities and NaN."""
     import torch
-    s = Setup(9, [50, 131], [5, 4], dtype=dtype, kind="tree")
+    s = Setup(9, [50, 131], [5, 4], dtype=dtype, kind="tree", hq=hq)
     m = np.zeros((s.nrows, 32), bool)
     for f, t in s.rows:
         m[f:f + t, :t] = np.eye(t, dtype=bool)
