@@ -290,38 +290,34 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[2 * NT][NQ], float c, flo
 // A value whose bf16 part is infinite or NaN: a zero weight does not silence it.
 __device__ __forceinline__ bool is_special(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
 
-// Takes infinities and NaN out of bf16 values of an edge; whether the lane held any.
-template <typename V>
-__device__ __forceinline__ bool clean_words(V &v) {
-  bool bad = false;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const bool x = is_special(v[w]), y = is_special(v[w] >> 16);
-    bad = bad || x || y;
-    v[w] &= (x ? 0u : 0xffffu) | (y ? 0u : 0xffff0000u);
-  }
-  return bad;
+// Bits 15 and 31: whether the word's bf16 halves are special.
+__device__ __forceinline__ uint32_t special_halves(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// A word of two bf16 values without its special ones.
+__device__ __forceinline__ uint32_t clean_word(uint32_t w) {
+  return w & ((is_special(w) ? 0u : 0xffffu) | (is_special(w >> 16) ? 0u : 0xffff0000u));
 }
 
-// The same of a tile of V; whether the wave held any.
+// Takes infinities and NaN out of an edge's V; whether there were any.
 template <bool F32, int D>
 __device__ __forceinline__ bool clean_values(VTile<F32, D> &v) {
-  bool bad = false;
+  constexpr int VW = Tile<F32, D>::VW;
+  uint32_t bad = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int w = 0; w < Tile<F32, D>::VW; ++w) {
-      if constexpr (F32) {
-        const bool x = is_special(pack_bf16x2(__builtin_bit_cast(float, v[i][w]), 0.f));
-        bad = bad || x;
-        v[i][w] = x ? 0u : v[i][w];
-      } else {
-        const bool x = is_special(v[i][w]), y = is_special(v[i][w] >> 16);
-        bad = bad || x || y;
-        v[i][w] &= (x ? 0u : 0xffffu) | (y ? 0u : 0xffff0000u);
-      }
+    for (int w = 0; w < VW; ++w) bad |= special_halves(F32 ? pack_bf16x2(__builtin_bit_cast(float, v[i][w]), 0.f) : v[i][w]);
+  if (!__any(bad)) return false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int w = 0; w < VW; ++w) {
+      if constexpr (F32)
+        v[i][w] = is_special(pack_bf16x2(__builtin_bit_cast(float, v[i][w]), 0.f)) ? 0u : v[i][w];
+      else
+        v[i][w] = clean_word(v[i][w]);
     }
-  return __any(bad);
+  return true;
 }
 
 // O^T += V^T P^T over a tile.
@@ -706,6 +702,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   constexpr int kPlane = SR * D * 2, kBuf = 2 * QP * kPlane;  // a bf16 part of K or V of a stage; all of them
   constexpr int kJoin = NW * 16 * NQ * (kLd<D> + 2) * 4, kLds = 2 * kBuf > kJoin ? 2 * kBuf : kJoin;
   __shared__ __align__(16) char lds[kLds];
+  __shared__ int odd;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4, wk = wave % KW, wr = wave / KW;
   Item it;
@@ -801,11 +798,29 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       }
     }
   };
-  auto put = [&](char *buf, const u32x4 (&x)[NI]) {
+  // edge: V without infinities and NaN, which `odd` (LDS) then tells of
+  auto put = [&](auto edge, char *buf, u32x4 (&x)[NI]) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), r = w * RPI + lr;
       char *row = buf + isv * QP * kPlane + r * (D * 2);
+      if constexpr (decltype(edge)::value)
+        if (isv) {
+          uint32_t bad = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t y = x[i][e];
+            bad |= special_halves(F32 ? pack_bf16x2(__builtin_bit_cast(float, y), 0.f) : y);
+          }
+          if (__any(bad)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t y = x[i][e];
+              x[i][e] = F32 ? (is_special(pack_bf16x2(__builtin_bit_cast(float, y), 0.f)) ? 0u : y) : clean_word(y);
+            }
+            odd = 1;
+          }
+        }
       if constexpr (F32) {
         const f32x4 f = __builtin_bit_cast(f32x4, x[i]);
         uint32_t h0, l0, h1, l1;
@@ -848,8 +863,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   typedef short v4i16 __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) v4i16 lds4;
   const int vr = 4 * h + (m >> 2), vf = chunk_xor<D>(vr), vf1 = chunk_xor<D>(vr + 16);
-  bool special = false;  // an edge held infinities or NaN
-  auto values = [&](auto edge, const char *buf, int r0, const u32x4 (&p)[NQ]) {
+  auto values = [&](const char *buf, int r0, const u32x4 (&p)[NQ]) {
     const char *x0 = buf + QP * kPlane + (r0 + vr) * (D * 2) + (m & 1) * 8, *x1 = x0 + 16 * (D * 2);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
@@ -860,7 +874,6 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x0 + y * kPlane + ((c2 ^ vf) << 4))));
         const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(x1 + y * kPlane + ((c2 ^ vf1) << 4))));
         v[y] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-        if constexpr (decltype(edge)::value) special = clean_words(v[y]) || special;
       }
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
@@ -877,7 +890,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
   fetch(0, st, okst);
   for (int s = 0; s < nplain; ++s) {
     char *buf = lds + (s & 1) * kBuf;
-    put(buf, st);
+    put(std::false_type{}, buf, st);
     bool ok = okst[0];
 #pragma unroll
     for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
@@ -893,13 +906,14 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     weigh<D, NQ, NT>(sc, a.q.c, mx, sum, oacc, pb);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) values(std::false_type{}, buf, wr0 + 32 * i, pb[i]);
+    for (int i = 0; i < NT; ++i) values(buf, wr0 + 32 * i, pb[i]);
     __builtin_amdgcn_s_setprio(0);
   }
   // the few stages of drafted rows and the end
+  if (tid == 0) odd = 0;
   for (int s = nplain; s < nst; ++s) {
     __syncthreads();
-    put(lds, st);
+    put(std::true_type{}, lds, st);
     bool ok = okst[0];
 #pragma unroll
     for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
@@ -915,17 +929,48 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
       for (int u = 0; u < 2; ++u) scores(lds, r + 16 * u, sc[u]);
       mask_scores<NQ>(ro, tq, j, h, sc);
       weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
-      values(std::true_type{}, lds, r, pb[0]);
+      values(lds, r, pb[0]);
     }
   }
-  __syncthreads();  // the buffers become the parts' results: part wk of row group wr at rows 32 wr
-  float *so = (float *)lds, *sml = so + NW * 16 * NQ * kLd<D>;
+  __syncthreads();
+  const bool special = odd;
+  const int slot = it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
+  if (KW == 1 && !special) {
+    // a wave's rows are its own: lane (m, h) writes dimensions 16t + 4h .. + 3 of row m
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const float z = sum4(sum[n]);
+      const int r = 32 * wr + 16 * n + m;
+      if (r0 + r >= nr) continue;
+      if (it.npieces == 1) {
+        const int t = tq[n], hh = it.g * G + r0 + r - t * G;
+        const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
+        char *o = a.o + ((it.first + t) * a.so_t + hh * a.so_h + 4 * h) * 2;
+#pragma unroll
+        for (int x = 0; x < DT; ++x)
+          *(u32x2 *)(o + 32 * x) = u32x2{pack_bf16x2(oacc[n][x][0] * inv, oacc[n][x][1] * inv), pack_bf16x2(oacc[n][x][2] * inv, oacc[n][x][3] * inv)};
+        if (a.lse && h == 0)
+          a.lse[(int64_t)hh * a.q.nrows + it.first + t] = z == 0.f ? -__builtin_inff() : (mx[n] + __builtin_amdgcn_logf(z)) * kLn2;
+      } else {
+        float *o = a.po + ((int64_t)slot * a.trows + r) * D + 4 * h;
+#pragma unroll
+        for (int x = 0; x < DT; ++x) *(f32x4 *)(o + 16 * x) = oacc[n][x];
+        if (h == 0) {
+          float *ml = a.pml + ((int64_t)slot * a.trows + r) * 2;
+          ml[0] = mx[n];
+          ml[1] = z;
+        }
+      }
+    }
+    return;
+  }
+  float *so = (float *)lds, *sml = so + NW * 16 * NQ * kLd<D>;  // part wk of row group wr at rows 32 wr
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int at = wk * 32 * RW + 32 * wr + 16 * n;
     store_wave<D, true>(so + at * kLd<D>, sml + at * 2, m, h, mx[n], sum[n], oacc[n]);
   }
-  if (__any(special))
+  if (special)
     for (int s = nplain; s < nst; ++s)
       for (int i = 0; i < NT; ++i) {
         const int j = j0 + s * SR + wr0 + 32 * i;
@@ -933,20 +978,21 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
           add_special<F32, D, false>(c, it, ro, j, so + (wk * 32 * RW + 32 * wr) * kLd<D>, 32, r0 + 32 * wr, nr, G, 0, lane);
       }
   __syncthreads();
-  join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0,
-                                it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g);
+  join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0, slot);
 }
 
-// Joins the pieces of every item: a workgroup per new row and head.  Every wave reads all maxima and sums (a
-// lane per piece), so that each knows its weights before its share of the O parts arrives; LDS joins the waves.
-template <int D, bool SEL>
+// Joins the pieces of every item: WV waves per new row and head (all four of a workgroup, or one where there are so
+// many rows that the chip is full of them).  Every wave reads all maxima and sums (a lane per piece), so that each
+// knows its weights before its share of the O parts arrives; LDS joins the waves.
+template <int D, bool SEL, int WV>
 __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   __shared__ float so[kWaves][D];
   constexpr int PL = D / 64;  // dimensions per lane
   typedef float fv __attribute__((ext_vector_type(PL)));
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6), wave = WV == 1 ? 0 : wv;
   const CacheView &c = a.c;
-  const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = blockIdx.y, g = hh / G;
+  const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = WV == 1 ? blockIdx.y * kWaves + wv : blockIdx.y, g = hh / G;
+  if (hh >= a.q.hq) return;
   int slot, np, stride, row;
   bool mine = true;
   if constexpr (SEL) {
@@ -998,32 +1044,40 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   const float base = M == -__builtin_inff() ? 0.f : M;
   fv v{};
   constexpr int kAhead = 8;
-  for (int k0 = wave; k0 < np; k0 += kWaves * kAhead) {
+  for (int k0 = wave; k0 < np; k0 += WV * kAhead) {
     fv p[kAhead];
     float m[kAhead];
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) {
-      const int k = k0 + x * kWaves < np ? k0 + x * kWaves : k0;
+      const int k = k0 + x * WV < np ? k0 + x * WV : k0;
       p[x] = *(const fv *)(po + k * step * D);
       m[x] = pml[k * step * 2];
     }
 #pragma unroll
     for (int x = 0; x < kAhead; ++x)
-      if (k0 + x * kWaves < np && m[x] != -__builtin_inff()) v += p[x] * exp2_fast(m[x] - base);
+      if (k0 + x * WV < np && m[x] != -__builtin_inff()) v += p[x] * exp2_fast(m[x] - base);
   }
-  *(fv *)&so[wave][lane * PL] = v;
   if constexpr (SEL) mine = seq_of_row(c, a.q, r, lane) >= 0;
-  __syncthreads();
-  if (tid >= D / 2 || !mine) return;
+  *(fv *)&so[wv][lane * PL] = v;
+  int at = tid;
+  if constexpr (WV == 1) {
+    at = lane;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  } else {
+    __syncthreads();
+  }
+  if (at >= D / 2 || !mine) return;
   float x = 0.f, y = 0.f;
 #pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
-    x += so[k][2 * tid];
-    y += so[k][2 * tid + 1];
+  for (int k = 0; k < WV; ++k) {
+    x += so[WV == 1 ? wv : k][2 * at];
+    y += so[WV == 1 ? wv : k][2 * at + 1];
   }
   const float inv = z > 0.f ? 1.f / z : z == 0.f ? 0.f : z;
-  *(uint32_t *)(a.o + (r * a.so_t + hh * a.so_h + 2 * tid) * 2) = pack_bf16x2(x * inv, y * inv);
-  if (a.lse && tid == 0)
+  *(uint32_t *)(a.o + (r * a.so_t + hh * a.so_h + 2 * at) * 2) = pack_bf16x2(x * inv, y * inv);
+  if (a.lse && at == 0)
     a.lse[(int64_t)hh * a.q.nrows + r] = z == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(z)) * kLn2;
 }
 
@@ -1426,11 +1480,12 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   }
   // A piece of many rows writes, and the join reads, as much as 2 trows rows of fp32: where the items alone fill
   // the chip, it walks so many groups that this stays small beside K and V (49 sequences of 0 to 433 rows, 448 rows
-  // of Q per head: 215 us in pieces of one group, NEW4 us so).
+  // of Q per head: 215 us in pieces of one group, 53 us in one piece each).
   s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
   s.least = items <= resident / 2 ? 1 : s.trows / 16;
+  if (c.cap <= s.least * kGroup) s.slots = 0;  // no sequence is long enough for two pieces
   const int64_t grid = items + s.slots;
-  s.grid = (int)(grid < most ? grid : most);
+  s.grid = (int)(grid < most && s.slots ? grid : s.slots ? most : items);
   return s;
 }
 
@@ -1495,8 +1550,13 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
         draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
     });
   if (SEL ? s.pieces > 1 : s.slots > 0) {
-    const dim3 grid(a.q.nrows, a.q.hq);
-    d == 128 ? draft_join_kernel<128, SEL><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL><<<grid, 256, 0, st>>>(a);
+    if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
+      const dim3 grid(a.q.nrows, (a.q.hq + kWaves - 1) / kWaves);
+      d == 128 ? draft_join_kernel<128, SEL, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL, 1><<<grid, 256, 0, st>>>(a);
+    } else {
+      const dim3 grid(a.q.nrows, a.q.hq);
+      d == 128 ? draft_join_kernel<128, SEL, kWaves><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL, kWaves><<<grid, 256, 0, st>>>(a);
+    }
   }
   RS_HIP(hipGetLastError());
   return RS_OK;
