@@ -513,12 +513,13 @@ EvictPlan plan_at(Arena &a, int64_t items, int budget, int cap) {
   return pl;
 }
 
-// Slices of 8K rows (their counts fit 16 bits) where a cache is long enough for more than two of them; 16 at most
-// to add up for the longest.
+// Slices of 8K rows or more (their counts fit 16 bits), about 16 of them, where a cache holds more than one
+// workgroup keeps in registers: at 19K rows of 2 x 2 to 16 x 8 heads one workgroup per head takes 28 to 32 us, slices
+// 37; at 43K rows 50 to 68 (its registers spill) against 37.
 constexpr int kSliceRows = 8192;
 EvictSlices slices_at(Arena &a, int64_t items, int budget, int cap) {
   EvictSlices sl{};
-  if (cap <= 2 * kSliceRows) return sl;
+  if (cap <= 32 * kPlanThreads) return sl;
   const int r = (cap + 15) / 16;
   sl.rows = r > kSliceRows ? r : kSliceRows;
   sl.n1 = (budget + sl.rows - 1) / sl.rows;
@@ -592,8 +593,10 @@ rs_status evict_launch(const CacheView &c, int dtype, int d, int budget, int nsi
     const dim3 grid(c.hkv, c.nseq);
     if (c.cap <= 4 * kPlanThreads)
       evict_plan_kernel<4><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
-    else
+    else if (c.cap <= 16 * kPlanThreads)
       evict_plan_kernel<16><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
+    else
+      evict_plan_kernel<32><<<grid, kPlanThreads, 0, st>>>(c, budget, nsink, nrecent, pl);
   }
   const int e = dtype == RS_BF16 ? 2 : 4;
   evict_move_kernel<<<dim3((pl.most + kMoveRows - 1) / kMoveRows, c.hkv, c.nseq), 256, 0, st>>>(c, budget, pl, log2i(d * e / 16));

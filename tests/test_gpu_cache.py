@@ -211,6 +211,7 @@ def test_evict_with_equal_weights(kind):
     ([70001, 8193], 8192, 100, 1000, "random"),
     ([40000, 17000], 20001, 0, 7, "few"),        # ties across slices of rows, on both sides of the budget
     ([33333], 33332, 5, 300, "tiny"),
+    ([32000, 9000], 15000, 5, 300, "few"),
     ([20000, 100, 16500], 100, 4, 10, "equal"),
     ([150000], 60000, 0, 0, "random"),           # slices longer than 8K rows
 ])
