@@ -767,6 +767,9 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
     off[i] = (w * RPI % 64 + lr) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc;
   }
   const char *kg = c.k + it.g * c.sk_h, *vg = c.v + it.g * c.sv_h;
+  // (x[y] with y known to the wave only would put x into memory)
+  static_assert(NP <= 2, "pages of a stage");
+  auto of = [](const auto &x, int y) { return NP == 2 && y ? x[NP - 1] : x[0]; };
   auto fetch = [&](int stage, u32x4 (&x)[NI], bool (&ok)[NP]) {
     const int js = j0 + stage * SR;
     bool whole = js + SR <= total;
@@ -788,13 +791,14 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64;
-        x[i] = *(const u32x4 *)((isv ? vb[y] : kb[y]) + off[i]);
+        x[i] = *(const u32x4 *)((isv ? of(vb, y) : of(kb, y)) + off[i]);
       }
     } else {  // rows behind the end are read as the last, all without a page as its row 0
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64, r = w * RPI % 64 + lr;
-        x[i] = *(const u32x4 *)((isv ? vb[y] : kb[y]) + (r < left[y] ? r : left[y]) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc);
+        const int most = of(left, y);
+        x[i] = *(const u32x4 *)((isv ? of(vb, y) : of(kb, y)) + (r < most ? r : most) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc);
       }
     }
   };
