@@ -373,7 +373,8 @@ rs_status rs_dense_attn_prefill(const rs_qkv *qkv, const rs_unit *units, int32_t
  *   page_id = table[b * max_pages + j / page], or b * max_pages + j / page without a table.
  * A prefill writes the same rows: with head-major pages a prompt's K and V of rs_qkv are pages.
  *  - One sequence holds at most cap = max_pages * page rows, cap <= 262144.  page is a multiple
- *    of 64, or any size where max_pages == 1.  Pages of different sequences are distinct.
+ *    of 64, or any size where max_pages == 1.  Sequences may share pages that are only read; rows that a
+ *    call writes lie in pages of one sequence.
  *  - len (device) counts the rows held; it is read clamped to [0, cap].  Rows behind it are neither
  *    read nor, but by rs_cache_append, written.
  *  - A table entry outside [0, npages) names no page: rows there are not written, and no query sees
@@ -409,7 +410,9 @@ typedef struct rs_cache {
  * belong to no sequence are neither read nor written. */
 typedef struct rs_draft {
   const void *q;             /* device [nrows][hq][d] with element strides (sq_t, sq_h) */
-  int32_t hq, nrows, max_rows, nwords;  /* max_rows <= 256; nwords: words per mask row, 32 nwords >= max_rows */
+  int32_t hq, nrows, max_rows, nwords;  /* max_rows <= 256, nseq x hq x max_rows <= 2^28, nrows <= 2^20 and
+                                nrows x hkv <= 2^24; nwords: words per
+                                mask row, 32 nwords >= max_rows */
   int64_t sq_t, sq_h;
   const int32_t *start;      /* device [nseq + 1]; NULL: sequence b's rows are [b * max_rows, (b + 1) * max_rows) */
   const uint32_t *mask;      /* device [nrows][nwords], or NULL */
@@ -425,8 +428,8 @@ rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *
                           int64_t sv_t, int64_t sv_h, const int32_t *start, int32_t nrows, int32_t max_rows,
                           rs_stream stream);
 /* Keeps naccept[b] (device; clamped to [0, max_new]) of the rows behind len[b]: row len + i takes the
- * row len + path[b * max_new + i] (K, V and acc) for i < naccept[b]; path must ascend (entries outside
- * [i, max_new) are read as i); NULL: the first ones.  With a path max_new <= 256.  Then writes pos =
+ * row len + path[b * max_new + i] (K, V and acc) for i < naccept[b] (an ascending path has path[i] >= i; entries
+ * outside [i, max_new) are read as i); NULL: the first ones.  With a path max_new <= 256.  Then writes pos =
  * seen + i, the block means that the rows complete, and adds naccept to len (at most cap) and seen. */
 rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const int32_t *path, int32_t max_new,
                           rs_stream stream);

@@ -520,6 +520,7 @@ def _want(ok, what):
 def _on_device(fn, device, stream, args):
     """fn(*args, stream) on `stream` (default: the current stream of `device`), launched with `device` current."""
     import torch
+    _want(device.type == "cuda", "the tensors must be on a GPU")
     if device.index == torch.cuda.current_device():
         return _check(fn(*args, _stream(stream)))
     with torch.cuda.device(device):

@@ -67,6 +67,9 @@ static rs_status check_draft(const rs_cache *x, const rs_draft *y, DraftView *q)
   if (y->nrows < 0 || y->max_rows < 1) return fail(RS_ERR_INVALID_ARG, "draft: nrows < 0 or max_rows < 1");
   if (y->max_rows > kMaxDraft) return fail(RS_ERR_UNSUPPORTED, "draft: at most 256 new rows per sequence");
   if (y->nrows > (1 << 20)) return fail(RS_ERR_UNSUPPORTED, "draft: at most 1048576 new rows");
+  if ((int64_t)x->nseq * y->hq * y->max_rows > (1 << 28))
+    return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^28 rows of queries (nseq x hq x max_rows)");
+  if ((int64_t)y->nrows * x->hkv > (1 << 24)) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^24 new rows x key/value heads");
   if (!y->start && (int64_t)x->nseq * y->max_rows > y->nrows)
     return fail(RS_ERR_INVALID_ARG, "draft: without start every sequence has max_rows rows");
   if (y->mask && (y->nwords < 1 || (int64_t)y->nwords * 32 < y->max_rows)) return fail(RS_ERR_INVALID_ARG, "draft: mask rows shorter than max_rows");

@@ -61,6 +61,7 @@ def test_bad_caches_are_refused(kw, want):
     (dict(q=None), INV), (dict(q=4104), INV), (dict(hq=7), INV), (dict(nrows=-1), INV), (dict(max_rows=0), INV),
     (dict(max_rows=257), UNS), (dict(start=None, nrows=1), INV), (dict(mask=4096, max_rows=33), INV), (dict(sq_t=4), INV),
     (dict(scale=-1.0), INV), (dict(scale=float("nan")), INV), (dict(nrows=1 << 21), UNS),
+    (dict(hq=0), INV),
 ])
 def test_bad_drafts_are_refused(kw, want):
     L = _rs.lib()
@@ -214,3 +215,21 @@ def test_no_new_rows_are_nothing_to_do():
     assert attend(c, d, o=None, ws=None) == _rs.RS_OK and attend(c, d, o=None, ws=None, nsel=4) == _rs.RS_OK
     assert L.rs_attn_weights(C.byref(c), C.byref(d), None, None, None, None, None) == _rs.RS_OK
     assert L.rs_cache_append(C.byref(c), None, None, 0, 0, 0, 0, 4096, 0, 1, None) == _rs.RS_OK
+
+
+def test_batches_beyond_the_index_range_are_refused():
+    c = cache(nseq=60000, npages=8)
+    assert attend(c, draft(hq=64, max_rows=256)) == UNS
+    assert attend(cache(nseq=60000, hkv=64), draft(hq=64, nrows=1 << 19)) == UNS
+
+
+def test_tensors_in_host_memory_are_refused():
+    import torch
+    k, n = torch.zeros(2, 2, 64, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    c, d = _rs.KvCache(k, k, n, kmean=torch.zeros(2, 2, 1, 64, dtype=torch.bfloat16)), _rs.Draft(k[:, :, 0].contiguous())
+    o, acc = torch.zeros(2, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64)
+    for f in (lambda: _rs.rs_draft_attn(c, d, o, None, None), lambda: _rs.rs_select_attn(c, d, 1, 0, 0, o, None, None),
+              lambda: _rs.rs_attn_weights(c, d, torch.zeros(2, 2), None, acc), lambda: _rs.rs_cache_append(c, o, o),
+              lambda: _rs.rs_cache_commit(c, n, 1), lambda: _rs.rs_cache_evict(c, 1, 0, 0, None)):
+        with pytest.raises(ValueError, match="GPU"):
+            f()

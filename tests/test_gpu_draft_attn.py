@@ -200,3 +200,17 @@ def test_two_streams_and_graph_replays():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, eager) and torch.equal(l, el)
+
+
+def test_shared_pages_and_head_major_outputs():
+    """Sequences that share the pages of their beginning; O as [hq][nrows][d]."""
+    import torch
+    s = Setup(23, [200, 330, 64], [2, 1, 3], hq=8, hkv=2, d=128, page=64)
+    s.table[1, :3] = s.table[0, :3]
+    s.table[2, 0] = s.table[0, 0]
+    s.dtable.copy_(torch.from_numpy(s.table))
+    c = s.cache()
+    o = torch.full((s.hq, s.nrows, s.d), -7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(s.hq, s.nrows, device="cuda")
+    _rs.rs_draft_attn(c, s.draft, o.transpose(0, 1), lse, _rs.workspace(_rs.rs_draft_attn_workspace_size(c, s.draft)))
+    check_rows(s, s.oracle(), o.transpose(0, 1), lse)

@@ -37,6 +37,7 @@ def check(s, kmean, got, nsel, nsink=0, nlocal=0):
     (20, 1, 64, "bf16", 256, "head", [5000], [1], None, 40, 1, 4),        # 20 heads of one group, several pieces
     (8, 2, 64, "bf16", 64, "head", [640, 641, 700], [2, 1, 5], "random", 50, 3, 5),  # every block is taken
     (40, 1, 128, "f32", 64, "head", [1200], [2], None, 1, 0, 1),          # the forced block alone; two row tiles
+    (4, 2, 64, "bf16", 64, "head", [300, 0, 777] * 30, [1, 2, 1] * 30, None, 3, 1, 1),  # more sequences than lanes
 ])
 def test_selected_blocks(hq, hkv, d, dtype, page, layout, lens, rows, kind, nsel, nsink, nlocal):
     s = Setup(len(lens) + hq, lens, rows, hq=hq, hkv=hkv, d=d, dtype=dtype, page=page, layout=layout, kind=kind, extra=2, spread=2.0)
