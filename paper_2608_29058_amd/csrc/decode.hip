@@ -12,8 +12,8 @@
 //     whose S the lane holds, so P needs no exchange of lanes; and the lane reads dimensions
 //     (d / 16) m ... of those 8 rows, a whole row per 16 lanes, whose transposition into the instructions'
 //     operands (dimension (d / 16) m + t of the t-th) stays inside the lane: one v_perm per two values.
-// Each wave takes every fourth tile of 32 rows with a running maximum and sum of its own and keeps the next
-// tile in flight; the four waves are joined once, through LDS, at the end.
+// Each of the four (short caches: eight) waves takes every fourth (eighth) tile of 32 rows with a running maximum and
+// sum of its own and keeps the next tile in flight; the waves are joined once, through LDS, at the end.
 #include "common.h"
 #include "cache.h"
 
@@ -339,6 +339,7 @@ __device__ __forceinline__ void add_values(const VTile<F32, D> &v, const u32x4 (
 // Sequences differ in length, and their lengths are known on the device only.  Every workgroup reads all
 // lengths and derives the same plan: the pieces of every item (sequence, head, row tile) in groups of 128
 // rows, equal to within one, so that all items together make about `slots` pieces.
+
 // Pieces of a sequence of `tiles` groups at `per` groups a piece.
 RS_HD int pieces_of(int tiles, int per) { return tiles > per ? (tiles + per - 1) / per : 1; }
 
@@ -521,12 +522,12 @@ __device__ __forceinline__ void join_waves(const DraftArgs &a, const Item &it, c
   }
 }
 
-// NQ: 16-row tiles of Q per wave.
-template <bool F32, int D, int NQ, bool SEL>
-__global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draft_kernel(const DraftArgs a) {
+// NQ: 16-row tiles of Q per wave; W: waves (8 only where every item is one piece).
+template <bool F32, int D, int NQ, bool SEL, int W = kWaves>
+__global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1)) ? 1 : 2) void draft_kernel(const DraftArgs a) {
   using T = Tile<F32, D>;
   constexpr int KC = T::KC, DT = T::DT, E = F32 ? 4 : 2, QP = F32 ? 2 : 1;
-  __shared__ float so[kWaves * 16 * NQ * kLd<D>], sml[kWaves * 16 * NQ * 2];
+  __shared__ float so[W * 16 * NQ * kLd<D>], sml[W * 16 * NQ * 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4;
   Item it;
@@ -615,11 +616,11 @@ __global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draf
 
   const RowsOf ro{&a.q, len, total, it.t, it.first};
   bool special = false;  // an edge held infinities or NaN
-  auto compute = [&](T &kv, const TileAt &at, int j) {
-    if (!at.ok) return;  // no page: nobody sees these rows
-    f32x4 sc[2][NQ];
+  auto scores = [&](const T &kv, f32x4 (&sc)[2][NQ]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) score_rows<F32, D, NQ>(kv.k[u], q, sc[u]);
+  };
+  auto use = [&](T &kv, int j, f32x4 (&sc)[2][NQ]) {
     if (j + kTile > len) {
       mask_scores<NQ>(ro, tq, j, h, sc);
       special = clean_values<F32, D>(kv.v) || special;
@@ -628,18 +629,47 @@ __global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draf
     weigh<D, NQ, 1>(sc, a.q.c, mx, sum, oacc, pb);
     add_values<F32, D, NQ>(kv.v, pb[0], oacc);
   };
+  auto compute = [&](T &kv, const TileAt &at, int j) {
+    if (!at.ok) return;  // no page: nobody sees these rows
+    f32x4 sc[2][NQ];
+    scores(kv, sc);
+    use(kv, j, sc);
+  };
 
-  // two tiles take turns: one is in flight while the other is used
   const int s_end = g1 * kGroup < steps ? g1 * kGroup : steps;
   int s = g0 * kGroup + wave * kTile;
-  if (s < s_end) {
+  if constexpr (F32 && (D == 128 || NQ > 1)) {
+    // two tiles do not fit the registers: the next K is in flight while V is used, and the other way round (16
+    // sequences of 16000 rows, 8 heads of 128: one token 405 us, eight 425, at 5.2 TB/s; with two tiles, part of
+    // them in scratch, 689 and 1507)
+    if (s < s_end) {
+      T t;
+      int j, jn = 0;
+      TileAt at = place(s, j), an{};
+      load_k<F32, D>(t, at, c.sk_t, m, h);
+      load_v<F32, D>(t, at, c.sv_t, m, h);
+      while (true) {
+        s += W * kTile;
+        const bool more = s < s_end;
+        if (more) an = place(s, jn);
+        f32x4 sc[2][NQ];
+        scores(t, sc);
+        if (more) load_k<F32, D>(t, an, c.sk_t, m, h);
+        if (at.ok) use(t, j, sc);
+        if (!more) break;
+        load_v<F32, D>(t, an, c.sv_t, m, h);
+        at = an, j = jn;
+      }
+    }
+  } else if (s < s_end) {
+    // two tiles take turns: one is in flight while the other is used
     T ta, tb;
     int ja, jb = 0;
     TileAt aa = place(s, ja), ab{};
     load_k<F32, D>(ta, aa, c.sk_t, m, h);
     load_v<F32, D>(ta, aa, c.sv_t, m, h);
     while (true) {
-      s += kGroup;
+      s += W * kTile;
       const bool more = s < s_end;
       if (more) {
         ab = place(s, jb);
@@ -648,7 +678,7 @@ __global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draf
       }
       compute(ta, aa, ja);
       if (!more) break;
-      s += kGroup;
+      s += W * kTile;
       const bool again = s < s_end;
       if (again) {
         aa = place(s, ja);
@@ -665,14 +695,14 @@ __global__ __launch_bounds__(256, D == 128 && (F32 || NQ > 1) ? 1 : 2) void draf
   for (int n = 0; n < NQ; ++n)
     store_wave<D, false>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
   if (special)
-    for (s = g0 * kGroup + wave * kTile; s < s_end; s += kGroup) {
+    for (s = g0 * kGroup + wave * kTile; s < s_end; s += W * kTile) {
       const int j = uniform(row_of(s));
       if (j + kTile > len && tile_at(c, it.b, it.g, j, total).ok)
         add_special<F32, D, SEL>(c, it, ro, j, &so[wave * NQ * 16 * kLd<D>], 16 * NQ, r0, nr, G, row_t0, lane);
     }
   __syncthreads();
   const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
-  join_waves<D, kWaves, 256, SEL>(a, it, so, sml, 16 * NQ, r0, nr, G, row_t0, slot);
+  join_waves<D, W, 64 * W, SEL>(a, it, so, sml, 16 * NQ, r0, nr, G, row_t0, slot);
 }
 
 // Many rows (a tree: more than 32 per head).  Streaming K and V into each wave's registers would read them once
@@ -1301,7 +1331,7 @@ constexpr int kRowsLds = 512;  // rows of Q whose factors LDS holds
 
 // NQ: 16-row tiles of Q kept in registers; 0: more rows than that, Q is read again for every 64 cached rows.
 template <bool F32, int D, int NQ>
-__global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
+__global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weights_kernel(const WeightArgs a) {
   constexpr int KC = D / 32, E = F32 ? 4 : 2, QP = F32 ? 2 : 1, NK = NQ ? NQ : 1;
   constexpr int NU = F32 && D == 128 ? 2 : 4, RW = 16 * NU;  // 16-row pieces of K in a wave's step (registers)
   __shared__ float sl[kRowsLds], sw[kRowsLds];
@@ -1339,6 +1369,15 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
       for (int y = 0; y < QP; ++y) k[i][y] = *(const u32x4 *)(x + i * 32 * E + 16 * y);
   };
 
+  // fp32: the values of 16 rows become their bf16 parts, once for all tiles of Q (one tile: as it uses them)
+  auto split = [&](u32x4 (&k)[KC][QP]) {
+    if constexpr (F32 && NQ != 1)
+#pragma unroll
+      for (int i = 0; i < KC; ++i) {
+        const f32x4 x = __builtin_bit_cast(f32x4, k[i][0]), y = __builtin_bit_cast(f32x4, k[i][1]);
+        split8(x, y, k[i][0], k[i][1]);
+      }
+  };
   u32x4 q[NK][KC][QP];
   if constexpr (NQ > 0)
 #pragma unroll
@@ -1351,8 +1390,8 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 #pragma unroll
     for (int x = 0; x < KC; ++x) {
       if constexpr (F32) {
-        u32x4 kh, kl;
-        split8(__builtin_bit_cast(f32x4, kk[x][0]), __builtin_bit_cast(f32x4, kk[x][1]), kh, kl);
+        u32x4 kh = kk[x][0], kl = kk[x][1];
+        if constexpr (NQ == 1) split8(__builtin_bit_cast(f32x4, kk[x][0]), __builtin_bit_cast(f32x4, kk[x][1]), kh, kl);
         s = mfma16(qq[x][0], kl, s);
         s = mfma16(qq[x][1], kh, s);
         s = mfma16(qq[x][0], kh, s);
@@ -1397,23 +1436,10 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 #pragma unroll
       for (int u = 0; u < NU; ++u) load_k(j0 + 16 * u < end ? j0 + 16 * u : j0, x[u], o[u]);
     };
-    auto step = [&](int j0, const u32x4 (&x)[NU][KC][QP], const bool (&o)[NU]) {
-      float sum[NU] = {};
-      if constexpr (NQ > 0) {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int u = 0; u < NU; ++u) add(q[n], x[u], 16 * n, j0 + 16 * u, sum[u]);
-      } else {
-        for (int r0 = 0; r0 < rows; r0 += 16) {
-          load_q(base + r0, q[0]);
-#pragma unroll
-          for (int u = 0; u < NU; ++u) add(q[0], x[u], r0, j0 + 16 * u, sum[u]);
-        }
-      }
+    // lane (m, h) writes row 16 h + m
+    auto finish = [&](int j0, float (&sum)[NU], const bool (&o)[NU]) {
 #pragma unroll
       for (int u = 0; u < NU; ++u) sum[u] = sum4(sum[u]);
-      // lane (m, h) writes row 16 h + m
       float x0 = sum[0];
       bool has = o[0];
 #pragma unroll
@@ -1427,9 +1453,53 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
         a.acc_out[at + j] = in + x0;
       }
     };
+    auto step = [&](int j0, u32x4 (&x)[NU][KC][QP], const bool (&o)[NU]) {
+      float sum[NU] = {};
+      if constexpr (NQ > 0) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int u = 0; u < NU; ++u) add(q[n], x[u], 16 * n, j0 + 16 * u, sum[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) split(x[u]);
+        for (int r0 = 0; r0 < rows; r0 += 16) {
+          load_q(base + r0, q[0]);
+#pragma unroll
+          for (int u = 0; u < NU; ++u) add(q[0], x[u], r0, j0 + 16 * u, sum[u]);
+        }
+      }
+      finish(j0, sum, o);
+    };
     int j = first + wave * RW;
     if (j >= end) continue;
     fetch(j, k, ok);
+    if constexpr (F32 && NQ > 1) {
+      // two steps do not fit the registers: 16 rows at a time become bf16 parts and make room for the next step's
+      // (16 sequences of 16000 rows, 8 heads of 128, 32 rows of Q: 206 us; read again for every 16 rows of Q: 378)
+      while (true) {
+        const int jn = j + 4 * RW;
+        float sum[NU] = {};
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          split(k[u]);
+          u32x4 x[KC][QP];
+#pragma unroll
+          for (int i = 0; i < KC; ++i)
+#pragma unroll
+            for (int y = 0; y < QP; ++y) x[i][y] = k[u][i][y];
+          if (jn < end) load_k(jn + 16 * u < end ? jn + 16 * u : jn, k[u], okn[u]);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) add(q[n], x, 16 * n, j + 16 * u, sum[u]);
+        }
+        finish(j, sum, ok);
+        if (jn >= end) break;
+        j = jn;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) ok[u] = okn[u];
+      }
+      continue;
+    }
     while (true) {
       if (j + 4 * RW < end) fetch(j + 4 * RW, kn, okn);
       step(j, k, ok);
@@ -1452,13 +1522,14 @@ int tile_rows(bool f32, bool sel, int rows) {
 }
 
 struct DraftShape {
-  int trows, rtiles, slots, least, grid, pieces;
+  int trows, rtiles, slots, least, grid, pieces, waves;
 };
 
 constexpr int kShort = 256;
 
 DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
   DraftShape s{};
+  s.waves = kWaves;
   const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
   s.trows = tile_rows(f32, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
@@ -1474,10 +1545,12 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
     return s;
   }
   const int64_t items = (int64_t)c.nseq * c.hkv * s.rtiles, most = items * ((c.cap + kGroup - 1) / kGroup);
-  // A cache of up to kShort rows stays in one piece and needs no joining launch (4 us).  Longer ones gain from pieces
-  // (one token over 1001 rows, 8 heads: 16 us in one piece, 13 with the launch): few items make one round of
-  // workgroups; many, pieces of a quarter of a round, so that the last round is short.
-  if (c.cap <= kShort) {
+  // A short cache stays in one piece and needs no joining launch (4 us): up to kShort rows in four waves, twice that in
+  // eight where a CU holds two waves per SIMD (8 heads over 500 rows: one sequence 12.6 -> 10.0 us, 64 of them 36.7 ->
+  // 27.5).  Longer ones gain from pieces (one token over 1001 rows: 14.7 us in one piece, 12.3 in several): few items
+  // make one round of workgroups; many, pieces of a quarter of a round, so that the last round is short.
+  if (c.cap <= (resident == 512 ? 2 * kShort : kShort)) {
+    s.waves = c.cap > kShort ? 8 : kWaves;
     s.slots = 0;
     s.grid = (int)items;
     return s;
@@ -1550,8 +1623,11 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
       constexpr int D = decltype(dd)::value, NQ = decltype(nn)::value;
       if constexpr (SEL)
         draft_kernel<F, D, NQ, true><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
-      else
+      else {
+        if constexpr (D == 64 || (!F && NQ == 1))
+          if (s.waves > kWaves) return draft_kernel<F, D, NQ, false, 8><<<s.grid, 512, 0, st>>>(a);
         draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
+      }
     });
   if (SEL ? s.pieces > 1 : s.slots > 0) {
     if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
@@ -1618,12 +1694,13 @@ rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d
   auto run = [&](auto x, auto dd) {
     constexpr bool F = decltype(x)::value;
     constexpr int DD = decltype(dd)::value;
-    if (rows <= 16)
-      weights_kernel<F, DD, 1><<<grid, 256, 0, st>>>(a);
-    else if (rows > 32 || F)
-      weights_kernel<F, DD, 0><<<grid, 256, 0, st>>>(a);
-    else if constexpr (!F)
-      weights_kernel<F, DD, 2><<<grid, 256, 0, st>>>(a);
+    // (16 sequences of 16000 rows, 8 heads, 64 rows of Q each: fp32 289 us in four tiles kept, 535 read again; bf16 181
+    // and 158)
+    if (rows <= 16) return weights_kernel<F, DD, 1><<<grid, 256, 0, st>>>(a);
+    if (rows <= 32) return weights_kernel<F, DD, 2><<<grid, 256, 0, st>>>(a);
+    if constexpr (F)
+      if (rows <= 64) return weights_kernel<F, DD, 4><<<grid, 256, 0, st>>>(a);
+    weights_kernel<F, DD, 0><<<grid, 256, 0, st>>>(a);
   };
   auto with_d = [&](auto x) { d == 128 ? run(x, std::integral_constant<int, 128>{}) : run(x, std::integral_constant<int, 64>{}); };
   f32 ? with_d(std::true_type{}) : with_d(std::false_type{});

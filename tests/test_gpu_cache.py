@@ -124,6 +124,10 @@ def test_append_and_commit_stop_at_the_capacity_and_at_missing_pages():
     (24, 2, 64, "bf16", [200, 3], [90, 40], "tree", 64),      # 1080 rows of Q per head: in parts of 512
     (12, 1, 128, "f32", [70], [50], None, 128),
     (4, 2, 64, "bf16", [9, 2100] * 40, [1] * 80, None, 64),   # more sequences than a wave has lanes
+    (8, 2, 128, "f32", [2000, 1, 500], [8, 2, 5], "tree", 64),       # 32 rows of Q
+    (14, 2, 64, "f32", [1111, 64], [3, 4], None, 64),                # 28
+    (16, 2, 128, "f32", [1500, 0, 77], [8, 3, 6], "random", 128),    # 64
+    (7, 1, 64, "f32", [2049, 31], [9, 8], "tree", 64),               # 63
 ])
 def test_weights(hq, hkv, d, dtype, lens, rows, kind, page):
     import torch

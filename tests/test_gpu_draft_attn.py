@@ -62,6 +62,34 @@ def test_drafted_rows(hq, hkv, d, dtype, lens, rows, kind):
         assert empty.any() and (o[:used].cpu().float().numpy()[empty.T] == 0).all()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype,t", [
+    (8, 2, 128, "bf16", 3), (28, 4, 64, "bf16", 4), (4, 4, 64, "f32", 2), (10, 2, 64, "f32", 5), (8, 2, 128, "f32", 7)])
+@pytest.mark.parametrize("top", [250, 300, 505])
+def test_caches_of_one_piece(hq, hkv, d, dtype, t, top):
+    """Capacities around those that are attended in one piece, with infinities and NaN behind the ends."""
+    lens = [top, 0, 1, 31, 32, 127, 128, 224, 225, 249, top - 32]
+    rows = [1 + (3 * i) % t for i in range(len(lens))]
+    s = Setup(top + hq, lens, rows, hq=hq, hkv=hkv, d=d, dtype=dtype, kind="tree" if t > 2 else None, spread=2.0)
+    for b, n in enumerate(s.lens + s.counts):
+        p, j = divmod(int(n), 64)
+        if p < s.table.shape[1] and s.table[b, p] >= 0:
+            s.dk[int(s.table[b, p]), :, j:], s.dv[int(s.table[b, p]), :, j:] = float("inf"), float("nan")
+    o, l = run(s)
+    check_rows(s, s.oracle(), o, l)
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,rows,kind", [
+    (8, 2, 128, [2500, 40, 700], [8, 5, 2], "tree"),     # 32 rows of Q
+    (5, 1, 128, [5000], [5], None),                      # 25
+    (3, 1, 128, [3001, 0, 900], [5, 1, 3], "tree"),      # 15
+    (12, 2, 64, [4100, 333], [4, 5], "random"),          # 30
+])
+def test_long_fp32_caches(hq, hkv, d, lens, rows, kind):
+    s = Setup(hq * d, lens, rows, hq=hq, hkv=hkv, d=d, dtype="f32", kind=kind, page=128, spread=2.0)
+    o, l = run(s)
+    check_rows(s, s.oracle(), o, l)
+
+
 @pytest.mark.parametrize("lens,rows,hq,hkv,kind", [
     ([20011], [1], 8, 2, None),                 # one item per head, many pieces
     ([9000, 1, 0, 4097], [16, 1, 1, 3], 4, 1, "tree"),
