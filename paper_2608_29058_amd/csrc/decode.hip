@@ -1327,15 +1327,18 @@ struct WeightArgs {
   int rows;  // cached rows per workgroup
 };
 
-constexpr int kRowsLds = 512;  // rows of Q whose factors LDS holds
-
-// NQ: 16-row tiles of Q kept in registers; 0: more rows than that, Q is read again for every 64 cached rows.
+// NQ: 16-row tiles of Q kept in registers; 0: more rows than that, 128 at a time in LDS (in the order and parts in
+// which the instructions take them), and K once for each of these.  16 sequences of 16000 rows, 8 heads of 128: 64
+// rows of Q 125 us in bf16 (158 with Q read from memory for every 64 cached rows, 181 from registers) and 214 in
+// fp32 (535; floor 205); 256 rows 290 and 519.
 template <bool F32, int D, int NQ>
-__global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weights_kernel(const WeightArgs a) {
+__global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
   constexpr int KC = D / 32, E = F32 ? 4 : 2, QP = F32 ? 2 : 1, NK = NQ ? NQ : 1;
-  constexpr int NU = F32 && D == 128 ? 2 : 4, RW = 16 * NU;  // 16-row pieces of K in a wave's step (registers)
+  constexpr int NU = F32 && (D == 128 || NQ == 0) ? 2 : 4, RW = 16 * NU;  // 16-row pieces of K in a wave's step (registers)
+  constexpr int kRowsLds = NQ ? 16 * NQ : 128;  // rows of Q whose factors (and values) LDS holds
   __shared__ float sl[kRowsLds], sw[kRowsLds];
   __shared__ int st[kRowsLds];
+  __shared__ u32x4 sq[NQ ? 1 : kRowsLds / 16][KC][QP][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4, g = blockIdx.y, b = blockIdx.z;
   const CacheView &c = a.c;
@@ -1416,8 +1419,16 @@ __global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weig
     }
   };
 
-  for (int base = 0; base < nr; base += kRowsLds) {  // (once, but for the widest groups of the most rows)
+  for (int base = 0; base < nr; base += kRowsLds) {  // (once, but for more rows than LDS holds)
     __syncthreads();
+    if constexpr (NQ == 0)
+      for (int x = wave; x < kRowsLds / 16 && base + 16 * x < nr; x += 4) {
+        load_q(base + 16 * x, q[0]);
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+#pragma unroll
+          for (int y = 0; y < QP; ++y) sq[x][i][y][lane] = q[0][i][y];
+      }
     for (int x = tid; x < kRowsLds; x += 256) {
       const int r = base + x, t = r < nr ? r / G : 0;
       const float l = r < nr ? a.lse[(int64_t)(g * G + r - t * G) * a.q.nrows + rr.first + t] * kLog2e : 0.f;
@@ -1464,7 +1475,10 @@ __global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weig
 #pragma unroll
         for (int u = 0; u < NU; ++u) split(x[u]);
         for (int r0 = 0; r0 < rows; r0 += 16) {
-          load_q(base + r0, q[0]);
+#pragma unroll
+          for (int i = 0; i < KC; ++i)
+#pragma unroll
+            for (int y = 0; y < QP; ++y) q[0][i][y] = sq[r0 / 16][i][y][lane];
 #pragma unroll
           for (int u = 0; u < NU; ++u) add(q[0], x[u], r0, j0 + 16 * u, sum[u]);
         }
@@ -1476,7 +1490,7 @@ __global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weig
     fetch(j, k, ok);
     if constexpr (F32 && NQ > 1) {
       // two steps do not fit the registers: 16 rows at a time become bf16 parts and make room for the next step's
-      // (16 sequences of 16000 rows, 8 heads of 128, 32 rows of Q: 206 us; read again for every 16 rows of Q: 378)
+      // (16 sequences of 16000 rows, 8 heads of 128, 32 rows of Q: 198 us; 378 with Q read again for every 16 rows)
       while (true) {
         const int jn = j + 4 * RW;
         float sum[NU] = {};
@@ -1497,6 +1511,16 @@ __global__ __launch_bounds__(256, F32 && (NQ == 0 || NQ == 4) ? 1 : 2) void weig
         j = jn;
 #pragma unroll
         for (int u = 0; u < NU; ++u) ok[u] = okn[u];
+      }
+      continue;
+    }
+    if constexpr (F32 && NQ == 0 && D == 128) {
+      // (the steps are long: the SIMD's other wave covers their loads, and nothing goes to scratch)
+      while (true) {
+        step(j, k, ok);
+        j += 4 * RW;
+        if (j >= end) break;
+        fetch(j, k, ok);
       }
       continue;
     }
@@ -1694,12 +1718,8 @@ rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d
   auto run = [&](auto x, auto dd) {
     constexpr bool F = decltype(x)::value;
     constexpr int DD = decltype(dd)::value;
-    // (16 sequences of 16000 rows, 8 heads, 64 rows of Q each: fp32 289 us in four tiles kept, 535 read again; bf16 181
-    // and 158)
     if (rows <= 16) return weights_kernel<F, DD, 1><<<grid, 256, 0, st>>>(a);
     if (rows <= 32) return weights_kernel<F, DD, 2><<<grid, 256, 0, st>>>(a);
-    if constexpr (F)
-      if (rows <= 64) return weights_kernel<F, DD, 4><<<grid, 256, 0, st>>>(a);
     weights_kernel<F, DD, 0><<<grid, 256, 0, st>>>(a);
   };
   auto with_d = [&](auto x) { d == 128 ? run(x, std::integral_constant<int, 128>{}) : run(x, std::integral_constant<int, 64>{}); };

@@ -121,7 +121,7 @@ def test_append_and_commit_stop_at_the_capacity_and_at_missing_pages():
     (8, 1, 128, "f32", [130, 64], [9, 20], "tree", 64),
     (16, 16, 64, "f32", [90], [4], "random", 64),
     (4, 2, 128, "bf16", [700, 0, 40], [40, 3, 0], "random", 64),
-    (24, 2, 64, "bf16", [200, 3], [90, 40], "tree", 64),      # 1080 rows of Q per head: in parts of 512
+    (24, 2, 64, "bf16", [200, 3], [90, 40], "tree", 64),      # 1080 rows of Q per head: in parts
     (12, 1, 128, "f32", [70], [50], None, 128),
     (4, 2, 64, "bf16", [9, 2100] * 40, [1] * 80, None, 64),   # more sequences than a wave has lanes
     (8, 2, 128, "f32", [2000, 1, 500], [8, 2, 5], "tree", 64),       # 32 rows of Q
