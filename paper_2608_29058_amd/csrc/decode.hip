@@ -706,15 +706,19 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
 }
 
 // Many rows (a tree: more than 32 per head).  Streaming K and V into each wave's registers would read them once
-// per 32 rows; here 8 waves share a stage in LDS: 8 / KW groups of 32 rows of Q, KW parts of the stage (64, 128 or
-// 256 rows per workgroup), one or two tiles of 32 rows per wave and stage.  A stage travels through registers (the
+// per 32 rows; here NW waves share a stage in LDS: NW / KW groups of 32 rows of Q (64, 128 or 256 rows per workgroup),
+// KW parts of the stage, one or two tiles of 32 rows per wave and stage.  A stage travels through registers (the
 // next one is in flight meanwhile), is written to one of two buffers and read after one barrier.  The 16-byte
 // chunks of a row are permuted by an XOR with the row, so that the reads spread over all banks; V is read
 // transposed (ds_read_b64_tr_b16).  At 256 rows, per wave and 64 rows of the cache: 64 v_mfma of 16 cycles, 32
-// v_exp of 16 and about 190 other vector instructions of 4; LDS passes 32 KB to each wave.  61 rows x 4 heads per
-// group over 128K rows: 195 us, 0.67 of 1.22 PFLOP/s; what is left over the matrix instructions is their lockstep
-// with the exponents (one barrier per stage).  64 rows per wave halve the LDS traffic, but O then lives in
-// accumulation registers and is copied at every rescale test: 418 us.
+// v_exp of 16 and about 190 other vector instructions of 4; LDS passes 32 KB to each wave.
+// A stage's barrier keeps its waves in step, so that they wait for the matrix unit together and then for the vector
+// unit.  With four waves, two workgroups share a CU and fill each other's gaps (16 sequences of 16000 rows, 8 heads,
+// four waves against eight: 64 rows of Q 203 against 303 us, 96 rows 221 / 367, 256 rows of d = 64 293 / 390, in fp32
+// 568 / 713).  With d = 128 and 256 rows they would read K and V twice; eight waves stay ahead there (61 rows x 4
+// heads per group over 128K rows: 195 us, 0.67 of 1.22 PFLOP/s; 208 in two tiles of 128).  64 rows per wave halve the
+// LDS traffic, but O then lives in accumulation registers and is copied at every rescale test: 418 us.
+
 // Chunks of K: 16 rows' equal chunks in different banks; of V: the chunk pairs 2t, 2t + 1 of 8 rows.
 template <int D>
 __device__ __forceinline__ int chunk_xor(int r) {
@@ -722,10 +726,10 @@ __device__ __forceinline__ int chunk_xor(int r) {
 }
 
 // F32: values are split into their bf16 parts as they enter LDS, a plane each.
-template <bool F32, int D, int KW>
-__global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
-  constexpr int NT = KW == 4 || F32 ? 1 : 2;                     // tiles of 32 rows per wave and stage
-  constexpr int NQ = 2, NW = 8, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
+template <bool F32, int D, int KW, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void draft_wide_kernel(const DraftArgs a) {
+  constexpr int NT = KW == 2 || F32 ? 1 : 2;                 // tiles of 32 rows per wave and stage
+  constexpr int NQ = 2, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
   constexpr int E = F32 ? 4 : 2, QP = F32 ? 2 : 1;                // bytes of a value; bf16 parts of it
   constexpr int KC = D / 32, DT = D / 16, CPR = D * E / 16, RPI = 64 / CPR;
   constexpr int NI = 2 * SR / RPI / NW;  // 16-byte loads per lane and stage, K before V
@@ -1012,7 +1016,7 @@ __global__ __launch_bounds__(512, 2) void draft_wide_kernel(const DraftArgs a) {
           add_special<F32, D, false>(c, it, ro, j, so + (wk * 32 * RW + 32 * wr) * kLd<D>, 32, r0 + 32 * wr, nr, G, 0, lane);
       }
   __syncthreads();
-  join_waves<D, KW, 512, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0, slot);
+  join_waves<D, KW, 64 * NW, false>(a, it, so, sml, 32 * RW, r0, nr, G, 0, slot);
 }
 
 // Joins the pieces of every item: WV waves per new row and head (all four of a workgroup, or one where there are so
@@ -1538,11 +1542,15 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 }
 
 // ---- launches --------------------------------------------------------------------------------------
-// Rows of an item: up to 32 are held by every wave (16 or 32); more of them share stages (64, 128 or 256 per
-// workgroup; fp32 stages are twice as large and serve 128 or 256).  Selections belong to one token, whose heads rarely
-// are that many: row tiles of 32.
-int tile_rows(bool f32, bool sel, int rows) {
-  return rows <= 16 ? 16 : rows <= 32 || sel ? 32 : rows <= 64 && !f32 ? 64 : rows <= 128 ? 128 : 256;
+// Rows of an item: up to 32 are held by every wave (16 or 32); more of them share stages, in tiles of 64 or 128 rows (four
+// waves, two workgroups per CU; fp32 and d = 64 only gain from 128), or of 256 where that pads less: up to 192 rows
+// of d = 128 take three tiles of 64 (16 x 16000 rows, 132 rows of Q: 373 us, 520 in one tile of 256), an odd number of
+// 128s those (44 sequences of 1 to 1599 rows, 264 rows of Q: 88 us, 133 in two of 256).  Selections belong to one
+// token, whose heads rarely are that many: row tiles of 32.
+int tile_rows(bool f32, int d, bool sel, int rows) {
+  if (rows <= 32 || sel) return rows <= 16 ? 16 : 32;
+  if (!f32 && (rows <= 64 || (d == 128 && rows > 128 && rows <= 192))) return 64;
+  return f32 || d == 64 || (rows + 127) / 128 % 2 ? 128 : 256;
 }
 
 struct DraftShape {
@@ -1555,10 +1563,11 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   DraftShape s{};
   s.waves = kWaves;
   const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
-  s.trows = tile_rows(f32, nsel > 0, rows);
+  s.trows = tile_rows(f32, d, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
-  // workgroups that the chip holds at once: two per CU with d = 64 or 16 rows of bf16, else one
-  const int resident = s.trows <= 32 && (d == 64 || (!f32 && s.trows == 16)) ? 512 : 256;
+  // workgroups that the chip holds at once: two per CU of four waves with d = 64, 16 rows of bf16 or stages, else one
+  const bool two = d == 64 || (!f32 && s.trows == 16), wide = s.trows > 32;
+  const int resident = (wide ? s.trows < 256 : two) ? 512 : 256;
   if (nsel) {
     const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
     const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
@@ -1573,7 +1582,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   // eight where a CU holds two waves per SIMD (8 heads over 500 rows: one sequence 12.6 -> 10.0 us, 64 of them 36.7 ->
   // 27.5).  Longer ones gain from pieces (one token over 1001 rows: 14.7 us in one piece, 12.3 in several): few items
   // make one round of workgroups; many, pieces of a quarter of a round, so that the last round is short.
-  if (c.cap <= (resident == 512 ? 2 * kShort : kShort)) {
+  if (c.cap <= (two && !wide ? 2 * kShort : kShort)) {
     s.waves = c.cap > kShort ? 8 : kWaves;
     s.slots = 0;
     s.grid = (int)items;
@@ -1581,9 +1590,10 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   }
   // A piece of many rows writes, and the join reads, as much as 2 trows rows of fp32: where the items alone fill
   // the chip, it walks so many groups that this stays small beside K and V (49 sequences of 0 to 433 rows, 448 rows
-  // of Q per head: 215 us in pieces of one group, 53 us in one piece each).
+  // of Q per head: 215 us in pieces of one group, 53 us in one piece each; 33 sequences of 2000 to 8000 rows, 132 rows
+  // in tiles of 128: 448 us from 8 groups on, 347 from 16).
   s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
-  s.least = items <= resident / 2 ? 1 : s.trows / 16;
+  s.least = items <= resident / 2 ? 1 : s.trows >= 128 ? 16 : s.trows / 16;
   if (c.cap <= s.least * kGroup) s.slots = 0;  // no sequence is long enough for two pieces
   const int64_t grid = items + s.slots;
   s.grid = (int)(grid < most && s.slots ? grid : s.slots ? most : items);
@@ -1603,12 +1613,11 @@ void by_tiles(bool f32, int d, int trows, F f) {
 
 template <bool F32, int D>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
-  if (s.trows == 256)
-    draft_wide_kernel<F32, D, 1><<<s.grid, 512, 0, st>>>(a);
-  else if (s.trows == 128)
-    draft_wide_kernel<F32, D, 2><<<s.grid, 512, 0, st>>>(a);
-  else if constexpr (!F32)
-    draft_wide_kernel<F32, D, 4><<<s.grid, 512, 0, st>>>(a);
+  if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4><<<s.grid, 256, 0, st>>>(a);
+  if constexpr (!F32) {
+    if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4><<<s.grid, 256, 0, st>>>(a);
+    if constexpr (D == 128) draft_wide_kernel<F32, D, 1, 8><<<s.grid, 512, 0, st>>>(a);
+  }
 }
 
 DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const DraftShape &s, int d) {
