@@ -713,9 +713,9 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
 // transposed (ds_read_b64_tr_b16).  At 256 rows, per wave and 64 rows of the cache: 64 v_mfma of 16 cycles, 32
 // v_exp of 16 and about 190 other vector instructions of 4; LDS passes 32 KB to each wave.
 // A stage's barrier keeps its waves in step, so that they wait for the matrix unit together and then for the vector
-// unit.  With four waves, two workgroups share a CU and fill each other's gaps (16 sequences of 16000 rows, 8 heads,
-// four waves against eight: 64 rows of Q 203 against 303 us, 96 rows 221 / 367, 256 rows of d = 64 293 / 390, in fp32
-// 568 / 713).  With d = 128 and 256 rows they would read K and V twice; eight waves stay ahead there (61 rows x 4
+// unit.  With four waves, two workgroups (d = 64: three) share a CU and fill each other's gaps (16 sequences of 16000
+// rows, 8 heads, four waves against eight: 64 rows of Q 203 against 303 us, 96 rows 221 / 367, 256 rows of d = 64 232 /
+// 390, in fp32 443 / 713).  With d = 128 and 256 rows they would read K and V twice; eight waves stay ahead there (61 rows x 4
 // heads per group over 128K rows: 195 us, 0.67 of 1.22 PFLOP/s; 208 in two tiles of 128).  64 rows per wave halve the
 // LDS traffic, but O then lives in accumulation registers and is copied at every rescale test: 418 us.
 
@@ -727,7 +727,7 @@ __device__ __forceinline__ int chunk_xor(int r) {
 
 // F32: values are split into their bf16 parts as they enter LDS, a plane each.
 template <bool F32, int D, int KW, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void draft_wide_kernel(const DraftArgs a) {
+__global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(const DraftArgs a) {
   constexpr int NT = KW == 2 || F32 ? 1 : 2;                 // tiles of 32 rows per wave and stage
   constexpr int NQ = 2, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
   constexpr int E = F32 ? 4 : 2, QP = F32 ? 2 : 1;                // bytes of a value; bf16 parts of it
@@ -1565,9 +1565,10 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
   s.trows = tile_rows(f32, d, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
-  // workgroups that the chip holds at once: two per CU of four waves with d = 64, 16 rows of bf16 or stages, else one
+  // workgroups that the chip holds at once: with stages three per CU (d = 64: 16 sequences of 16000 rows, 256 rows of Q,
+  // 232 us, planned for two 295), two (d = 128, four waves) or one; else two with d = 64 or 16 rows of bf16, or one
   const bool two = d == 64 || (!f32 && s.trows == 16), wide = s.trows > 32;
-  const int resident = (wide ? s.trows < 256 : two) ? 512 : 256;
+  const int resident = 256 * (!wide ? 1 + two : d == 64 ? 3 : s.trows < 256 ? 2 : 1);
   if (nsel) {
     const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
     const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
