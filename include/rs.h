@@ -386,7 +386,8 @@ rs_status rs_dense_attn_prefill(const rs_qkv *qkv, const rs_unit *units, int32_t
  *    evicted cache holds fewer rows than that, in an order of its own, each head its own rows.
  * Strides are in elements, 16-byte multiples.  dtype is that of K, V and of the queries; fp32 values
  * enter the products as two bf16 parts each, hi = bf16(x) and lo = bf16(x - hi), without lo.lo
- * (within about 2^-16 of sum_d |q_d k_d| x scale of the exact logit). */
+ * (within about 2^-16 of sum_d |q_d k_d| x scale of the exact logit); beyond 2^96 hi is 2^96, which leaves
+ * 8 bits, and infinities and NaN are lo's: they do what they do in bf16. */
 typedef struct rs_cache {
   void *k, *v;               /* device */
   int32_t dtype, nseq, hkv, d;

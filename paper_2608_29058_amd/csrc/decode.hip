@@ -70,9 +70,14 @@ __device__ __forceinline__ float wave_total(float x) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x as hi + lo, both bf16 (8 + 8 bits of its 24)
+// x as hi + lo, both bf16 (8 + 8 bits of its 24).  hi ends at 2^96, so that it is finite, and what is infinite or
+// undefined lies in lo alone: the products hi.lo and hi.hi beside it stay finite and keep its sign (a lo that
+// subtracts an infinite hi is NaN).  Magnitudes beyond 2^96 have lo's 8 bits.  The clamp is one v_med3 per value: up to
+// 4 % of a call's time, 9 % with 32 rows of Q of d = 128 (427 -> 465 us; testing the scores and
+// trying again, or walking a piece again, spills registers and takes longer).
+constexpr float kSplitMax = 0x1p96f;
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
-  hi = pack_bf16x2(a, b);
+  hi = pack_bf16x2(__builtin_amdgcn_fmed3f(a, -kSplitMax, kSplitMax), __builtin_amdgcn_fmed3f(b, -kSplitMax, kSplitMax));
   lo = pack_bf16x2(a - __builtin_bit_cast(float, hi << 16), b - __builtin_bit_cast(float, hi & 0xffff0000u));
 }
 
@@ -640,7 +645,7 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
   int s = g0 * kGroup + wave * kTile;
   if constexpr (F32 && (D == 128 || NQ > 1)) {
     // two tiles do not fit the registers: the next K is in flight while V is used, and the other way round (16
-    // sequences of 16000 rows, 8 heads of 128: one token 405 us, eight 425, at 5.2 TB/s; with two tiles, part of
+    // sequences of 16000 rows, 8 heads of 128: one token 405 us, eight 465, at 5.2 and 4.5 TB/s; with two tiles, part of
     // them in scratch, 689 and 1507)
     if (s < s_end) {
       T t;
