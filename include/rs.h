@@ -423,8 +423,9 @@ typedef struct rs_draft {
 
 /* Writes new rows into the cache: k_new, v_new (device [nrows][hkv][d], the cache's dtype, element
  * strides (token, head)), row start[b] + i to row len[b] + i of sequence b (rows behind cap are left
- * out).  len stays: the rows are drafts until rs_cache_commit.  max_rows bounds t_b (any size up to
- * cap here).  acc of the written rows, if any, becomes 0. */
+ * out).  len stays: the rows are drafts until rs_cache_commit.  max_rows bounds t_b (any size here, beyond
+ * cap too) and, as in rs_draft, is the number of rows of every sequence where start is NULL.  acc of the
+ * written rows, if any, becomes 0. */
 rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *v_new, int64_t sk_t, int64_t sk_h,
                           int64_t sv_t, int64_t sv_h, const int32_t *start, int32_t nrows, int32_t max_rows,
                           rs_stream stream);

@@ -544,8 +544,9 @@ void by_type(int dtype, int d, F f) {
 
 rs_status append_launch(const CacheView &c, int dtype, int d, const void *kn, const void *vn, int64_t skt, int64_t skh,
                         int64_t svt, int64_t svh, const int32_t *start, int nrows, int max_rows, hipStream_t st) {
-  const int e = dtype == RS_BF16 ? 2 : 4;
-  append_kernel<<<dim3((max_rows + kAppendRows - 1) / kAppendRows, c.nseq), 256, 0, st>>>(
+  // max_rows is also the distance of the sequences' rows without `start`; no sequence takes more than cap of them
+  const int e = dtype == RS_BF16 ? 2 : 4, most = max_rows < c.cap ? max_rows : c.cap;
+  append_kernel<<<dim3((most + kAppendRows - 1) / kAppendRows, c.nseq), 256, 0, st>>>(
       c, (const char *)kn, (const char *)vn, skt * e, skh * e, svt * e, svh * e, start, nrows, max_rows, log2i(d * e / 16));
   RS_HIP(hipGetLastError());
   return RS_OK;

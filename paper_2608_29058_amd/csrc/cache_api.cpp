@@ -121,7 +121,6 @@ rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *
   for (int i = 0; i < 4; ++i)
     if (s[i] < 0 || s[i] % vec != 0) return fail(RS_ERR_INVALID_ARG, "append: strides must be non-negative multiples of 16 bytes");
   if (nrows < 0 || max_rows < 1) return fail(RS_ERR_INVALID_ARG, "append: nrows < 0 or max_rows < 1");
-  if (max_rows > c.cap) max_rows = c.cap;
   if (!start && (int64_t)c.nseq * max_rows > nrows) return fail(RS_ERR_INVALID_ARG, "append: without start every sequence has max_rows rows");
   if (nrows == 0) return RS_OK;
   return append_launch(c, cache->dtype, cache->d, k_new, v_new, sk_t, sk_h, sv_t, sv_h, start, nrows, max_rows, (hipStream_t)stream);
