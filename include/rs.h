@@ -467,7 +467,7 @@ rs_status rs_attn_weights(const rs_cache *cache, const rs_draft *draft, const fl
 
 /* Leaves `budget` rows of every sequence that holds more: per key/value head those with pos < nsink or
  * pos >= seen - nrecent (the lower ones, should there be more), then those of the largest acc (total order of
- * the index construction: score descending, -0.0 after +0.0, row ascending; a NaN may take any place).  The kept
+ * the index construction: score descending, -0.0 after +0.0, row ascending; a NaN may take any place among them).  The kept
  * rows behind the budget move to the places that evicted rows leave before it, the i-th to the i-th, with their
  * acc and pos; all other rows stay where
  * they are.  So a step that evicts one row moves one row, whatever the length.  len becomes budget and

@@ -181,9 +181,11 @@ struct EvictPlan {
 
 constexpr int kPlanThreads = 1024;
 
-// Key of a row in the order of the selection: firm rows share the highest, which no finite weight has.
+// Key of a row in the order of the selection: firm rows share the highest, which no other row has (a NaN with all
+// bits set would).
 __device__ __forceinline__ uint32_t evict_key(float a, int pos, int nsink, int firm_from) {
-  return pos < nsink || pos >= firm_from ? 0xffffffffu : float_key(a);
+  const uint32_t k = float_key(a);
+  return pos < nsink || pos >= firm_from ? 0xffffffffu : k < 0xfffffffeu ? k : 0xfffffffeu;
 }
 
 // The bin in which the count from the highest key down reaches `need`: pick = {bin, rows of it that still
