@@ -602,8 +602,12 @@ def _check_rows_out(cache, draft, o, lse):
     _want(_like(lse, torch.float32, (draft.hq, draft.nrows), cache.device), "lse must be contiguous float32 [hq, nrows]")
 
 
-def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+def _ws(ws, cache):
+    """Address and bytes of a workspace (or None)."""
+    if ws is None:
+        return None, 0
+    _want(ws.is_contiguous() and ws.device == cache.device, "the workspace must be a contiguous tensor on the device of the cache")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _at(t):
@@ -638,7 +642,7 @@ def rs_draft_attn(cache, draft, o, lse, ws, stream=None):
     """o: bf16 [nrows, hq, d]; lse: float32 [hq, nrows] or None."""
     _check_rows_out(cache, draft, o, lse)
     return _on_device(lib().rs_draft_attn, cache.device, stream,
-                      (cache.ref, draft.ref, o.data_ptr(), o.stride(0), o.stride(1), _at(lse), *_ws(ws)))
+                      (cache.ref, draft.ref, o.data_ptr(), o.stride(0), o.stride(1), _at(lse), *_ws(ws, cache)))
 
 
 def rs_select_attn_workspace_size(cache, draft, nsel):
@@ -652,7 +656,7 @@ def rs_select_attn(cache, draft, nsel, nsink, nlocal, o, lse, ws, blocks=None, s
     _want(_like(blocks, torch.int32, (draft.nrows, cache.hkv, nsel), cache.device), "blocks must be contiguous int32 [nrows, hkv, nsel]")
     return _on_device(lib().rs_select_attn, cache.device, stream,
                       (cache.ref, draft.ref, nsel, nsink, nlocal, o.data_ptr(), o.stride(0), o.stride(1), _at(lse),
-                       _at(blocks), *_ws(ws)))
+                       _at(blocks), *_ws(ws, cache)))
 
 
 def rs_attn_weights(cache, draft, lse, acc_in, acc_out, row_w=None, stream=None):
@@ -673,4 +677,4 @@ def rs_cache_evict_workspace_size(cache, budget):
 
 
 def rs_cache_evict(cache, budget, nsink, nrecent, ws, stream=None):
-    return _on_device(lib().rs_cache_evict, cache.device, stream, (cache.ref, budget, nsink, nrecent, *_ws(ws)))
+    return _on_device(lib().rs_cache_evict, cache.device, stream, (cache.ref, budget, nsink, nrecent, *_ws(ws, cache)))
