@@ -735,6 +735,7 @@ template <bool F32, int D, int KW, int NW>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(const DraftArgs a) {
   constexpr int NT = KW == 2 || F32 ? 1 : 2;                 // tiles of 32 rows per wave and stage
   constexpr int NQ = 2, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
+  static_assert(64 % SR == 0, "a stage lies in one page");
   constexpr int E = F32 ? 4 : 2, QP = F32 ? 2 : 1;                // bytes of a value; bf16 parts of it
   constexpr int KC = D / 32, DT = D / 16, CPR = D * E / 16, RPI = 64 / CPR;
   constexpr int NI = 2 * SR / RPI / NW;  // 16-byte loads per lane and stage, K before V
@@ -783,61 +784,43 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   }
   const bool idle = r0 + 32 * wr >= nr;  // a wave without rows only carries its part of the stages
 
-  // Load i of a stage: RPI rows of K or V.  64 rows of a stage lie in one page; the table's entries are read a
-  // stage ahead of their use.
-  constexpr int NP = SR > 64 ? SR / 64 : 1;
+  // Load i of a stage: RPI rows of K or V.  The table's entry is read a stage ahead of its use.
   const int lr = lane / CPR, lc = lane % CPR;
   u32x4 st[NI];
-  bool okst[NP];
-  int entry[NP];
+  bool okst;
+  int entry;
+  auto first_row = [&](int stage) {  // (behind the end: the last row)
+    const int j = j0 + stage * SR;
+    return __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
+  };
   auto look = [&](int stage) {
-#pragma unroll
-    for (int x = 0; x < NP; ++x) {
-      int j = j0 + stage * SR + 64 * x;
-      j = __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
-      const int p = page_of(c, j);
-      entry[x] = c.table ? uload(c.table, (int64_t)it.b * c.max_pages + p) : it.b * c.max_pages + p;
-    }
+    const int p = page_of(c, first_row(stage));
+    entry = c.table ? uload(c.table, (int64_t)it.b * c.max_pages + p) : it.b * c.max_pages + p;
   };
   int off[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI);
-    off[i] = (w * RPI % 64 + lr) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc;
+    off[i] = (w * RPI + lr) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc;
   }
   const char *kg = c.k + it.g * c.sk_h, *vg = c.v + it.g * c.sv_h;
-  // (x[y] with y known to the wave only would put x into memory)
-  static_assert(NP <= 2, "pages of a stage");
-  auto of = [](const auto &x, int y) { return NP == 2 && y ? x[NP - 1] : x[0]; };
-  auto fetch = [&](int stage, u32x4 (&x)[NI], bool (&ok)[NP]) {
-    const int js = j0 + stage * SR;
-    bool whole = js + SR <= total;
-    const char *kb[NP], *vb[NP];
-    int left[NP];  // last row that may be read
-#pragma unroll
-    for (int y = 0; y < NP; ++y) {
-      int j = js + 64 * y;
-      j = __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
-      const int id = checked_page(c, entry[y]), in = j - page_of(c, j) * c.page;
-      ok[y] = id >= 0;
-      kb[y] = kg + (ok[y] ? id * c.sk_p + in * c.sk_t : 0);
-      vb[y] = vg + (ok[y] ? id * c.sv_p + in * c.sv_t : 0);
-      left[y] = ok[y] ? total - 1 - j : 0;
-      whole = whole && ok[y];
-    }
+  auto fetch = [&](int stage, u32x4 (&x)[NI], bool &ok) {
+    const int j = first_row(stage), id = checked_page(c, entry), in = j - page_of(c, j) * c.page;
+    ok = id >= 0;
+    const char *kb = kg + (ok ? id * c.sk_p + in * c.sk_t : 0), *vb = vg + (ok ? id * c.sv_p + in * c.sv_t : 0);
+    const int most = ok ? total - 1 - j : 0;  // last row that may be read
     look(stage + 1);
-    if (whole) {
+    if (most >= SR - 1) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64;
-        x[i] = *(const u32x4 *)((isv ? of(vb, y) : of(kb, y)) + off[i]);
+        const int isv = (i * NW + wave) / (SR / RPI);
+        x[i] = *(const u32x4 *)((isv ? vb : kb) + off[i]);
       }
     } else {  // rows behind the end are read as the last, all without a page as its row 0
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), y = w * RPI / 64, r = w * RPI % 64 + lr;
-        const int most = of(left, y);
-        x[i] = *(const u32x4 *)((isv ? of(vb, y) : of(kb, y)) + (r < most ? r : most) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc);
+        const int w = (i * NW + wave) % (SR / RPI), isv = (i * NW + wave) / (SR / RPI), r = w * RPI + lr;
+        x[i] = *(const u32x4 *)((isv ? vb : kb) + (r < most ? r : most) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc);
       }
     }
   };
@@ -928,15 +911,12 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
 
   // stages of cached rows alone, which every row sees (and none what has no page)
   const int nplain = len < j1 ? (len > j0 ? (len - j0) / SR : 0) : (j1 - j0) / SR, wr0 = wk * NT * 32;
-  const int page_of_wave = wr0 / 64 < NP ? wr0 / 64 : 0;
   look(0);
   fetch(0, st, okst);
   for (int s = 0; s < nplain; ++s) {
     char *buf = lds + (s & 1) * kBuf;
     put(std::false_type{}, buf, st);
-    bool ok = okst[0];
-#pragma unroll
-    for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
+    const bool ok = okst;
     fetch(s + 1, st, okst);  // (behind the last: its last row)
     stage_barrier();
     if (idle || !ok) continue;
@@ -957,9 +937,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   for (int s = nplain; s < nst; ++s) {
     __syncthreads();
     put(std::true_type{}, lds, st);
-    bool ok = okst[0];
-#pragma unroll
-    for (int y = 1; y < NP; ++y) ok = page_of_wave == y ? okst[y] : ok;
+    const bool ok = okst;
     fetch(s + 1, st, okst);
     stage_barrier();
     if (idle || !ok) continue;
