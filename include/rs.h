@@ -439,7 +439,8 @@ rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const i
 /* Attention of the drafted rows over the cache: O (bf16 [nrows][hq][d], element strides so_t, so_h)
  * and, if lse != NULL, lse[head * nrows + row] = log of the sum of the exp of its logits (-inf, and O = 0,
  * for a row that sees nothing).  Long sequences are split over workgroups and joined; the workspace
- * holds the pieces. */
+ * holds the pieces.  A launch has fewer than 2^23 workgroups: nseq x hkv x tiles of 16 to 256 of the
+ * hq / hkv x max_rows rows of a head. */
 size_t rs_draft_attn_workspace_size(const rs_cache *cache, const rs_draft *draft);
 rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, int64_t so_t, int64_t so_h, float *lse,
                         void *ws, size_t ws_bytes, rs_stream stream);

@@ -1613,8 +1613,10 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   a.slots = s.slots;
   a.least = s.least;
   a.pieces = s.pieces;
-  a.po = ar.take<float>((size_t)s.grid * s.trows * d);
-  a.pml = ar.take<float>((size_t)s.grid * s.trows * 2);
+  // (a single piece is the result itself; its call asks for one line all the same, so that no caller does without one)
+  const size_t rows = s.slots > 0 || s.pieces > 1 ? (size_t)s.grid * s.trows : 0;
+  a.po = ar.take<float>(rows ? rows * d : 64);
+  a.pml = ar.take<float>(rows * 2);
   return a;
 }
 
@@ -1671,6 +1673,7 @@ size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, i
 rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
                        void *ws, size_t ws_bytes, hipStream_t st) {
   const DraftShape s = draft_shape(c, q, f32, d, 0);
+  if (s.grid >= 1 << 23) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^23 - 1 workgroups (nseq x hkv x row tiles)");  // of up to 512 threads
   Arena ar(ws, ws_bytes);
   DraftArgs a = draft_parts(ar, c, q, s, d);
   if (!ws || !ar.ok())

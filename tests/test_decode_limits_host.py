@@ -2,7 +2,7 @@
 import ctypes as C
 
 from paper_2608_29058_amd import _rs
-from test_decode_host import INV, cache
+from test_decode_host import INV, UNS, attend, cache, draft
 
 
 def test_new_rows_without_starts_are_max_rows_apart_beyond_the_capacity_too():
@@ -31,3 +31,24 @@ def test_workspaces_elsewhere_or_with_gaps_are_refused():
                   lambda: _rs.rs_cache_evict(c, 8, 0, 0, ws)):
             with pytest.raises(ValueError, match="workspace"):
                 f()
+
+
+def test_workspaces_hold_pieces_only_where_there_are_several():
+    """Caches of one piece, and selections whose rows fill the chip, write their results themselves."""
+    L = _rs.lib()
+    size = lambda c, d, nsel=None: (L.rs_draft_attn_workspace_size(C.byref(c), C.byref(d)) if nsel is None
+                                    else L.rs_select_attn_workspace_size(C.byref(c), C.byref(d), nsel))
+    many = dict(nseq=500, npages=5000)
+    assert 256 <= size(cache(**many), draft(nrows=500 * 64, max_rows=64)) <= 4096          # 256 rows per sequence
+    assert size(cache(**many, max_pages=40), draft(nrows=500 * 64, max_rows=64)) > 500 * 2 * 256 * 128 * 4
+    c, d, nsel = cache(**many, max_pages=400, page=64), draft(nrows=500), 10
+    blocks, scores = 500 * 2 * nsel * 4, 500 * 2 * 400 * 8
+    assert blocks + scores <= size(c, d, nsel) <= blocks + scores + 4096                    # 1000 items
+    few = draft(nrows=3)
+    assert size(c, few, nsel) > 3 * 2 * (nsel * 4 + 400 * 8) + 6 * 2 * 16 * 130 * 4
+
+
+def test_more_workgroups_than_a_launch_has_are_refused():
+    c = cache(nseq=65535, hkv=256, npages=1 << 18)
+    d = draft(hq=256, nrows=65535)
+    assert attend(c, d, nbytes=1 << 40) == UNS
