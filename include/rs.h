@@ -380,7 +380,7 @@ rs_status rs_dense_attn_prefill(const rs_qkv *qkv, const rs_unit *units, int32_t
  *  - A table entry outside [0, npages) names no page: rows there are not written, and no query sees
  *    them.
  *  - kmean (optional): bf16 [npages][hkv][ceil(page / 64)][d], the mean of the K rows of each complete
- *    block of 64 rows (sum in fp64, rounded once).  rs_cache_commit and rs_cache_evict keep it.
+ *    block of 64 rows (sum in fp64, rounded to fp32 and that to bf16).  rs_cache_commit and rs_cache_evict keep it.
  *  - acc, pos (optional): [nseq][hkv][cap], the accumulated attention weight and the position in the
  *    sequence of every row; seen (optional, device [nseq]): tokens that a sequence has had.  An
  *    evicted cache holds fewer rows than that, in an order of its own, each head its own rows.

@@ -37,8 +37,10 @@ __global__ __launch_bounds__(256) void append_kernel(CacheView c, const char *kn
 
 // ---- block means ---------------------------------------------------------------------------
 // Mean of the 64 K rows of block blk, by one wave: lane l sums rows l / (D / 8), ... of its 8 dimensions in
-// fp64 (bf16 sums of 64 rows are exact there, so no order shows), the lanes of equal dimensions add up, and
-// the mean is rounded to bf16 once: it is a score's factor, and 8 bits of it rank blocks as well as 24.
+// fp64, then the lanes of equal dimensions add up (in one order; exact while values lie within 2^39 of each other in
+// bf16, 53 bits less 8 and 6 of carry, or 2^23 in fp32).  The mean is rounded to fp32 and that to bf16, so what lies
+// within 2^-25 of the middle of two bf16 values counts as the middle: it is a score's factor, and 8 bits of it rank
+// blocks as well as 24.
 template <typename T, int D>
 __device__ void block_mean(const CacheView &c, int b, int g, int blk, int lane) {
   constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes per row, rows per step
