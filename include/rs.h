@@ -459,10 +459,13 @@ rs_status rs_select_attn(const rs_cache *cache, const rs_draft *draft, int32_t n
 
 /* Attention weight that the drafted rows put on each cached row, summed over the rows and the query
  * heads of each key/value head:
- *   acc_out[b][g][j] = acc_in[b][g][j] + sum over rows i and heads h of g of row_w[i] exp(l_hij - lse_hi)
- * for j < len[b] + t_b that row i sees; other entries are left as they are.  lse: as rs_draft_attn
- * wrote it; row_w (device [nrows], NULL: 1): 0 for drafts that were not accepted; acc_in (NULL: 0) may
- * be acc_out.  Both are [nseq][hkv][cap] as rs_cache.acc. */
+ *   acc_out[b][g][j] = acc_in[b][g][j] + sum over the rows i that see j and the heads h of g of
+ *                      row_w[i] exp(l_hij - lse_hi)
+ * for the rows j < len[b] + t_b, seen or not, of every sequence with new rows (t_b > 0).  Other entries of
+ * acc_out are left as they are, also where acc_in is another buffer: those behind a sequence, in no page, and of
+ * sequences without new rows.  lse: as rs_draft_attn wrote it; row_w (device [nrows], NULL: 1): 0 for
+ * drafts that were not accepted; acc_in (NULL: 0) may be acc_out.  Both are [nseq][hkv][cap] as
+ * rs_cache.acc. */
 rs_status rs_attn_weights(const rs_cache *cache, const rs_draft *draft, const float *lse, const float *row_w,
                           const float *acc_in, float *acc_out, rs_stream stream);
 
