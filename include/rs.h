@@ -374,7 +374,7 @@ rs_status rs_dense_attn_prefill(const rs_qkv *qkv, const rs_unit *units, int32_t
  * A prefill writes the same rows: with head-major pages a prompt's K and V of rs_qkv are pages.
  *  - One sequence holds at most cap = max_pages * page rows, cap <= 262144.  page is a multiple
  *    of 64, or any size where max_pages == 1.  Sequences may share pages that are only read; rows that a
- *    call writes lie in pages of one sequence.
+ *    call writes lie in pages of one sequence, whose table names them once.
  *  - len (device) counts the rows held; it is read clamped to [0, cap].  Rows behind it are neither
  *    read nor, but by rs_cache_append, written.
  *  - A table entry outside [0, npages) names no page: rows there are not written, and no query sees
@@ -438,9 +438,10 @@ rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const i
 
 /* Attention of the drafted rows over the cache: O (bf16 [nrows][hq][d], element strides so_t, so_h)
  * and, if lse != NULL, lse[head * nrows + row] = log of the sum of the exp of its logits (-inf, and O = 0,
- * for a row that sees nothing).  Long sequences are split over workgroups and joined; the workspace
- * holds the pieces.  A launch has fewer than 2^23 workgroups: nseq x hkv x tiles of 16 to 256 of the
- * hq / hkv x max_rows rows of a head. */
+ * for a row that sees nothing).  Sums and maxima are fp32, the weights p that multiply V bf16, for caches of
+ * either type (within 2^-8 of sum p |v|; O itself is rounded to bf16).  Long sequences are split over
+ * workgroups and joined; the workspace holds the pieces.  A launch has fewer than 2^23 workgroups: nseq x hkv x
+ * tiles of 16 to 256 of the hq / hkv x max_rows rows of a head. */
 size_t rs_draft_attn_workspace_size(const rs_cache *cache, const rs_draft *draft);
 rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, int64_t so_t, int64_t so_h, float *lse,
                         void *ws, size_t ws_bytes, rs_stream stream);
@@ -449,7 +450,8 @@ rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, i
  * key/value head reads min(nsel, F): the first nsink, the last nlocal (nsink + nlocal <= nsel), and
  * those of the largest score
  *   score(c) = max over the head's query heads of q . kmean_c
- * (exact: products of bf16 means and q are summed in fp64; equal scores, the lower block first; NaN
+ * (products of bf16 means and q summed in fp64, in one order: exact while a sum's terms lie within 2^30 of each
+ * other for bf16 q, 2^14 for fp32 q, else rounded to 53 bits; equal scores, the lower block first; NaN
  * counts as minus infinity), and always the rows behind the last complete block.  blocks (optional,
  * device int32 [nrows][hkv][nsel]): the selected blocks ascending, -1 behind them.  1 <= nsel <= 4096. */
 size_t rs_select_attn_workspace_size(const rs_cache *cache, const rs_draft *draft, int32_t nsel);

@@ -284,8 +284,9 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[2 * NT][NQ], float c, flo
         p[e] = exp2_fast(__builtin_fmaf(s[2 * i + (e >> 2)][n][e & 3], c, -base));
         sum[n] += p[e];
       }
-      // P is rounded to bf16 for the product, as in the prefill kernels (half a step of each weight, 2^-8 of
-      // sum p |v| at most); its sum is taken before
+      // P is rounded to bf16 for the product, as in the prefill kernels and for fp32 caches too (half a step of each
+      // weight, 2^-8 of sum p |v| at most, as much as the result's own rounding; a second part would be a third more
+      // products with V in fp32, twice as many in bf16); its sum is taken before
 #pragma unroll
       for (int w = 0; w < 4; ++w) pb[i][n][w] = pack_bf16x2(p[2 * w], p[2 * w + 1]);
     }
@@ -1103,9 +1104,10 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
 }
 
 // ---- scores and selection of blocks ------------------------------------------------------------
-// score(c) = max over the heads h of g of q_h . mean_c, in fp64: products of bf16 means and bf16 (or fp32) q
-// are exact, and so are the sums as long as their terms lie within 2^37 of each other, so that the
-// selection does not depend on the order of a sum.  The products are v_mfma_f64_16x16x4: 16 rows of a
+// score(c) = max over the heads h of g of q_h . mean_c, in fp64.  A product has 16 bits with bf16 q and 32 with fp32 q, a
+// sum of 128 of them 7 more: of fp64's 53 that leaves 30 and 14, so sums of terms that lie within 2^30 (2^14) of each
+// other are exact and the selection does not depend on their order; others are rounded to 53 bits in the order
+// of the instructions, which is always the same.  The products are v_mfma_f64_16x16x4: 16 rows of a
 // sequence (tokens and heads) against 16 blocks per wave, both operands straight from memory (a lane holds a
 // quarter of a row: the contraction may run in any order), the means converted once for all rows.  The
 // vector ALU has the same fp64 rate without padding rows to 16, but its q operands come through LDS: 80 rows x 8
