@@ -73,8 +73,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // x as hi + lo, both bf16 (8 + 8 bits of its 24).  hi ends at 2^96, so that it is finite, and what is infinite or
 // undefined lies in lo alone: the products hi.lo and hi.hi beside it stay finite and keep its sign (a lo that
 // subtracts an infinite hi is NaN).  Magnitudes beyond 2^96 have lo's 8 bits.  The clamp is one v_med3 per value: up to
-// 4 % of a call's time, 9 % with 32 rows of Q of d = 128 (427 -> 465 us; testing the scores and
-// trying again, or walking a piece again, spills registers and takes longer).
+// 6 % of a call's time, 10 % with 17 to 32 rows of Q of d = 128 (16 sequences of 16000 rows, 8 heads: 452 -> 495 us; testing
+// the scores and trying again, or walking a piece again, spills registers and takes as long).
 constexpr float kSplitMax = 0x1p96f;
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
   hi = pack_bf16x2(__builtin_amdgcn_fmed3f(a, -kSplitMax, kSplitMax), __builtin_amdgcn_fmed3f(b, -kSplitMax, kSplitMax));
@@ -646,7 +646,7 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
   int s = g0 * kGroup + wave * kTile;
   if constexpr (F32 && (D == 128 || NQ > 1)) {
     // two tiles do not fit the registers: the next K is in flight while V is used, and the other way round (16
-    // sequences of 16000 rows, 8 heads of 128: one token 405 us, eight 465, at 5.2 and 4.5 TB/s; with two tiles, part of
+    // sequences of 16000 rows, 8 heads of 128: one token 410 us, eight 495, at 5.1 and 4.2 TB/s; with two tiles, part of
     // them in scratch, 689 and 1507)
     if (s < s_end) {
       T t;
@@ -720,10 +720,10 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
 // v_exp of 16 and about 190 other vector instructions of 4; LDS passes 32 KB to each wave.
 // A stage's barrier keeps its waves in step, so that they wait for the matrix unit together and then for the vector
 // unit.  With four waves, two workgroups (d = 64: three) share a CU and fill each other's gaps (16 sequences of 16000
-// rows, 8 heads, four waves against eight: 64 rows of Q 203 against 303 us, 96 rows 221 / 367, 256 rows of d = 64 232 /
-// 390, in fp32 443 / 713).  With d = 128 and 256 rows they would read K and V twice; eight waves stay ahead there (61 rows x 4
-// heads per group over 128K rows: 195 us, 0.67 of 1.22 PFLOP/s; 208 in two tiles of 128).  64 rows per wave halve the
-// LDS traffic, but O then lives in accumulation registers and is copied at every rescale test: 418 us.
+// rows, 8 heads: 64 rows of Q 205 us, 0.67 of what eight waves take; 96 rows 227, 0.60; 256 rows of d = 64 233, 0.59, in
+// fp32 461, 0.62).  With d = 128 and 256 rows they would read K and V twice; eight waves stay ahead there (61 rows x 4
+// heads per group over 128K rows: 188 us, 0.70 of 1.22 PFLOP/s; 1.07 times that in two tiles of 128).  64 rows per wave
+// halve the LDS traffic, but O then lives in accumulation registers and is copied at every rescale test: 2.1 times.
 
 // Chunks of K: 16 rows' equal chunks in different banks; of V: the chunk pairs 2t, 2t + 1 of 8 rows.
 template <int D>
@@ -922,7 +922,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
     stage_barrier();
     if (idle || !ok) continue;
     f32x4 sc[2 * NT][NQ];
-    __builtin_amdgcn_s_setprio(1);  // matrix instructions first: the other wave's exponents fill their gaps (206 -> 198 us)
+    __builtin_amdgcn_s_setprio(1);  // matrix instructions first: the other wave's exponents fill their gaps (4 % less)
     u32x4 pb[NT][NQ];
 #pragma unroll
     for (int u = 0; u < 2 * NT; ++u) scores(buf, wr0 + 16 * u, sc[u]);
@@ -1318,8 +1318,8 @@ struct WeightArgs {
 
 // NQ: 16-row tiles of Q kept in registers; 0: more rows than that, 128 at a time in LDS (in the order and parts in
 // which the instructions take them), and K once for each of these.  16 sequences of 16000 rows, 8 heads of 128: 64
-// rows of Q 125 us in bf16 (158 with Q read from memory for every 64 cached rows, 181 from registers) and 214 in
-// fp32 (535; floor 205); 256 rows 290 and 519.
+// rows of Q 129 us in bf16 (158 with Q read from memory for every 64 cached rows, 181 from registers) and 217 in
+// fp32 (535; floor 206); 256 rows 291 and 533.
 template <bool F32, int D, int NQ>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
   constexpr int KC = D / 32, E = F32 ? 4 : 2, QP = F32 ? 2 : 1, NK = NQ ? NQ : 1;
@@ -1479,7 +1479,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
     fetch(j, k, ok);
     if constexpr (F32 && NQ > 1) {
       // two steps do not fit the registers: 16 rows at a time become bf16 parts and make room for the next step's
-      // (16 sequences of 16000 rows, 8 heads of 128, 32 rows of Q: 198 us; 378 with Q read again for every 16 rows)
+      // (16 sequences of 16000 rows, 8 heads of 128, 32 rows of Q: 209 us; 378 with Q read again for every 16 rows)
       while (true) {
         const int jn = j + 4 * RW;
         float sum[NU] = {};
@@ -1529,7 +1529,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightArgs a) {
 // ---- launches --------------------------------------------------------------------------------------
 // Rows of an item: up to 32 are held by every wave (16 or 32); more of them share stages, in tiles of 64 or 128 rows (four
 // waves, two workgroups per CU; fp32 and d = 64 only gain from 128), or of 256 where that pads less: up to 192 rows
-// of d = 128 take three tiles of 64 (16 x 16000 rows, 132 rows of Q: 373 us, 520 in one tile of 256), an odd number of
+// of d = 128 take three tiles of 64 (16 x 16000 rows, 132 rows of Q: 370 us, 520 in one tile of 256), an odd number of
 // 128s those (44 sequences of 1 to 1599 rows, 264 rows of Q: 88 us, 133 in two of 256).  Selections belong to one
 // token, whose heads rarely are that many: row tiles of 32.
 int tile_rows(bool f32, int d, bool sel, int rows) {
@@ -1551,7 +1551,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   s.trows = tile_rows(f32, d, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
   // workgroups that the chip holds at once: with stages three per CU (d = 64: 16 sequences of 16000 rows, 256 rows of Q,
-  // 232 us, planned for two 295), two (d = 128, four waves) or one; else two with d = 64 or 16 rows of bf16, or one
+  // 233 us, planned for two 295), two (d = 128, four waves) or one; else two with d = 64 or 16 rows of bf16, or one
   const bool two = d == 64 || (!f32 && s.trows == 16), wide = s.trows > 32;
   const int resident = 256 * (!wide ? 1 + two : d == 64 ? 3 : s.trows < 256 ? 2 : 1);
   if (nsel) {
