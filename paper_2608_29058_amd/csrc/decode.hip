@@ -1543,6 +1543,7 @@ struct DraftShape {
 };
 
 constexpr int kShort = 256;
+constexpr int kMaxGrid = 1 << 23;  // workgroups of up to 512 threads, of which a launch has fewer than 2^32
 
 DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
   DraftShape s{};
@@ -1667,15 +1668,17 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
 
 size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
   Arena ar(nullptr, 0);
+  const DraftShape s = draft_shape(c, q, f32, d, nsel);
+  if (!nsel && s.grid >= kMaxGrid) return 0;
   if (nsel) select_parts(ar, c, q, nsel);
-  draft_parts(ar, c, q, draft_shape(c, q, f32, d, nsel), d);
+  draft_parts(ar, c, q, s, d);
   return ar.off + 256;
 }
 
 rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
                        void *ws, size_t ws_bytes, hipStream_t st) {
   const DraftShape s = draft_shape(c, q, f32, d, 0);
-  if (s.grid >= 1 << 23) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^23 - 1 workgroups (nseq x hkv x row tiles)");  // of up to 512 threads
+  if (s.grid >= kMaxGrid) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^23 - 1 workgroups (nseq x hkv x row tiles)");
   Arena ar(ws, ws_bytes);
   DraftArgs a = draft_parts(ar, c, q, s, d);
   if (!ws || !ar.ok())

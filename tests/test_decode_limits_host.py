@@ -52,3 +52,6 @@ def test_more_workgroups_than_a_launch_has_are_refused():
     c = cache(nseq=65535, hkv=256, npages=1 << 18)
     d = draft(hq=256, nrows=65535)
     assert attend(c, d, nbytes=1 << 40) == UNS
+    assert _rs.lib().rs_draft_attn_workspace_size(C.byref(c), C.byref(d)) == 0
+    fits = draft(hq=256, nrows=32767)              # a launch of 2^23 - 256
+    assert _rs.lib().rs_draft_attn_workspace_size(C.byref(cache(nseq=32767, hkv=256, npages=1 << 17)), C.byref(fits)) > 0
