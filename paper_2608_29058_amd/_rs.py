@@ -542,6 +542,7 @@ class KvCache:
         npages, hkv, page, d = k.shape
         nseq = length.numel()
         _want(nseq > 0 and (table is not None or npages % nseq == 0), "without a table every sequence has the same number of pages")
+        _want(table is None or table.dim() == 2, "table must be [nseq, max_pages]")
         max_pages = table.shape[1] if table is not None else npages // nseq
         cap = max_pages * page
         i32 = torch.int32

@@ -55,3 +55,12 @@ def test_more_workgroups_than_a_launch_has_are_refused():
     assert _rs.lib().rs_draft_attn_workspace_size(C.byref(c), C.byref(d)) == 0
     fits = draft(hq=256, nrows=32767)              # a launch of 2^23 - 256
     assert _rs.lib().rs_draft_attn_workspace_size(C.byref(cache(nseq=32767, hkv=256, npages=1 << 17)), C.byref(fits)) > 0
+
+
+def test_tables_of_other_than_two_dimensions_are_refused():
+    import pytest
+    import torch
+    k, n = torch.zeros(4, 2, 64, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    for table in (torch.zeros(4, dtype=torch.int32), torch.zeros((), dtype=torch.int32), torch.zeros(2, 2, 1, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="table"):
+            _rs.KvCache(k, k, n, table=table)
