@@ -436,6 +436,69 @@ rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *
 rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const int32_t *path, int32_t max_new,
                           rs_stream stream);
 
+/* ---- rotary positions ----------------------------------------------------------------------
+ * Pair i < dim / 2 of a head's first dim elements, (x_i, x_{i + dim / 2}) in the half layout and (x_2i, x_{2i + 1}) in
+ * the interleaved one, turns by the angle a = position x f_i:
+ *   y_1 = mscale (x_1 cos a - x_2 sin a),  y_2 = mscale (x_2 cos a + x_1 sin a);
+ * elements from dim on stay as they are.  The angle is the product of the position and the pair's turns per position
+ * in fp64, less its whole turns; cosines, sines, products and sums are fp32 and y is rounded once, to its type.
+ * rs_rope is a host struct that calls read by value.  rs_rope_init (host only, pure) fills it: with
+ * g_i = base^(-2i / dim),
+ *   RS_ROPE_PLAIN   f_i = g_i;
+ *   RS_ROPE_LINEAR  f_i = g_i / factor;
+ *   RS_ROPE_TURNS   f_i = g_i (w_i + (1 - w_i) / factor), w_i = clamp((context g_i / 2 pi - low) / (high - low), 0, 1): pairs
+ *                   of more than `high` turns in the context keep their frequency, those of less than `low` are divided;
+ *   RS_ROPE_PAIRS   the same with a ramp over the pairs: w_i = 1 - clamp((i - a) / (b - a), 0, 1), where a = floor(p(high)),
+ *                   at least 0, b = ceil(p(low)), at most dim - 1, b - a at least 0.001, and p(r) = (dim / 2)
+ *                   ln(context / (2 pi r)) / ln(base) is the pair of r turns.
+ * Frequencies of another rule go into turns (f_i / 2 pi) directly. */
+typedef enum { RS_ROPE_HALF = 0, RS_ROPE_INTERLEAVED = 1 } rs_rope_layout;
+typedef enum { RS_ROPE_PLAIN = 0, RS_ROPE_LINEAR = 1, RS_ROPE_TURNS = 2, RS_ROPE_PAIRS = 3 } rs_rope_scaling;
+typedef struct rs_rope_cfg {
+  int32_t dim;               /* rotated elements of a head: even, 2 .. 128 */
+  int32_t layout, scaling;   /* rs_rope_layout, rs_rope_scaling */
+  int32_t _pad0;
+  double base;               /* > 1 */
+  double factor;             /* >= 1; unused by RS_ROPE_PLAIN */
+  double context, low, high; /* > 0, 0 < low < high: RS_ROPE_TURNS and RS_ROPE_PAIRS */
+  double mscale;             /* 0 => 1 */
+} rs_rope_cfg;
+typedef struct rs_rope {
+  int32_t dim, layout;
+  float mscale;              /* finite */
+  int32_t _pad0;
+  double turns[64];          /* turns per position of each pair, finite */
+} rs_rope;
+rs_status rs_rope_init(const rs_rope_cfg *cfg, rs_rope *rope);
+
+/* Rows [n][heads][d] with element strides (token, head) and a contiguous last dimension, all 16-byte multiples: x is
+ * read, y written.  y may be x (with the same strides); they overlap in no other way. */
+typedef struct rs_rope_part {
+  const void *x;             /* device */
+  void *y;                   /* device */
+  int32_t heads, _pad0;
+  int64_t sx_t, sx_h, sy_t, sy_h;
+} rs_rope_part;
+/* Rows that are rotated by the same positions in one launch: row r of each part by pos[r], or by pos0 + r. */
+typedef struct rs_rope_rows {
+  int32_t dtype, n, d, nparts;  /* rs_dtype; rows, at most 2^24; 64 or 128; 1 .. 4 */
+  const int32_t *pos;        /* device [n], or NULL */
+  int64_t pos0;              /* |pos0| <= 2^31 */
+  rs_rope_part part[4];
+} rs_rope_rows;
+/* Rotates them; with `transpose` by the transposed matrices, mscale times the turn by -a, which takes a gradient of y
+ * to that of x (and, where mscale is 1, y back to x).  fp32 rows stay fp32. */
+rs_status rs_rope_apply(const rs_rope *rope, const rs_rope_rows *rows, int32_t transpose, rs_stream stream);
+
+/* rs_cache_append with the new rows' keys rotated on the way and, with `q`, their queries too: q->x is [nrows][hq][d] in the
+ * cache's dtype, row r the query of the new row r, and q->y (which may be q->x) is what rs_draft_attn then reads.  Row
+ * start[b] + i has the position pos[start[b] + i] (a tree's depths, say), or without pos seen[b] + i, or without that
+ * len[b] + i.  V enters as it is.  Queries of rows behind cap or in no page are rotated all the same; those of rows of no
+ * sequence are neither read nor written. */
+rs_status rs_cache_append_rope(const rs_cache *cache, const rs_rope *rope, const void *k_new, const void *v_new,
+                               int64_t sk_t, int64_t sk_h, int64_t sv_t, int64_t sv_h, const rs_rope_part *q,
+                               const int32_t *pos, const int32_t *start, int32_t nrows, int32_t max_rows, rs_stream stream);
+
 /* Attention of the drafted rows over the cache: O (bf16 [nrows][hq][d], element strides so_t, so_h)
  * and, if lse != NULL, lse[head * nrows + row] = log of the sum of the exp of its logits (-inf, and O = 0,
  * for a row that sees nothing).  Sums and maxima are fp32, the weights p that multiply V bf16, for caches of
@@ -482,6 +545,28 @@ rs_status rs_attn_weights(const rs_cache *cache, const rs_draft *draft, const fl
 size_t rs_cache_evict_workspace_size(const rs_cache *cache, int32_t budget);
 rs_status rs_cache_evict(const rs_cache *cache, int32_t budget, int32_t nsink, int32_t nrecent, void *ws,
                          size_t ws_bytes, rs_stream stream);
+
+/* ---- cross attention -------------------------------------------------------------------------
+ * A decoder's rows over states of another sequence and length: the cache holds the keys and values of an encoder's (or
+ * another model's) states, written once, and every row of sequence b sees all of its len[b] rows, whatever their order, but
+ * those that the key mask hides (padding inside a sequence).  Any number of rows per sequence: a prompt, or one token. */
+typedef struct rs_cross {
+  const void *q;             /* device [nrows][hq][d] of the cache's dtype, element strides (sq_t, sq_h) */
+  int32_t hq, nrows, max_rows, nwords;  /* max_rows bounds a sequence's rows; nseq x hq x max_rows <= 2^28, nrows <= 2^20,
+                                nrows x hkv <= 2^24; nwords: words per sequence of the key mask, 32 nwords >= cap */
+  int64_t sq_t, sq_h;
+  const int32_t *start;      /* device [nseq + 1] as in rs_draft; NULL: sequence b's rows are [b * max_rows, (b + 1) * max_rows) */
+  const uint32_t *kmask;     /* device [nseq][nwords], bit j % 32 of word j / 32: row j of the cache is seen; NULL: all are */
+  float scale;               /* logit scale; 0 => 1/sqrt(d) */
+  int32_t _pad0;
+} rs_cross;
+
+/* O (bf16) and lse as rs_draft_attn writes them, with its arithmetic: rows that see nothing (no states, all hidden) get
+ * O = 0 and lse = -inf, hidden states count for nothing whatever they hold, and rows of no sequence are neither read nor written.
+ * Of the cache only k, v, table and len are read. */
+size_t rs_cross_attn_workspace_size(const rs_cache *cache, const rs_cross *cross);
+rs_status rs_cross_attn(const rs_cache *cache, const rs_cross *cross, void *o, int64_t so_t, int64_t so_h, float *lse,
+                        void *ws, size_t ws_bytes, rs_stream stream);
 
 /* Message describing the last failure of the calling thread ("" if none). */
 const char *rs_last_error(void);

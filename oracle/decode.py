@@ -121,3 +121,26 @@ def evict(acc, pos, seen, n, budget, nsink, nrecent):
     neg = np.signbit(acc[:n]) & ~must  # -0.0 comes after +0.0
     stay = np.lexsort((np.arange(n), neg, -key, ~must))[:budget]
     return np.setdiff1d(np.arange(budget), stay), np.sort(stay[stay >= budget])
+
+
+def cross(q, k, v, lens, table, page, rows, kmask, cap, scale):
+    """Attention of a decoder's rows over the cached rows that kmask [nseq, words] (or None) leaves: dict of o, lse,
+    abs and span as of draft()."""
+    nrows, hq, d = q.shape
+    hkv = k.shape[1]
+    G = hq // hkv
+    o, lse, ab, span = np.full((nrows, hq, d), np.nan), np.full((hq, nrows), np.nan), np.zeros((nrows, hq, d)), 0.0
+    for b, (f, t) in enumerate(rows):
+        n = min(max(int(lens[b]), 0), cap)
+        bits = np.ones(n, bool) if kmask is None else seen_drafts(kmask, b, 0, n)
+        for g in range(hkv):
+            if t == 0:
+                continue
+            kk, ok = cache_rows(k, table, page, b, g, n)
+            vv, _ = cache_rows(v, table, page, b, g, n)
+            for i in range(t):
+                for h in range(g * G, g * G + G):
+                    r = softmax_row(q[f + i, h], kk, vv, ok & bits, scale)
+                    o[f + i, h], lse[h, f + i], ab[f + i, h] = r[0], r[1], r[3]
+                    span = max(span, r[4])
+    return dict(o=o, lse=lse, abs=ab, span=span)

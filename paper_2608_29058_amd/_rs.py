@@ -17,6 +17,8 @@ RS_OK, RS_ERR_INVALID_ARG, RS_ERR_UNSUPPORTED, RS_ERR_HIP, RS_ERR_WORKSPACE, RS_
 RS_BF16, RS_F32 = 0, 1
 RS_DENSE, RS_ASHAPE, RS_VSLASH, RS_BSPARSE = 0, 1, 2, 3
 RS_PROBE_ROWS, RS_PROBE_BLOCKMEAN = 1, 2
+RS_ROPE_HALF, RS_ROPE_INTERLEAVED = 0, 1
+RS_ROPE_PLAIN, RS_ROPE_LINEAR, RS_ROPE_TURNS, RS_ROPE_PAIRS = 0, 1, 2, 3
 
 EXPORTS = ["rs_unit_table_size", "rs_unit_table_init",
            "rs_probe_workspace_size", "rs_probe", "rs_build_indices_workspace_size",
@@ -27,6 +29,7 @@ EXPORTS = ["rs_unit_table_size", "rs_unit_table_init",
            "rs_cache_append", "rs_cache_commit", "rs_draft_attn_workspace_size", "rs_draft_attn",
            "rs_select_attn_workspace_size", "rs_select_attn", "rs_attn_weights",
            "rs_cache_evict_workspace_size", "rs_cache_evict",
+           "rs_rope_init", "rs_rope_apply", "rs_cache_append_rope", "rs_cross_attn_workspace_size", "rs_cross_attn",
            "rs_last_error", "rs_version"]
 
 P = C.c_void_p
@@ -115,6 +118,28 @@ class RsDraft(C.Structure):
                 ("sq_h", I64), ("start", P), ("mask", P), ("scale", C.c_float), ("_pad0", I32)]
 
 
+class RsRopeCfg(C.Structure):
+    _fields_ = [("dim", I32), ("layout", I32), ("scaling", I32), ("_pad0", I32), ("base", C.c_double), ("factor", C.c_double),
+                ("context", C.c_double), ("low", C.c_double), ("high", C.c_double), ("mscale", C.c_double)]
+
+
+class RsRope(C.Structure):
+    _fields_ = [("dim", I32), ("layout", I32), ("mscale", C.c_float), ("_pad0", I32), ("turns", C.c_double * 64)]
+
+
+class RsRopePart(C.Structure):
+    _fields_ = [("x", P), ("y", P), ("heads", I32), ("_pad0", I32), ("sx_t", I64), ("sx_h", I64), ("sy_t", I64), ("sy_h", I64)]
+
+
+class RsRopeRows(C.Structure):
+    _fields_ = [("dtype", I32), ("n", I32), ("d", I32), ("nparts", I32), ("pos", P), ("pos0", I64), ("part", RsRopePart * 4)]
+
+
+class RsCross(C.Structure):
+    _fields_ = [("q", P), ("hq", I32), ("nrows", I32), ("max_rows", I32), ("nwords", I32), ("sq_t", I64), ("sq_h", I64),
+                ("start", P), ("kmask", P), ("scale", C.c_float), ("_pad0", I32)]
+
+
 _lib = None
 
 
@@ -124,13 +149,14 @@ def lib():
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_2608_29058_amd.build`")
+        import torch  # noqa: F401  (first: the library then shares torch's HIP runtime instead of loading another one)
         L = C.CDLL(LIB_PATH)
         L.rs_last_error.restype = C.c_char_p
         L.rs_version.restype = C.c_char_p
         for name in ("rs_unit_table_size", "rs_probe_workspace_size", "rs_build_indices_workspace_size",
                      "rs_attn_workspace_size", "rs_route_layer_device_workspace_size",
                      "rs_routed_attn_workspace_size", "rs_vt_bytes", "rs_draft_attn_workspace_size",
-                     "rs_select_attn_workspace_size", "rs_cache_evict_workspace_size"):
+                     "rs_select_attn_workspace_size", "rs_cache_evict_workspace_size", "rs_cross_attn_workspace_size"):
             getattr(L, name).restype = C.c_size_t
         L.rs_unit_table_size.argtypes = [C.POINTER(RsQkv), C.POINTER(RsUnit), I32, C.POINTER(RsProbeCfg)]
         L.rs_unit_table_init.argtypes = [C.POINTER(RsQkv), C.POINTER(RsUnit), I32, C.POINTER(RsProbeCfg), P,
@@ -171,8 +197,14 @@ def lib():
         L.rs_attn_weights.argtypes = [ca, dr, P, P, P, P, P]
         L.rs_cache_evict_workspace_size.argtypes = [ca, I32]
         L.rs_cache_evict.argtypes = [ca, I32, I32, I32, P, C.c_size_t, P]
+        rp, cr = C.POINTER(RsRope), C.POINTER(RsCross)
+        L.rs_rope_init.argtypes = [C.POINTER(RsRopeCfg), rp]
+        L.rs_rope_apply.argtypes = [rp, C.POINTER(RsRopeRows), I32, P]
+        L.rs_cache_append_rope.argtypes = [ca, rp, P, P, I64, I64, I64, I64, C.POINTER(RsRopePart), P, P, I32, I32, P]
+        L.rs_cross_attn_workspace_size.argtypes = [ca, cr]
+        L.rs_cross_attn.argtypes = [ca, cr, P, I64, I64, P, P, C.c_size_t, P]
         for name in ("rs_cache_append", "rs_cache_commit", "rs_draft_attn", "rs_select_attn", "rs_attn_weights",
-                     "rs_cache_evict"):
+                     "rs_cache_evict", "rs_rope_init", "rs_rope_apply", "rs_cache_append_rope", "rs_cross_attn"):
             getattr(L, name).restype = C.c_int
         for name in ("rs_unit_table_init", "rs_probe", "rs_build_indices", "rs_route_layer", "rs_sparse_attn_prefill",
                      "rs_dense_attn_prefill", "rs_error_predict", "rs_route_layer_device",
@@ -615,13 +647,17 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def rs_cache_append(cache, k_new, v_new, max_rows=1, start=None, stream=None):
-    """k_new, v_new: [nrows, hkv, d] of the cache's dtype (last dim contiguous)."""
+def _check_new_rows(cache, k_new, v_new, start):
     import torch
     _want(k_new.dim() == 3 and k_new.shape == v_new.shape and k_new.shape[1] == cache.hkv and k_new.shape[2] == cache.d
           and k_new.dtype is cache.dtype is v_new.dtype and (k_new.stride(2) == v_new.stride(2) == 1 or not k_new.numel())
           and k_new.device == cache.device == v_new.device, "k_new and v_new must be [nrows, hkv, d] like the cache")
     _want(_like(start, torch.int32, (cache.nseq + 1,), cache.device), "start must be contiguous int32 [nseq + 1]")
+
+
+def rs_cache_append(cache, k_new, v_new, max_rows=1, start=None, stream=None):
+    """k_new, v_new: [nrows, hkv, d] of the cache's dtype (last dim contiguous)."""
+    _check_new_rows(cache, k_new, v_new, start)
     return _on_device(lib().rs_cache_append, cache.device, stream,
                       (cache.ref, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), v_new.stride(0),
                        v_new.stride(1), _at(start), k_new.shape[0], max_rows))
@@ -679,3 +715,110 @@ def rs_cache_evict_workspace_size(cache, budget):
 
 def rs_cache_evict(cache, budget, nsink, nrecent, ws, stream=None):
     return _on_device(lib().rs_cache_evict, cache.device, stream, (cache.ref, budget, nsink, nrecent, *_ws(ws, cache)))
+
+
+# ---- rotary positions -----------------------------------------------------------------------
+
+class Rope:
+    """Rotary positions (rs_rope): the first dim elements of a head, base, layout RS_ROPE_HALF or RS_ROPE_INTERLEAVED,
+    frequencies scaled by RS_ROPE_PLAIN, _LINEAR, _TURNS or _PAIRS with factor, context, low and high; mscale.  turns:
+    frequencies of another rule, in turns per position, dim / 2 of them."""
+
+    def __init__(self, dim, base=10000.0, layout=RS_ROPE_HALF, scaling=RS_ROPE_PLAIN, factor=1.0, context=0.0, low=1.0, high=32.0,
+                 mscale=1.0, turns=None):
+        self.c = RsRope()
+        cfg = RsRopeCfg(dim=dim, layout=layout, scaling=scaling, base=base, factor=factor, context=context, low=low, high=high,
+                        mscale=mscale)
+        _check(lib().rs_rope_init(C.byref(cfg), C.byref(self.c)))
+        if turns is not None:
+            turns = [float(x) for x in turns]
+            _want(len(turns) == dim // 2, "turns must have dim / 2 entries")
+            self.c.turns[:len(turns)] = turns
+        self.ref = C.byref(self.c)
+
+
+def _row_strides(t):
+    """Strides of [rows, heads, d] in elements; a dimension of one entry is given a row's length."""
+    return [t.stride(i) if t.shape[i] > 1 else t.shape[2] for i in (0, 1)]
+
+
+def _rope_part(x, y):
+    _want(x.dim() == 3 and y.shape == x.shape and y.dtype is x.dtype and y.device == x.device
+          and (x.stride(2) == y.stride(2) == 1 or not x.numel()), "x and y must be [n, heads, d] alike, with a contiguous last dimension")
+    (xt, xh), (yt, yh) = _row_strides(x), _row_strides(y)
+    return RsRopePart(x=x.data_ptr(), y=y.data_ptr(), heads=x.shape[1], sx_t=xt, sx_h=xh, sy_t=yt, sy_h=yh)
+
+
+class RopeRows:
+    """Descriptor (rs_rope_rows) of rows that share positions: parts: 1 to 4 pairs (x, y) of [n, heads, d] tensors (bf16 or
+    float32, any strides, last dim contiguous; y may be x), Q and K for instance; pos: int32 [n], or None: pos0 + row."""
+
+    def __init__(self, parts, pos=None, pos0=0):
+        import torch
+        parts = [tuple(p) for p in parts]
+        _want(1 <= len(parts) <= 4, "1 to 4 parts")
+        x0 = parts[0][0]
+        _want(x0.dtype in (torch.bfloat16, torch.float32), "the rows must be bf16 or float32")
+        _want(x0.dim() == 3 and all(x.dim() == 3 and x.shape[0] == x0.shape[0] and x.shape[2] == x0.shape[2] and x.dtype is x0.dtype
+                                    and x.device == x0.device for x, _ in parts), "the parts must share n, d, dtype and device")
+        _want(_like(pos, torch.int32, (x0.shape[0],), x0.device), "pos must be contiguous int32 [n] on the device of the rows")
+        self.parts, self.pos, self.device = parts, pos, x0.device
+        self.c = RsRopeRows(dtype=RS_BF16 if x0.dtype is torch.bfloat16 else RS_F32, n=x0.shape[0], d=x0.shape[2], nparts=len(parts),
+                            pos=_at(pos), pos0=pos0)
+        for i, (x, y) in enumerate(parts):
+            self.c.part[i] = _rope_part(x, y)
+        self.ref = C.byref(self.c)
+
+
+def rs_rope_apply(rope, rows, transpose=False, stream=None):
+    return _on_device(lib().rs_rope_apply, rows.device, stream, (rope.ref, rows.ref, int(transpose)))
+
+
+def rs_cache_append_rope(cache, rope, k_new, v_new, q=None, q_out=None, max_rows=1, start=None, pos=None, stream=None):
+    """As rs_cache_append, K rotated; q (or None): [nrows, hq, d], rotated into q_out (None: in place); pos: int32 [nrows] or
+    None."""
+    import torch
+    _check_new_rows(cache, k_new, v_new, start)
+    _want(_like(pos, torch.int32, (k_new.shape[0],), cache.device), "pos must be contiguous int32 [nrows]")
+    part = None
+    if q is not None:
+        _want(q.dim() == 3 and q.shape[0] == k_new.shape[0] and q.shape[2] == cache.d and q.dtype is cache.dtype
+              and q.device == cache.device, "q must be [nrows, hq, d] with the cache's dtype and device")
+        part = C.byref(_rope_part(q, q if q_out is None else q_out))
+    return _on_device(lib().rs_cache_append_rope, cache.device, stream,
+                      (cache.ref, rope.ref, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), v_new.stride(0),
+                       v_new.stride(1), part, _at(pos), _at(start), k_new.shape[0], max_rows))
+
+
+# ---- cross attention -------------------------------------------------------------------------
+
+class Cross:
+    """Descriptor (rs_cross) of a decoder's rows: q: [nrows, hq, d] (last dim contiguous); start: int32 [nseq + 1] (None: max_rows
+    rows per sequence); kmask: int32 [nseq, nwords], bit j of a row: the sequence's cached row j is seen."""
+
+    def __init__(self, q, max_rows=1, start=None, kmask=None, scale=0.0):
+        import torch
+        _want(q.dim() == 3 and (q.stride(2) == 1 or not q.numel()), "q must be [nrows, hq, d] with a contiguous last dimension")
+        for name, t in (("start", start), ("kmask", kmask)):
+            _want(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == q.device),
+                  f"{name} must be a contiguous int32 tensor on the device of q")
+        _want(kmask is None or kmask.dim() == 2, "kmask must be [nseq, nwords]")
+        self.q, self.start, self.mask = q, start, kmask
+        self.nrows, self.hq, self.d, self.device = q.shape[0], q.shape[1], q.shape[2], q.device
+        st, sh = _row_strides(q)
+        self.c = RsCross(q=q.data_ptr(), hq=q.shape[1], nrows=q.shape[0], max_rows=max_rows,
+                         nwords=kmask.shape[1] if kmask is not None else 0, sq_t=st, sq_h=sh, start=_at(start), kmask=_at(kmask),
+                         scale=scale)
+        self.ref = C.byref(self.c)
+
+
+def rs_cross_attn_workspace_size(cache, cross):
+    return lib().rs_cross_attn_workspace_size(cache.ref, cross.ref)
+
+
+def rs_cross_attn(cache, cross, o, lse, ws, stream=None):
+    """o: bf16 [nrows, hq, d]; lse: float32 [hq, nrows] or None."""
+    _check_rows_out(cache, cross, o, lse)
+    _want(cross.mask is None or cross.mask.shape[0] == cache.nseq, "kmask must be [nseq, nwords]")
+    return _on_device(lib().rs_cross_attn, cache.device, stream,
+                      (cache.ref, cross.ref, o.data_ptr(), o.stride(0), o.stride(1), _at(lse), *_ws(ws, cache)))

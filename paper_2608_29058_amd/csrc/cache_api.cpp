@@ -5,7 +5,8 @@
 #include <string>
 
 #include "common.h"
-#include "cache.h"
+#include "draft_plan.h"
+#include "rope.h"
 
 namespace rs {
 
@@ -16,9 +17,9 @@ rs_status commit_launch(const CacheView &c, int dtype, int d, const int32_t *nac
 size_t evict_ws_bytes(int64_t items, int budget, int cap);
 rs_status evict_launch(const CacheView &c, int dtype, int d, int budget, int nsink, int nrecent, void *ws, size_t ws_bytes,
                        hipStream_t st);
-size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel);
-rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
-                       void *ws, size_t ws_bytes, hipStream_t st);
+size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int what);
+rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, int what, void *o, int64_t so_t, int64_t so_h,
+                       float *lse, void *ws, size_t ws_bytes, hipStream_t st);
 rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int nsink, int nlocal, void *o,
                         int64_t so_t, int64_t so_h, float *lse, int32_t *blocks, void *ws, size_t ws_bytes, hipStream_t st);
 rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d, const float *lse, const float *row_w,
@@ -60,30 +61,48 @@ static rs_status check_cache(const rs_cache *x, CacheView *c) {
   return RS_OK;
 }
 
-static rs_status check_draft(const rs_cache *x, const rs_draft *y, DraftView *q) {
-  if (!y) return fail(RS_ERR_INVALID_ARG, "draft is NULL");
-  if ((!y->q && y->nrows != 0) || !aligned16(y->q)) return fail(RS_ERR_INVALID_ARG, "draft: q must be a 16-byte aligned device pointer");
-  if (y->hq < 1 || y->hq > 65535 || y->hq % x->hkv != 0) return fail(RS_ERR_INVALID_ARG, "draft: hq must be a positive multiple of hkv");
-  if (y->nrows < 0 || y->max_rows < 1) return fail(RS_ERR_INVALID_ARG, "draft: nrows < 0 or max_rows < 1");
-  if (y->max_rows > kMaxDraft) return fail(RS_ERR_UNSUPPORTED, "draft: at most 256 new rows per sequence");
-  if (y->nrows > (1 << 20)) return fail(RS_ERR_UNSUPPORTED, "draft: at most 1048576 new rows");
+// What rs_draft and rs_cross have in common: queries of new rows.
+template <typename Y>
+static rs_status check_queries(const rs_cache *x, const Y *y, int most_rows, const std::string &name, DraftView *q) {
+  if (!y) return fail(RS_ERR_INVALID_ARG, name + " is NULL");
+  if ((!y->q && y->nrows != 0) || !aligned16(y->q)) return fail(RS_ERR_INVALID_ARG, name + ": q must be a 16-byte aligned device pointer");
+  if (y->hq < 1 || y->hq > 65535 || y->hq % x->hkv != 0) return fail(RS_ERR_INVALID_ARG, name + ": hq must be a positive multiple of hkv");
+  if (y->nrows < 0 || y->max_rows < 1) return fail(RS_ERR_INVALID_ARG, name + ": nrows < 0 or max_rows < 1");
+  if (y->max_rows > most_rows) return fail(RS_ERR_UNSUPPORTED, name + ": at most " + std::to_string(most_rows) + " new rows per sequence");
+  if (y->nrows > (1 << 20)) return fail(RS_ERR_UNSUPPORTED, name + ": at most 1048576 new rows");
   if ((int64_t)x->nseq * y->hq * y->max_rows > (1 << 28))
-    return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^28 rows of queries (nseq x hq x max_rows)");
-  if ((int64_t)y->nrows * x->hkv > (1 << 24)) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^24 new rows x key/value heads");
+    return fail(RS_ERR_UNSUPPORTED, name + ": at most 2^28 rows of queries (nseq x hq x max_rows)");
+  if ((int64_t)y->nrows * x->hkv > (1 << 24)) return fail(RS_ERR_UNSUPPORTED, name + ": at most 2^24 new rows x key/value heads");
   if (!y->start && (int64_t)x->nseq * y->max_rows > y->nrows)
-    return fail(RS_ERR_INVALID_ARG, "draft: without start every sequence has max_rows rows");
-  if (y->mask && (y->nwords < 1 || (int64_t)y->nwords * 32 < y->max_rows)) return fail(RS_ERR_INVALID_ARG, "draft: mask rows shorter than max_rows");
+    return fail(RS_ERR_INVALID_ARG, name + ": without start every sequence has max_rows rows");
   const int vec = x->dtype == RS_BF16 ? 8 : 4;
-  if (y->sq_t < 0 || y->sq_h < 0 || y->sq_t % vec || y->sq_h % vec) return fail(RS_ERR_INVALID_ARG, "draft: strides must be non-negative multiples of 16 bytes");
+  if (y->sq_t < 0 || y->sq_h < 0 || y->sq_t % vec || y->sq_h % vec) return fail(RS_ERR_INVALID_ARG, name + ": strides must be non-negative multiples of 16 bytes");
   float sc = y->scale;
   if (sc == 0.f) sc = 1.f / std::sqrt((float)x->d);
-  if (!(sc > 0.f) || !std::isfinite(sc)) return fail(RS_ERR_INVALID_ARG, "draft: scale must be positive and finite");
+  if (!(sc > 0.f) || !std::isfinite(sc)) return fail(RS_ERR_INVALID_ARG, name + ": scale must be positive and finite");
   q->q = y->q;
   q->hq = y->hq, q->nrows = y->nrows, q->max_rows = y->max_rows, q->nwords = y->nwords;
   q->sq_t = y->sq_t, q->sq_h = y->sq_h;
   q->start = y->start;
-  q->mask = y->mask;
   q->c = sc * kLog2e;
+  return RS_OK;
+}
+
+static rs_status check_draft(const rs_cache *x, const rs_draft *y, DraftView *q) {
+  rs_status st;
+  if ((st = check_queries(x, y, kMaxDraft, "draft", q)) != RS_OK) return st;
+  if (y->mask && (y->nwords < 1 || (int64_t)y->nwords * 32 < y->max_rows)) return fail(RS_ERR_INVALID_ARG, "draft: mask rows shorter than max_rows");
+  q->mask = y->mask;
+  return RS_OK;
+}
+
+static rs_status check_cross(const rs_cache *x, const rs_cross *y, DraftView *q) {
+  rs_status st;
+  if ((st = check_queries(x, y, 1 << 28, "cross", q)) != RS_OK) return st;
+  if (y->kmask && (y->nwords < 1 || (int64_t)y->nwords * 32 < (int64_t)x->page * x->max_pages))
+    return fail(RS_ERR_INVALID_ARG, "cross: key mask shorter than the cache's capacity");
+  if ((uintptr_t)y->kmask & 3) return fail(RS_ERR_INVALID_ARG, "cross: kmask must be 4-byte aligned");
+  q->mask = y->kmask;
   return RS_OK;
 }
 
@@ -91,6 +110,21 @@ static rs_status check_rows_out(const void *o, int64_t so_t, int64_t so_h, int d
   if (!o) return fail(RS_ERR_INVALID_ARG, "output is NULL");
   if (((uintptr_t)o & 7) || so_t % 4 != 0 || so_h % 4 != 0 || so_t < d || so_h < d)
     return fail(RS_ERR_INVALID_ARG, "output must be 8-byte aligned with strides of at least d, multiples of 4 elements");
+  return RS_OK;
+}
+
+// The new rows of an append.
+static rs_status check_append(const rs_cache *cache, CacheView *c, const void *k_new, const void *v_new, int64_t sk_t, int64_t sk_h,
+                              int64_t sv_t, int64_t sv_h, const int32_t *start, int32_t nrows, int32_t max_rows) {
+  rs_status st;
+  if ((st = check_cache(cache, c)) != RS_OK) return st;
+  if (((!k_new || !v_new) && nrows != 0) || !aligned16(k_new) || !aligned16(v_new)) return fail(RS_ERR_INVALID_ARG, "append: k_new and v_new must be 16-byte aligned device pointers");
+  const int vec = cache->dtype == RS_BF16 ? 8 : 4;
+  const int64_t s[4] = {sk_t, sk_h, sv_t, sv_h};
+  for (int i = 0; i < 4; ++i)
+    if (s[i] < 0 || s[i] % vec != 0) return fail(RS_ERR_INVALID_ARG, "append: strides must be non-negative multiples of 16 bytes");
+  if (nrows < 0 || max_rows < 1) return fail(RS_ERR_INVALID_ARG, "append: nrows < 0 or max_rows < 1");
+  if (!start && (int64_t)c->nseq * max_rows > nrows) return fail(RS_ERR_INVALID_ARG, "append: without start every sequence has max_rows rows");
   return RS_OK;
 }
 
@@ -114,16 +148,23 @@ rs_status rs_cache_append(const rs_cache *cache, const void *k_new, const void *
   set_error("");
   CacheView c;
   rs_status st;
-  if ((st = check_cache(cache, &c)) != RS_OK) return st;
-  if (((!k_new || !v_new) && nrows != 0) || !aligned16(k_new) || !aligned16(v_new)) return fail(RS_ERR_INVALID_ARG, "append: k_new and v_new must be 16-byte aligned device pointers");
-  const int vec = cache->dtype == RS_BF16 ? 8 : 4;
-  const int64_t s[4] = {sk_t, sk_h, sv_t, sv_h};
-  for (int i = 0; i < 4; ++i)
-    if (s[i] < 0 || s[i] % vec != 0) return fail(RS_ERR_INVALID_ARG, "append: strides must be non-negative multiples of 16 bytes");
-  if (nrows < 0 || max_rows < 1) return fail(RS_ERR_INVALID_ARG, "append: nrows < 0 or max_rows < 1");
-  if (!start && (int64_t)c.nseq * max_rows > nrows) return fail(RS_ERR_INVALID_ARG, "append: without start every sequence has max_rows rows");
+  if ((st = check_append(cache, &c, k_new, v_new, sk_t, sk_h, sv_t, sv_h, start, nrows, max_rows)) != RS_OK) return st;
   if (nrows == 0) return RS_OK;
   return append_launch(c, cache->dtype, cache->d, k_new, v_new, sk_t, sk_h, sv_t, sv_h, start, nrows, max_rows, (hipStream_t)stream);
+}
+
+rs_status rs_cache_append_rope(const rs_cache *cache, const rs_rope *rope, const void *k_new, const void *v_new, int64_t sk_t,
+                               int64_t sk_h, int64_t sv_t, int64_t sv_h, const rs_rope_part *q, const int32_t *pos,
+                               const int32_t *start, int32_t nrows, int32_t max_rows, rs_stream stream) {
+  set_error("");
+  CacheView c;
+  rs_status st;
+  if ((st = check_append(cache, &c, k_new, v_new, sk_t, sk_h, sv_t, sv_h, start, nrows, max_rows)) != RS_OK) return st;
+  if ((st = check_rope(rope, cache->d)) != RS_OK) return st;
+  if (nrows == 0) return RS_OK;
+  if (q && (st = check_rope_part(q, cache->dtype, cache->d, nrows, "append: q")) != RS_OK) return st;
+  return append_rope_launch(c, cache->dtype, cache->d, *rope, k_new, v_new, sk_t, sk_h, sv_t, sv_h, q, pos, start, nrows, max_rows,
+                            (hipStream_t)stream);
 }
 
 rs_status rs_cache_commit(const rs_cache *cache, const int32_t *naccept, const int32_t *path, int32_t max_new, rs_stream stream) {
@@ -142,7 +183,7 @@ size_t rs_draft_attn_workspace_size(const rs_cache *cache, const rs_draft *draft
   CacheView c;
   DraftView q;
   if (check_cache(cache, &c) != RS_OK || check_draft(cache, draft, &q) != RS_OK) return 0;
-  return draft_ws_bytes(c, q, cache->dtype == RS_F32, cache->d, 0);
+  return draft_ws_bytes(c, q, cache->dtype == RS_F32, cache->d, 0, W_ALL);
 }
 
 rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, int64_t so_t, int64_t so_h, float *lse, void *ws,
@@ -156,14 +197,35 @@ rs_status rs_draft_attn(const rs_cache *cache, const rs_draft *draft, void *o, i
   if (q.nrows == 0) return RS_OK;
   if ((st = check_rows_out(o, so_t, so_h, cache->d)) != RS_OK) return st;
   if (!aligned16(ws)) return fail(RS_ERR_WORKSPACE, "workspace must be 16-byte aligned");
-  return draft_launch(c, q, cache->dtype == RS_F32, cache->d, o, so_t, so_h, lse, ws, ws_bytes, (hipStream_t)stream);
+  return draft_launch(c, q, cache->dtype == RS_F32, cache->d, W_ALL, o, so_t, so_h, lse, ws, ws_bytes, (hipStream_t)stream);
+}
+
+size_t rs_cross_attn_workspace_size(const rs_cache *cache, const rs_cross *cross) {
+  CacheView c;
+  DraftView q;
+  if (check_cache(cache, &c) != RS_OK || check_cross(cache, cross, &q) != RS_OK) return 0;
+  return draft_ws_bytes(c, q, cache->dtype == RS_F32, cache->d, 0, W_CROSS);
+}
+
+rs_status rs_cross_attn(const rs_cache *cache, const rs_cross *cross, void *o, int64_t so_t, int64_t so_h, float *lse, void *ws,
+                        size_t ws_bytes, rs_stream stream) {
+  set_error("");
+  CacheView c;
+  DraftView q;
+  rs_status st;
+  if ((st = check_cache(cache, &c)) != RS_OK) return st;
+  if ((st = check_cross(cache, cross, &q)) != RS_OK) return st;
+  if (q.nrows == 0) return RS_OK;
+  if ((st = check_rows_out(o, so_t, so_h, cache->d)) != RS_OK) return st;
+  if (!aligned16(ws)) return fail(RS_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+  return draft_launch(c, q, cache->dtype == RS_F32, cache->d, W_CROSS, o, so_t, so_h, lse, ws, ws_bytes, (hipStream_t)stream);
 }
 
 size_t rs_select_attn_workspace_size(const rs_cache *cache, const rs_draft *draft, int32_t nsel) {
   CacheView c;
   DraftView q;
   if (check_cache(cache, &c) != RS_OK || check_draft(cache, draft, &q) != RS_OK || nsel < 1 || nsel > kMaxN / 64) return 0;
-  return draft_ws_bytes(c, q, cache->dtype == RS_F32, cache->d, nsel);
+  return draft_ws_bytes(c, q, cache->dtype == RS_F32, cache->d, nsel, W_SELECT);
 }
 
 rs_status rs_select_attn(const rs_cache *cache, const rs_draft *draft, int32_t nsel, int32_t nsink, int32_t nlocal, void *o,

@@ -14,14 +14,11 @@
 //     operands (dimension (d / 16) m + t of the t-th) stays inside the lane: one v_perm per two values.
 // Each of the four (short caches: eight) waves takes every fourth (eighth) tile of 32 rows with a running maximum and
 // sum of its own and keeps the next tile in flight; the waves are joined once, through LDS, at the end.
-#include "common.h"
-#include "cache.h"
+#include "draft_plan.h"
 
 namespace rs {
 
 namespace {
-
-constexpr int kTile = 32, kWaves = 4, kGroup = kTile * kWaves;  // rows per wave and step, per workgroup and step
 
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
@@ -88,12 +85,6 @@ __device__ __forceinline__ void split8(f32x4 a, f32x4 b, u32x4 &hi, u32x4 &lo) {
   split2(a[2], a[3], h, l), hi[1] = h, lo[1] = l;
   split2(b[0], b[1], h, l), hi[2] = h, lo[2] = l;
   split2(b[2], b[3], h, l), hi[3] = h, lo[3] = l;
-}
-
-// Wave-uniform loads through the scalar cache of arrays that the kernel does not write.
-__device__ __forceinline__ int uload(const int32_t *p, int64_t i) {
-  typedef const __attribute__((address_space(4))) int32_t cint;
-  return ((cint *)p)[i];
 }
 
 // ---- one tile of K and V in registers --------------------------------------------------------
@@ -189,6 +180,7 @@ __device__ __forceinline__ void stage_barrier() {
 struct RowsOf {
   const DraftView *q;
   int len, total, t, first;  // cached rows; with the drafted ones; new rows and the first of them
+  int b;                     // the sequence
 };
 
 // S^T of 16 cached rows (operand k) and NQ x 16 rows of Q.
@@ -228,6 +220,12 @@ __device__ __forceinline__ uint32_t seen_rows(const RowsOf &ro, int i, int j) {
     drafts = (uint32_t)(((uint64_t)hi << 32 | lo) >> (x & 31));
   }
   return low_bits(-x) | (drafts & low_bits(ro.total - j));
+}
+
+// W_CROSS: which of the rows j .. j + 31 the sequence's queries see, as bits; j is a multiple of 32.
+__device__ __forceinline__ uint32_t seen_keys(const RowsOf &ro, int j) {
+  const uint32_t all = low_bits(ro.total - j);
+  return ro.q->mask ? all & (uint32_t)uload((const int32_t *)ro.q->mask, (int64_t)ro.b * ro.q->nwords + (j >> 5)) : all;
 }
 
 // An edge: a tile of 32 rows from row j that some row of Q may not see in whole (drafted rows, the end).  Scores
@@ -293,6 +291,18 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[2 * NT][NQ], float c, flo
   }
 }
 
+// W_CROSS: a tile of 32 rows some of which nobody sees (`see`).
+template <int NQ>
+__device__ __forceinline__ void hide_scores(uint32_t see, int h, f32x4 (&s)[2][NQ]) {
+  see >>= 4 * h;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[u][n][e] = see >> (16 * u + e) & 1 ? s[u][n][e] : -__builtin_inff();
+}
+
 // A value whose bf16 part is infinite or NaN: a zero weight does not silence it.
 __device__ __forceinline__ bool is_special(uint32_t bf) { return (bf & 0x7f80u) == 0x7f80u; }
 
@@ -326,6 +336,17 @@ __device__ __forceinline__ bool clean_values(VTile<F32, D> &v) {
   return true;
 }
 
+// Zeroes the rows of V that nobody sees: they count for nothing whatever they hold.
+template <bool F32, int D>
+__device__ __forceinline__ void hide_values(VTile<F32, D> &v, uint32_t see, int h) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t keep = see >> ((i < 4 ? i : 12 + i) + 4 * h) & 1 ? ~0u : 0u;
+#pragma unroll
+    for (int w = 0; w < Tile<F32, D>::VW; ++w) v[i][w] &= keep;
+  }
+}
+
 // O^T += V^T P^T over a tile.
 template <bool F32, int D, int NQ>
 __device__ __forceinline__ void add_values(const VTile<F32, D> &v, const u32x4 (&pb)[NQ], f32x4 (&oacc)[NQ][D / 16]) {
@@ -339,113 +360,6 @@ __device__ __forceinline__ void add_values(const VTile<F32, D> &v, const u32x4 (
       oacc[n][t] = mfma16(vh, pb[n], oacc[n][t]);
     }
   }
-}
-
-// ---- the work of a workgroup -------------------------------------------------------------------
-// Sequences differ in length, and their lengths are known on the device only.  Every workgroup reads all
-// lengths and derives the same plan: the pieces of every item (sequence, head, row tile) in groups of 128
-// rows, equal to within one, so that all items together make about `slots` pieces.
-
-// Pieces of a sequence of `tiles` groups at `per` groups a piece.
-RS_HD int pieces_of(int tiles, int per) { return tiles > per ? (tiles + per - 1) / per : 1; }
-
-struct DraftArgs {
-  CacheView c;
-  DraftView q;
-  char *o;
-  int64_t so_t, so_h;
-  float *lse;
-  float *po, *pml;   // pieces: O (unnormalised), then (max, sum) of every row
-  int rtiles, trows; // row tiles of a sequence with max_rows rows, rows of one
-  int slots, least;  // pieces that all items together may have beyond one each; groups of a piece at least
-  const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
-  int nsel, pieces;  // with a list: pieces per item
-};
-
-// Rows of keys of sequence b that the kernels walk: cached rows and drafts.
-__device__ __forceinline__ int walk_len(const DraftArgs &a, int len, int t) {
-  return len + t < a.c.cap ? len + t : a.c.cap;
-}
-
-// What a workgroup works on.
-struct Item {
-  int b, g, rt, piece, npieces, slot0;  // slot0: the item's first slot of pieces
-  int len, t, first;                    // rows held, new rows and the first of them
-};
-
-// (what lanes agree on, said so: scalar registers, scalar branches)
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ Item uniform(const Item &x) {
-  return Item{uniform(x.b), uniform(x.g), uniform(x.rt), uniform(x.piece), uniform(x.npieces), uniform(x.slot0),
-              uniform(x.len), uniform(x.t), uniform(x.first)};
-}
-
-// Sequence of new row r, by the wave; -1: none.
-__device__ __forceinline__ int seq_of_row(const CacheView &c, const DraftView &q, int r, int lane) {
-  for (int b0 = 0; b0 < c.nseq; b0 += 64) {
-    RowRange x{0, 0};
-    if (b0 + lane < c.nseq) x = new_rows(q.start, b0 + lane, q.nrows, q.max_rows);
-    const unsigned long long hit = __ballot(r >= x.first && r < x.first + x.count);
-    if (hit) return b0 + __builtin_ctzll(hit);
-  }
-  return -1;
-}
-
-// What a lane knows of sequence b = b0 + lane; without new rows it has no items.
-struct Seq {
-  RowRange r;
-  int len, groups;
-};
-__device__ __forceinline__ Seq seq_at(const DraftArgs &a, int b) {
-  Seq s{RowRange{0, 0}, 0, 0};
-  if (b < a.c.nseq) {
-    s.r = new_rows(a.q.start, b, a.q.nrows, a.q.max_rows);
-    s.len = cache_len(a.c, b);
-    if (s.r.count > 0) s.groups = (walk_len(a, s.len, s.r.count) + kGroup - 1) / kGroup;
-  }
-  return s;
-}
-
-// Groups per piece: the same from the lengths alone in every workgroup and in the joining kernel.  first: the
-// sequences of the first round of lanes.
-__device__ __forceinline__ int plan_groups(const DraftArgs &a, const Seq &first, int lane) {
-  if (a.slots == 0) return kMaxN;  // one piece each
-  int work = first.groups;  // (at most 65535 sequences of 2048 groups)
-  for (int b0 = 64; b0 < a.c.nseq; b0 += 64) work += seq_at(a, b0 + lane).groups;
-  work = wave_sum(work);
-  // with pieces of at most C = ceil(total / slots) groups an item of n groups has less than n / C + 1 of them:
-  // all together at most slots + the number of items, which is what the host counts
-  const long long total = (long long)work * a.c.hkv * a.rtiles, groups = (total + a.slots - 1) / a.slots;
-  return groups > a.least ? (int)groups : a.least;
-}
-
-// The id-th piece overall; false: there are fewer.
-__device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
-  Seq q = seq_at(a, lane);
-  const int groups = plan_groups(a, q, lane), per = a.c.hkv * a.rtiles;
-  int base = 0;
-  for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
-    if (b0) q = seq_at(a, b0 + lane);
-    const int np = q.r.count > 0 ? pieces_of(q.groups, groups) : 0;
-    const int s = wave_scan(np * per), all = __builtin_amdgcn_readlane(s, 63);
-    if (id < base + all) {
-      const int l = __builtin_ctzll(__ballot(id < base + s));
-      it.b = b0 + l;
-      it.npieces = __builtin_amdgcn_readlane(np, l);
-      it.first = __builtin_amdgcn_readlane(q.r.first, l);
-      it.t = __builtin_amdgcn_readlane(q.r.count, l);
-      it.len = __builtin_amdgcn_readlane(q.len, l);
-      it.slot0 = base + __builtin_amdgcn_readlane(s, l) - it.npieces * per;
-      const int x = id - it.slot0;  // piece-major: all heads' row tiles of a piece adjacent
-      it.piece = x / per;
-      const int y = x - it.piece * per;
-      it.rt = y / a.c.hkv;
-      it.g = y - it.rt * a.c.hkv;
-      return true;
-    }
-    base += all;
-  }
-  return false;
 }
 
 // ---- the end of a piece ---------------------------------------------------------------------------
@@ -529,9 +443,10 @@ __device__ __forceinline__ void join_waves(const DraftArgs &a, const Item &it, c
 }
 
 // NQ: 16-row tiles of Q per wave; W: waves (8 only where every item is one piece).
-template <bool F32, int D, int NQ, bool SEL, int W = kWaves>
+template <bool F32, int D, int NQ, int WHAT, int W = kWaves>
 __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1)) ? 1 : 2) void draft_kernel(const DraftArgs a) {
   using T = Tile<F32, D>;
+  constexpr bool SEL = WHAT == W_SELECT, CROSS = WHAT == W_CROSS;
   constexpr int KC = T::KC, DT = T::DT, E = F32 ? 4 : 2, QP = F32 ? 2 : 1;
   __shared__ float so[W * 16 * NQ * kLd<D>], sml[W * 16 * NQ * 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -546,7 +461,7 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
     it.npieces = a.pieces;
     it.b = -1;
     for (int b0 = 0; b0 < a.c.nseq && it.b < 0; b0 += 64) {
-      const Seq q = seq_at(a, b0 + lane);
+      const Seq q = seq_at<WHAT>(a, b0 + lane);
       const unsigned long long hit = __ballot(r >= q.r.first && r < q.r.first + q.r.count);
       if (hit) {
         const int l = __builtin_ctzll(hit);
@@ -558,9 +473,10 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
     }
     if (it.b < 0) return;  // a row of no sequence
     row_t0 = r - it.first;
+    it.per = 1;
     it.slot0 = ((r * a.rtiles + it.rt) * a.c.hkv + it.g) * a.pieces;
   } else {
-    if (!find_item(a, blockIdx.x, lane, it)) return;
+    if (!find_item<WHAT>(a, blockIdx.x, lane, it)) return;
   }
   it = uniform(it);
   row_t0 = uniform(row_t0);
@@ -570,7 +486,7 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
   const int r0 = it.rt * 16 * NQ;
   if (r0 >= nr) return;
   // the walk: rows [0, total), or the selected blocks' rows and then those behind the last complete block
-  const int total = walk_len(a, len, it.t), full = len >> 6;
+  const int total = walk_len<WHAT>(a, len, it.t), full = len >> 6;
   const int nblk = SEL ? (a.nsel < full ? a.nsel : full) : 0;
   const int steps = SEL ? nblk * 64 + (total - full * 64) : total;
   const int ngroups = (steps + kGroup - 1) / kGroup;
@@ -620,14 +536,21 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
     return tile_at(c, it.b, it.g, j, total);
   };
 
-  const RowsOf ro{&a.q, len, total, it.t, it.first};
+  const RowsOf ro{&a.q, len, total, it.t, it.first, it.b};
   bool special = false;  // an edge held infinities or NaN
   auto scores = [&](const T &kv, f32x4 (&sc)[2][NQ]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) score_rows<F32, D, NQ>(kv.k[u], q, sc[u]);
   };
   auto use = [&](T &kv, int j, f32x4 (&sc)[2][NQ]) {
-    if (j + kTile > len) {
+    if constexpr (CROSS) {
+      const uint32_t see = seen_keys(ro, j);
+      if (see == 0u) return;
+      if (see != ~0u) {
+        hide_scores<NQ>(see, h, sc);
+        hide_values<F32, D>(kv.v, see, h);
+      }
+    } else if (j + kTile > len) {
       mask_scores<NQ>(ro, tq, j, h, sc);
       special = clean_values<F32, D>(kv.v) || special;
     }
@@ -700,14 +623,14 @@ __global__ __launch_bounds__(64 * W, W > kWaves || (D == 128 && (F32 || NQ > 1))
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
     store_wave<D, false>(&so[(wave * NQ + n) * 16 * kLd<D>], &sml[(wave * NQ + n) * 32], m, h, mx[n], sum[n], oacc[n]);
-  if (special)
+  if (!CROSS && special)
     for (s = g0 * kGroup + wave * kTile; s < s_end; s += W * kTile) {
       const int j = uniform(row_of(s));
       if (j + kTile > len && tile_at(c, it.b, it.g, j, total).ok)
         add_special<F32, D, SEL>(c, it, ro, j, &so[wave * NQ * 16 * kLd<D>], 16 * NQ, r0, nr, G, row_t0, lane);
     }
   __syncthreads();
-  const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
+  const int slot = SEL ? it.slot0 + it.piece : it.slot0 + it.piece * it.per + it.rt * c.hkv + it.g;
   join_waves<D, W, 64 * W, SEL>(a, it, so, sml, 16 * NQ, r0, nr, G, row_t0, slot);
 }
 
@@ -732,8 +655,9 @@ __device__ __forceinline__ int chunk_xor(int r) {
 }
 
 // F32: values are split into their bf16 parts as they enter LDS, a plane each.
-template <bool F32, int D, int KW, int NW>
+template <bool F32, int D, int KW, int NW, int WHAT>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(const DraftArgs a) {
+  constexpr bool CROSS = WHAT == W_CROSS;
   constexpr int NT = KW == 2 || F32 ? 1 : 2;                 // tiles of 32 rows per wave and stage
   constexpr int NQ = 2, RW = NW / KW, SR = 32 * NT * KW;  // SR: rows of a stage
   static_assert(64 % SR == 0, "a stage lies in one page");
@@ -747,13 +671,13 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, h = lane >> 4, wk = wave % KW, wr = wave / KW;
   Item it;
-  if (!find_item(a, blockIdx.x, lane, it)) return;
+  if (!find_item<WHAT>(a, blockIdx.x, lane, it)) return;
   it = uniform(it);
   const CacheView &c = a.c;
   const int len = it.len;
   const int G = a.q.hq / c.hkv, nr = G * it.t, r0 = it.rt * 32 * RW;
   if (r0 >= nr) return;
-  const int total = walk_len(a, len, it.t), ngroups = (total + kGroup - 1) / kGroup;
+  const int total = walk_len<WHAT>(a, len, it.t), ngroups = (total + kGroup - 1) / kGroup;
   const int g0 = (int)((long long)ngroups * it.piece / it.npieces), g1 = (int)((long long)ngroups * (it.piece + 1) / it.npieces);
   const int j0 = g0 * kGroup, j1 = g1 * kGroup < total ? g1 * kGroup : total;
   const int nst = (j1 - j0 + SR - 1) / SR;
@@ -790,6 +714,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   u32x4 st[NI];
   bool okst;
   int entry;
+  [[maybe_unused]] uint64_t seest = 0;  // W_CROSS: the rows of the stage in st that are seen, as bits
   auto first_row = [&](int stage) {  // (behind the end: the last row)
     const int j = j0 + stage * SR;
     return __builtin_amdgcn_readfirstlane(j < total ? j : total - 1);
@@ -805,11 +730,18 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
     off[i] = (w * RPI + lr) * (int)(isv ? c.sv_t : c.sk_t) + 16 * lc;
   }
   const char *kg = c.k + it.g * c.sk_h, *vg = c.v + it.g * c.sv_h;
+  const RowsOf ro{&a.q, len, total, it.t, it.first, it.b};
   auto fetch = [&](int stage, u32x4 (&x)[NI], bool &ok) {
     const int j = first_row(stage), id = checked_page(c, entry), in = j - page_of(c, j) * c.page;
     ok = id >= 0;
     const char *kb = kg + (ok ? id * c.sk_p + in * c.sk_t : 0), *vb = vg + (ok ? id * c.sv_p + in * c.sv_t : 0);
     const int most = ok ? total - 1 - j : 0;  // last row that may be read
+    if constexpr (CROSS) {
+      const int js = j0 + stage * SR;
+      seest = seen_keys(ro, js);
+      if constexpr (SR == 64) seest |= (uint64_t)seen_keys(ro, js + 32) << 32;
+      ok = ok && seest != 0;
+    }
     look(stage + 1);
     if (most >= SR - 1) {
 #pragma unroll
@@ -848,6 +780,8 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
             odd = 1;
           }
         }
+      if constexpr (CROSS)
+        if (isv && !(seest >> r & 1)) x[i] = u32x4{0u, 0u, 0u, 0u};  // (counts for nothing whatever it holds)
       if constexpr (F32) {
         const f32x4 f = __builtin_bit_cast(f32x4, x[i]);
         uint32_t h0, l0, h1, l1;
@@ -861,7 +795,6 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
       }
     }
   };
-  const RowsOf ro{&a.q, len, total, it.t, it.first};
   // S^T of 16 rows from row r0 of the stage
   auto scores = [&](const char *buf, int r0, f32x4 (&s)[NQ]) {
     const char *row = buf + (r0 + m) * (D * 2);
@@ -911,13 +844,17 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   };
 
   // stages of cached rows alone, which every row sees (and none what has no page)
-  const int nplain = len < j1 ? (len > j0 ? (len - j0) / SR : 0) : (j1 - j0) / SR, wr0 = wk * NT * 32;
-  look(0);
-  fetch(0, st, okst);
+  // (W_CROSS: all stages, their hidden rows cleared)
+  const int nplain = CROSS ? nst : len < j1 ? (len > j0 ? (len - j0) / SR : 0) : (j1 - j0) / SR, wr0 = wk * NT * 32;
+  if (!CROSS || nst > 0) {
+    look(0);
+    fetch(0, st, okst);
+  }
   for (int s = 0; s < nplain; ++s) {
     char *buf = lds + (s & 1) * kBuf;
     put(std::false_type{}, buf, st);
     const bool ok = okst;
+    [[maybe_unused]] const uint64_t see = seest;
     fetch(s + 1, st, okst);  // (behind the last: its last row)
     stage_barrier();
     if (idle || !ok) continue;
@@ -927,6 +864,19 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
 #pragma unroll
     for (int u = 0; u < 2 * NT; ++u) scores(buf, wr0 + 16 * u, sc[u]);
     __builtin_amdgcn_s_setprio(0);
+    if constexpr (CROSS)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const uint32_t w = (uint32_t)(see >> (wr0 + 32 * i));
+        if (w != ~0u) {
+          f32x4 t[2][NQ];
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) t[0][n] = sc[2 * i][n], t[1][n] = sc[2 * i + 1][n];
+          hide_scores<NQ>(w, h, t);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) sc[2 * i][n] = t[0][n], sc[2 * i + 1][n] = t[1][n];
+        }
+      }
     weigh<D, NQ, NT>(sc, a.q.c, mx, sum, oacc, pb);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -956,7 +906,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
   }
   __syncthreads();
   const bool special = odd;
-  const int slot = it.slot0 + it.piece * (c.hkv * a.rtiles) + it.rt * c.hkv + it.g;
+  const int slot = it.slot0 + it.piece * it.per + it.rt * c.hkv + it.g;
   if (KW == 1 && !special) {
     // a wave's rows are its own: lane (m, h) writes dimensions 16t + 4h .. + 3 of row m
 #pragma unroll
@@ -1006,8 +956,9 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void draft_wide_kernel(co
 // Joins the pieces of every item: WV waves per new row and head (all four of a workgroup, or one where there are so
 // many rows that the chip is full of them).  Every wave reads all maxima and sums (a lane per piece), so that each
 // knows its weights before its share of the O parts arrives; LDS joins the waves.
-template <int D, bool SEL, int WV>
+template <int D, int WHAT, int WV>
 __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
+  constexpr bool SEL = WHAT == W_SELECT;
   __shared__ float so[kWaves][D];
   constexpr int PL = D / 64;  // dimensions per lane
   typedef float fv __attribute__((ext_vector_type(PL)));
@@ -1015,22 +966,21 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
   const CacheView &c = a.c;
   const int G = a.q.hq / c.hkv, r = blockIdx.x, hh = WV == 1 ? blockIdx.y * kWaves + wv : blockIdx.y, g = hh / G;
   if (hh >= a.q.hq) return;
-  int slot, np, stride, row;
+  int slot, np, stride = 1, row;
   bool mine = true;
   if constexpr (SEL) {
     const int rr = hh - g * G, rt = rr / a.trows;
     row = rr - rt * a.trows;
     slot = ((r * a.rtiles + rt) * c.hkv + g) * a.pieces;
     np = a.pieces;
-    stride = 1;
   } else {
-    Seq q = seq_at(a, lane);
-    const int groups = plan_groups(a, q, lane), per = c.hkv * a.rtiles;
+    Seq q = seq_at<WHAT>(a, lane);
+    const int groups = plan_groups<WHAT>(a, q, lane);
     int base = 0, b = -1, first = 0;
     np = 0;
     for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
-      if (b0) q = seq_at(a, b0 + lane);
-      const int k = q.r.count > 0 ? pieces_of(q.groups, groups) : 0;
+      if (b0) q = seq_at<WHAT>(a, b0 + lane);
+      const int k = q.r.count > 0 ? pieces_of(q.groups, groups) : 0, per = items_of<WHAT>(a, q);
       const int s = wave_scan(k * per);
       const unsigned long long hit = __ballot(r >= q.r.first && r < q.r.first + q.r.count);
       if (hit) {
@@ -1038,7 +988,8 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
         b = b0 + l;
         first = __builtin_amdgcn_readlane(q.r.first, l);
         np = __builtin_amdgcn_readlane(k, l);
-        base += __builtin_amdgcn_readlane(s, l) - np * per;
+        stride = WHAT == W_CROSS ? __builtin_amdgcn_readlane(per, l) : per;
+        base += __builtin_amdgcn_readlane(s, l) - np * stride;
       } else {
         base += __builtin_amdgcn_readlane(s, 63);
       }
@@ -1047,9 +998,10 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
     const int rr = (r - first) * G + hh - g * G, rt = rr / a.trows;
     row = rr - rt * a.trows;
     slot = base + rt * c.hkv + g;
-    stride = per;
+    // (sequences that share rows, which start does not allow, may have more pieces than there are workgroups)
+    if (WHAT == W_CROSS && slot + (np - 1) * stride >= a.grid) return;
   }
-  slot = uniform(slot), np = uniform(np), row = uniform(row);
+  slot = uniform(slot), np = uniform(np), row = uniform(row), stride = uniform(stride);
   const float *po = a.po + ((int64_t)slot * a.trows + row) * D + lane * PL, *pml = a.pml + ((int64_t)slot * a.trows + row) * 2;
   const int64_t step = (int64_t)stride * a.trows;
   float M = -__builtin_inff(), z = 0.f;
@@ -1545,10 +1497,11 @@ struct DraftShape {
 constexpr int kShort = 256;
 constexpr int kMaxGrid = 1 << 23;  // workgroups of up to 512 threads, of which a launch has fewer than 2^32
 
-DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
+DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int what) {
   DraftShape s{};
   s.waves = kWaves;
-  const int G = q.hq / c.hkv, rows = nsel ? G : G * q.max_rows;
+  const int G = q.hq / c.hkv, most_rows = what == W_CROSS && q.nrows < q.max_rows ? q.nrows : q.max_rows;
+  const int rows = nsel ? G : G * most_rows;
   s.trows = tile_rows(f32, d, nsel > 0, rows);
   s.rtiles = (rows + s.trows - 1) / s.trows;
   // workgroups that the chip holds at once: with stages three per CU (d = 64: 16 sequences of 16000 rows, 256 rows of Q,
@@ -1564,7 +1517,12 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
     s.grid = (int)(items * s.pieces);
     return s;
   }
-  const int64_t items = (int64_t)c.nseq * c.hkv * s.rtiles, most = items * ((c.cap + kGroup - 1) / kGroup);
+  int64_t tiles = (int64_t)c.nseq * s.rtiles;
+  if (what == W_CROSS) {  // a sequence has the row tiles of its own rows, less than one that is not full
+    const int64_t own = (int64_t)G * q.nrows / s.trows + c.nseq;
+    tiles = tiles < own ? tiles : own;
+  }
+  const int64_t items = tiles * c.hkv, most = items * ((c.cap + kGroup - 1) / kGroup);
   // A short cache stays in one piece and needs no joining launch (4 us): up to kShort rows in four waves, twice that in
   // eight where a CU holds two waves per SIMD (8 heads over 500 rows: one sequence 12.6 -> 10.0 us, 64 of them 36.7 ->
   // 27.5).  Longer ones gain from pieces (one token over 1001 rows: 14.7 us in one piece, 12.3 in several): few items
@@ -1572,7 +1530,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   if (c.cap <= (two && !wide ? 2 * kShort : kShort)) {
     s.waves = c.cap > kShort ? 8 : kWaves;
     s.slots = 0;
-    s.grid = (int)items;
+    s.grid = items < kMaxGrid ? (int)items : kMaxGrid;
     return s;
   }
   // A piece of many rows writes, and the join reads, as much as 2 trows rows of fp32: where the items alone fill
@@ -1583,7 +1541,8 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   s.least = items <= resident / 2 ? 1 : s.trows >= 128 ? 16 : s.trows / 16;
   if (c.cap <= s.least * kGroup) s.slots = 0;  // no sequence is long enough for two pieces
   const int64_t grid = items + s.slots;
-  s.grid = (int)(grid < most && s.slots ? grid : s.slots ? most : items);
+  const int64_t n = grid < most && s.slots ? grid : s.slots ? most : items;
+  s.grid = n < kMaxGrid ? (int)n : kMaxGrid;  // (refused)
   return s;
 }
 
@@ -1598,12 +1557,12 @@ void by_tiles(bool f32, int d, int trows, F f) {
   f32 ? with_t(std::true_type{}) : with_t(std::false_type{});
 }
 
-template <bool F32, int D>
+template <bool F32, int D, int WHAT>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
-  if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4><<<s.grid, 256, 0, st>>>(a);
+  if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
-    if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4><<<s.grid, 256, 0, st>>>(a);
-    if constexpr (D == 128) draft_wide_kernel<F32, D, 1, 8><<<s.grid, 512, 0, st>>>(a);
+    if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
+    if constexpr (D == 128) draft_wide_kernel<F32, D, 1, 8, WHAT><<<s.grid, 512, 0, st>>>(a);
   }
 }
 
@@ -1616,6 +1575,7 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   a.slots = s.slots;
   a.least = s.least;
   a.pieces = s.pieces;
+  a.grid = s.grid;
   // (a single piece is the result itself; its call asks for one line all the same, so that no caller does without one)
   const size_t rows = s.slots > 0 || s.pieces > 1 ? (size_t)s.grid * s.trows : 0;
   a.po = ar.take<float>(rows ? rows * d : 64);
@@ -1634,30 +1594,33 @@ SelectArgs select_parts(Arena &ar, const CacheView &c, const DraftView &q, int n
   return s;
 }
 
-template <bool SEL>
+template <int WHAT>
 rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipStream_t st) {
-  if (s.trows > 32)
-    f32 ? (d == 128 ? wide_launch<true, 128>(a, s, st) : wide_launch<true, 64>(a, s, st))
-        : (d == 128 ? wide_launch<false, 128>(a, s, st) : wide_launch<false, 64>(a, s, st));
-  else
+  constexpr bool SEL = WHAT == W_SELECT;
+  if constexpr (!SEL) {
+    if (s.trows > 32)
+      f32 ? (d == 128 ? wide_launch<true, 128, WHAT>(a, s, st) : wide_launch<true, 64, WHAT>(a, s, st))
+          : (d == 128 ? wide_launch<false, 128, WHAT>(a, s, st) : wide_launch<false, 64, WHAT>(a, s, st));
+  }
+  if (SEL || s.trows <= 32)
     by_tiles(f32, d, s.trows, [&](auto x, auto dd, auto nn) {
       constexpr bool F = decltype(x)::value;
       constexpr int D = decltype(dd)::value, NQ = decltype(nn)::value;
       if constexpr (SEL)
-        draft_kernel<F, D, NQ, true><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
+        draft_kernel<F, D, NQ, WHAT><<<dim3(a.q.nrows * s.pieces, a.c.hkv * s.rtiles), 256, 0, st>>>(a);
       else {
         if constexpr (D == 64 || (!F && NQ == 1))
-          if (s.waves > kWaves) return draft_kernel<F, D, NQ, false, 8><<<s.grid, 512, 0, st>>>(a);
-        draft_kernel<F, D, NQ, false><<<s.grid, 256, 0, st>>>(a);
+          if (s.waves > kWaves) return draft_kernel<F, D, NQ, WHAT, 8><<<s.grid, 512, 0, st>>>(a);
+        draft_kernel<F, D, NQ, WHAT><<<s.grid, 256, 0, st>>>(a);
       }
     });
   if (SEL ? s.pieces > 1 : s.slots > 0) {
     if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
       const dim3 grid(a.q.nrows, (a.q.hq + kWaves - 1) / kWaves);
-      d == 128 ? draft_join_kernel<128, SEL, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL, 1><<<grid, 256, 0, st>>>(a);
+      d == 128 ? draft_join_kernel<128, WHAT, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, WHAT, 1><<<grid, 256, 0, st>>>(a);
     } else {
       const dim3 grid(a.q.nrows, a.q.hq);
-      d == 128 ? draft_join_kernel<128, SEL, kWaves><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, SEL, kWaves><<<grid, 256, 0, st>>>(a);
+      d == 128 ? draft_join_kernel<128, WHAT, kWaves><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, WHAT, kWaves><<<grid, 256, 0, st>>>(a);
     }
   }
   RS_HIP(hipGetLastError());
@@ -1666,35 +1629,36 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
 
 }  // namespace
 
-size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel) {
+size_t draft_ws_bytes(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int what) {
   Arena ar(nullptr, 0);
-  const DraftShape s = draft_shape(c, q, f32, d, nsel);
+  const DraftShape s = draft_shape(c, q, f32, d, nsel, what);
   if (!nsel && s.grid >= kMaxGrid) return 0;
   if (nsel) select_parts(ar, c, q, nsel);
   draft_parts(ar, c, q, s, d);
   return ar.off + 256;
 }
 
-rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, void *o, int64_t so_t, int64_t so_h, float *lse,
-                       void *ws, size_t ws_bytes, hipStream_t st) {
-  const DraftShape s = draft_shape(c, q, f32, d, 0);
-  if (s.grid >= kMaxGrid) return fail(RS_ERR_UNSUPPORTED, "draft: at most 2^23 - 1 workgroups (nseq x hkv x row tiles)");
+rs_status draft_launch(const CacheView &c, const DraftView &q, bool f32, int d, int what, void *o, int64_t so_t, int64_t so_h,
+                       float *lse, void *ws, size_t ws_bytes, hipStream_t st) {
+  const std::string name = what == W_CROSS ? "cross" : "draft";
+  const DraftShape s = draft_shape(c, q, f32, d, 0, what);
+  if (s.grid >= kMaxGrid) return fail(RS_ERR_UNSUPPORTED, name + ": at most 2^23 - 1 workgroups (nseq x hkv x row tiles)");
   Arena ar(ws, ws_bytes);
   DraftArgs a = draft_parts(ar, c, q, s, d);
   if (!ws || !ar.ok())
-    return fail(RS_ERR_WORKSPACE, "draft attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, 0)));
+    return fail(RS_ERR_WORKSPACE, name + " attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, 0, what)));
   a.o = (char *)o, a.so_t = so_t, a.so_h = so_h, a.lse = lse;
-  return attend<false>(a, s, f32, d, st);
+  return what == W_CROSS ? attend<W_CROSS>(a, s, f32, d, st) : attend<W_ALL>(a, s, f32, d, st);
 }
 
 rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int nsink, int nlocal, void *o,
                         int64_t so_t, int64_t so_h, float *lse, int32_t *blocks, void *ws, size_t ws_bytes, hipStream_t st) {
-  const DraftShape s = draft_shape(c, q, f32, d, nsel);
+  const DraftShape s = draft_shape(c, q, f32, d, nsel, W_SELECT);
   Arena ar(ws, ws_bytes);
   SelectArgs sel = select_parts(ar, c, q, nsel);
   DraftArgs a = draft_parts(ar, c, q, s, d);
   if (!ws || !ar.ok())
-    return fail(RS_ERR_WORKSPACE, "selected attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, nsel)));
+    return fail(RS_ERR_WORKSPACE, "selected attention workspace too small: need " + std::to_string(draft_ws_bytes(c, q, f32, d, nsel, W_SELECT)));
   if (blocks) sel.list = blocks;
   sel.nsink = nsink, sel.nlocal = nlocal;
   a.o = (char *)o, a.so_t = so_t, a.so_h = so_h, a.lse = lse;
@@ -1706,7 +1670,7 @@ rs_status select_launch(const CacheView &c, const DraftView &q, bool f32, int d,
   }
   const dim3 rows(q.nrows, c.hkv);
   select_kernel<<<rows, kSelThreads, 0, st>>>(sel);
-  return attend<true>(a, s, f32, d, st);
+  return attend<W_SELECT>(a, s, f32, d, st);
 }
 
 rs_status weights_launch(const CacheView &c, const DraftView &q, bool f32, int d, const float *lse, const float *row_w,

@@ -1,0 +1,264 @@
+"""Cross attention over encoder states in a cache (rs_cross_attn) against the fp64 oracle: single tokens and prompts, lengths
+from none to several pieces, key masks that leave nothing, pages in any order and missing, strides, hidden infinities and NaN,
+streams, graphs, far pages."""
+import numpy as np
+import pytest
+
+from paper_2608_29058_amd import _rs
+from cross_helpers import Encoded
+from decode_helpers import check_rows
+
+pytestmark = pytest.mark.gpu
+
+LENS = [0, 1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 1000]
+HEADS = [
+    (8, 2, 128, "bf16", 64, "head"),
+    (4, 4, 64, "bf16", 128, "token"),
+    (7, 1, 128, "f32", 64, "token"),
+    (20, 4, 64, "f32", 192, "head"),
+    (40, 2, 128, "bf16", 64, "head"),    # 20 rows: two row tiles of a wave
+    (48, 1, 64, "bf16", 256, "head"),    # 48 rows
+    (48, 1, 128, "f32", 64, "head"),
+    (160, 1, 128, "bf16", 64, "token"),  # 160 rows
+]
+
+
+def untouched(s, o, l):
+    own = np.zeros(s.nrows, bool)
+    for f, t in s.rows:
+        own[f:f + t] = True
+    assert (o.float().cpu().numpy()[~own] == -7.0).all() and (l.cpu().numpy()[:, ~own] == -7.0).all()
+
+
+@pytest.mark.parametrize("hide", [None, 0.4, 0.97])
+@pytest.mark.parametrize("hq,hkv,d,dtype,page,layout", HEADS)
+def test_one_token_per_sequence(hq, hkv, d, dtype, page, layout, hide):
+    s = Encoded(hq * d, LENS, [1] * len(LENS), hq=hq, hkv=hkv, d=d, dtype=dtype, page=page, layout=layout, spread=2.0, hide=hide,
+                all_hidden=(4, 11))
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    if hide is not None:
+        assert (o[[0, 4, 11]] == 0).all() and (l[:, [0, 4, 11]] == -np.inf).all()
+
+
+@pytest.mark.parametrize("hide", [None, 0.3])
+@pytest.mark.parametrize("hq,hkv,d,dtype,lens,rows", [
+    (8, 2, 128, "bf16", [0, 5, 200, 64], [3, 1, 4, 20]),
+    (8, 2, 64, "bf16", [65, 37, 127], [33, 64, 1]),
+    (4, 4, 128, "bf16", [90, 31, 129], [127, 128, 129]),
+    (28, 4, 64, "f32", [0, 61, 130], [13, 5, 13]),
+    (4, 4, 128, "f32", [1, 100], [7, 70]),
+    (2, 2, 128, "bf16", [700, 64, 1], [300, 0, 5]),        # a sequence without rows
+    (6, 2, 64, "bf16", [1500, 0, 191], [200, 65, 43]),
+    (5, 1, 128, "f32", [2100, 31], [64, 52]),
+    (4, 1, 128, "bf16", [2500, 130], [40, 90]),
+    (1, 1, 64, "bf16", [333], [1000]),
+    (2, 1, 64, "f32", [500, 20], [257, 3]),
+])
+def test_prompts(hq, hkv, d, dtype, lens, rows, hide):
+    s = Encoded(sum(lens) + hq, lens, rows, hq=hq, hkv=hkv, d=d, dtype=dtype, extra=3, hide=hide, all_hidden=(1,), spread=1.5)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    untouched(s, o, l)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,lens,rows", [
+    (2, 1, 128, "bf16", [20000], [1]), (2, 1, 128, "bf16", [20000, 3], [40, 1]), (1, 1, 64, "bf16", [16385, 9000], [130, 2]),
+    (1, 1, 64, "f32", [12000], [20]), (2, 2, 128, "f32", [9000, 0], [33, 70]),
+])
+def test_long_states_in_pieces(hq, hkv, d, dtype, lens, rows):
+    s = Encoded(3, lens, rows, hq=hq, hkv=hkv, d=d, dtype=dtype, page=256, hide=0.2)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    again, l2 = s.run()
+    import torch
+    assert torch.equal(o, again) and torch.equal(l, l2)  # to the bit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 1, 1], [10, 60, 3], [200, 5, 130]])
+def test_hidden_states_count_for_nothing_whatever_they_hold(rows, dtype):
+    """Infinities and NaN behind the end, under the mask and in pages that no table entry names change no bit."""
+    import torch
+    s = Encoded(5, [70, 129, 200], rows, hq=4, hkv=2, d=128, dtype=dtype, hide=0.3, all_hidden=(2,), max_pages=5)
+    o, l = s.run()
+    see = np.unpackbits(s.kmask.view(np.uint8), axis=1, bitorder="little").astype(bool)
+    live = np.zeros(s.k.shape[:1] + s.k.shape[2:3], bool)
+    for b, n in enumerate(s.lens):
+        for j in range(int(n)):
+            if see[b, j]:
+                live[s.table[b, j // 64], j % 64] = True
+    for bad in (np.nan, np.inf, -np.inf):
+        for x in (s.k, s.v):
+            x[:] = np.where(live[:, None, :, None], x, bad)
+        s.upload()
+        o2, l2 = s.run()
+        assert torch.equal(o, o2) and torch.equal(l, l2)
+    assert (o[s.start[2]:] == 0).all() and torch.isneginf(l[:, s.start[2]:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1], [50], [300]])
+def test_seen_infinities_and_nan_are_seen(rows, dtype):
+    s = Encoded(6, [150], rows, hq=2, hkv=1, d=64, dtype=dtype, spread=0.2)
+    s.v[s.table[0, 1], 0, 9, 3] = np.inf      # a weight is 1 / 150 or so here
+    s.v[s.table[0, 2], 0, 20, 7] = -np.inf
+    s.v[s.table[0, 0], 0, 5, 11] = np.nan
+    s.upload()
+    o, l = s.run()
+    got = o.float().cpu().numpy()
+    assert (got[..., 3] == np.inf).all() and (got[..., 7] == -np.inf).all() and np.isnan(got[..., 11]).all()
+    rest = [i for i in range(64) if i not in (3, 7, 11)]
+    assert np.isfinite(got[..., rest]).all() and np.isfinite(l.cpu().numpy()).all()
+    s.k[s.table[0, 1], 0, 4] = np.nan          # a NaN logit in every row
+    s.upload()
+    o, l = s.run()
+    assert np.isnan(o.float().cpu().numpy()).all() and np.isnan(l.cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("rows", [[1, 2], [40, 7], [150, 300]])
+def test_pages_that_the_table_does_not_name(rows):
+    s = Encoded(7, [400, 190], rows, hq=4, hkv=2, d=64, page=64, hide=0.1)
+    s.table[0, 1], s.table[0, 4], s.table[1, :] = -1, s.k.shape[0] + 5, [2 ** 31 - 1] + [-5] * (s.table.shape[1] - 1)
+    s.upload()
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    assert (o[s.start[1]:] == 0).all()
+
+
+@pytest.mark.parametrize("rows,lens", [([1, 1], [40, 99]), ([70, 130], [99, 1])])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_page_of_an_odd_size_per_sequence_and_strides(rows, lens, dtype):
+    """Pages of 99 rows (one each), queries and outputs inside larger tensors."""
+    import torch
+    s = Encoded(8, lens, rows, hq=6, hkv=2, d=128, dtype=dtype, page=99, hide=0.2)
+    big = torch.full((s.nrows, s.hq + 3, 128 + 16), 9.0, dtype=s.td, device="cuda")
+    big[:, 1:1 + s.hq, :128] = s.dq
+    s.cross = _rs.Cross(big[:, 1:1 + s.hq, :128], max_rows=s.max_rows, start=s.dstart, kmask=s.dmask)
+    frame = torch.full((s.hq + 2, s.nrows, 192), -7.0, dtype=torch.bfloat16, device="cuda")  # heads outside
+    o = frame[1:-1, :, 32:160].transpose(0, 1)
+    c = s.cache()
+    l = torch.empty(s.hq, s.nrows, device="cuda")
+    _rs.rs_cross_attn(c, s.cross, o, l, _rs.workspace(_rs.rs_cross_attn_workspace_size(c, s.cross)))
+    check_rows(s, s.oracle(), o, l)
+    frame[1:-1, :, 32:160] = -7.0
+    assert (frame == -7.0).all()
+
+
+def test_without_starts_and_without_lse():
+    import torch
+    s = Encoded(9, [100, 300, 0], [4, 4, 4], hq=4, hkv=2, start=False, max_rows=4)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    o2, l2 = s.run(lse=False)
+    assert torch.equal(o, o2) and (l2 == -7.0).all()
+    # a looser bound of the rows changes nothing of what they are
+    s = Encoded(9, [100, 300, 0], [4, 1, 2], hq=4, hkv=2)
+    o, l = s.run()
+    s.cross = _rs.Cross(s.dq, max_rows=500, start=s.dstart)
+    s.max_rows = 500
+    o2, l2 = s.run()
+    check_rows(s, s.oracle(), o2, l2)
+
+
+def test_the_scale_and_equal_states():
+    s = Encoded(10, [77, 64], [3, 140], hq=2, hkv=1, scale=0.3)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    s.k[:] = s.k[0, 0, 0]
+    s.upload()
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+
+
+def test_absurd_starts_and_lengths_stay_in_bounds():
+    import torch
+    s = Encoded(11, [200, 90], [6, 6], hq=4, hkv=2)
+    for start, lens in (([5, 2, 90], [3, 1]), ([-4, 3, 4], [-9, 1 << 30]), ([0, 12, 0], [100, 5]), ([0, 1 << 30, -1], [100, 5])):
+        s.dlen.copy_(torch.tensor(lens))
+        s.dstart.copy_(torch.tensor(start))
+        s.lens, s.start = np.array(lens, np.int32), np.array(start, np.int32)
+        from oracle import decode as OD
+        s.rows = OD.row_ranges(s.start, 2, s.nrows, s.max_rows)
+        o, l = s.run()
+        check_rows(s, s.oracle(), o, l)
+
+
+def test_many_sequences_of_few_rows():
+    r = np.random.default_rng(0)
+    lens, rows = r.integers(0, 150, 150), r.integers(0, 4, 150)
+    s = Encoded(12, lens, rows, hq=2, hkv=1, d=64, hide=0.2, extra=1)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    untouched(s, o, l)
+
+
+def test_far_pages():
+    """Pages 4 GiB and more into the pool."""
+    import torch
+    hkv, d, page = 8, 128, 256
+    npages = (5 << 30) // (hkv * d * page * 2)
+    k = torch.empty(npages, hkv, page, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    for rows in ([2], [200]):
+        s = Encoded(13, [600], rows, hq=8, hkv=hkv, d=d, page=page)
+        ids = torch.tensor([npages - 1, npages - 7, 3], device="cuda")
+        k[ids], v[ids] = s.dk[s.dtable[0].long()], s.dv[s.dtable[0].long()]
+        c = _rs.KvCache(k, v, s.dlen, table=ids[None].int().contiguous())
+        o, l = s.outputs()
+        _rs.rs_cross_attn(c, s.cross, o, l, _rs.workspace(_rs.rs_cross_attn_workspace_size(c, s.cross)))
+        check_rows(s, s.oracle(), o, l)
+
+
+def test_the_longest_cache():
+    """262144 states, weights all but equal: the mean of V in fp64."""
+    import torch
+    n = 262144
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k = torch.randn(n // 1024, 1, 1024, 64, device="cuda", generator=g, dtype=torch.bfloat16)
+    v = torch.randn(n // 1024, 1, 1024, 64, device="cuda", generator=g, dtype=torch.bfloat16)
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    c = _rs.KvCache(k, v, ln)
+    for rows in (1, 5, 150):
+        q = torch.randn(rows, 2, 64, device="cuda", generator=g, dtype=torch.bfloat16)
+        x = _rs.Cross(q, max_rows=rows)
+        o, l = torch.empty(rows, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(2, rows, device="cuda")
+        _rs.rs_cross_attn(c, x, o, l, _rs.workspace(_rs.rs_cross_attn_workspace_size(c, x)))
+        kk, vv = k.double().reshape(n, 64), v.double().reshape(n, 64)
+        lg = torch.matmul(q.double().reshape(-1, 64), kk.t()) / 8.0
+        p = torch.softmax(lg, 1)
+        want, ab = torch.matmul(p, vv).reshape(rows, 2, 64), torch.matmul(p, vv.abs()).reshape(rows, 2, 64)
+        # half a bf16 step of O and of every weight, the weights' fp32 error (72 steps of 2^-24 of sum |q k| <= 100)
+        assert ((o.double() - want).abs() <= 1.01 * (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2 * 100 * 72 * 2.0 ** -24) * ab)).all()
+        assert ((l.double().t() - torch.logsumexp(lg, 1).reshape(rows, 2)).abs() <= 100 * 72 * 2.0 ** -24 + 2.0 ** -24 * n / 16).all()
+
+
+@pytest.mark.parametrize("rows", [[1, 1, 1, 1], [3, 160, 0, 40]])
+def test_a_replayed_graph_and_another_stream(rows):
+    """The captured call reads lengths, masks and tables as they are at each replay; two graphs, each with its own workspace."""
+    import torch
+    s = Encoded(14, [700, 64, 129, 300], rows, hq=4, hkv=2, d=128, hide=0.3)
+    c = s.cache()
+    o, l = s.outputs()
+    ws = [_rs.workspace(_rs.rs_cross_attn_workspace_size(c, s.cross)) for _ in range(2)]
+    outs = [s.outputs() for _ in range(2)]
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            _rs.rs_cross_attn(c, s.cross, outs[i][0], outs[i][1], ws[i])
+    st = torch.cuda.Stream()
+    for k in range(4):
+        s.dlen.copy_(torch.tensor([700 - 90 * k, 64 * (k > 1), 129 - k, 300]))
+        s.dmask.copy_(s.dmask.roll(1, 1))
+        torch.cuda.synchronize()
+        graphs[k & 1].replay()
+        graphs[1 - (k & 1)].replay()
+        want, wl = s.run()
+        with torch.cuda.stream(st):
+            st.wait_stream(torch.cuda.default_stream())
+            alone, al = s.run()
+        torch.cuda.synchronize()
+        for x, y in (*outs, (alone, al)):
+            assert torch.equal(x, want) and torch.equal(y, wl)
