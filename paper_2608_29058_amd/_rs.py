@@ -553,10 +553,12 @@ def _on_device(fn, device, stream, args):
     """fn(*args, stream) on `stream` (default: the current stream of `device`), launched with `device` current."""
     import torch
     _want(device.type == "cuda", "the tensors must be on a GPU")
+    # (the stream's number without a torch.cuda.Stream around it, 1 us of a call's host time)
+    on = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
     if device.index == torch.cuda.current_device():
-        return _check(fn(*args, _stream(stream)))
+        return _check(fn(*args, on))
     with torch.cuda.device(device):
-        return _check(fn(*args, _stream(stream)))
+        return _check(fn(*args, on))
 
 
 class KvCache:
@@ -648,19 +650,21 @@ def _at(t):
 
 
 def _check_new_rows(cache, k_new, v_new, start):
+    """The number of new rows and the strides of k_new and v_new."""
     import torch
-    _want(k_new.dim() == 3 and k_new.shape == v_new.shape and k_new.shape[1] == cache.hkv and k_new.shape[2] == cache.d
-          and k_new.dtype is cache.dtype is v_new.dtype and (k_new.stride(2) == v_new.stride(2) == 1 or not k_new.numel())
-          and k_new.device == cache.device == v_new.device, "k_new and v_new must be [nrows, hkv, d] like the cache")
-    _want(_like(start, torch.int32, (cache.nseq + 1,), cache.device), "start must be contiguous int32 [nseq + 1]")
+    shape, ks, vs, on = k_new.shape, k_new.stride(), v_new.stride(), cache.k.get_device()
+    _want(len(shape) == 3 and v_new.shape == shape and shape[1] == cache.hkv and shape[2] == cache.d
+          and k_new.dtype is cache.dtype is v_new.dtype and (ks[2] == vs[2] == 1 or not k_new.numel())
+          and k_new.get_device() == on == v_new.get_device(), "k_new and v_new must be [nrows, hkv, d] like the cache")
+    _want(start is None or _like(start, torch.int32, (cache.nseq + 1,), cache.device), "start must be contiguous int32 [nseq + 1]")
+    return shape[0], ks, vs
 
 
 def rs_cache_append(cache, k_new, v_new, max_rows=1, start=None, stream=None):
     """k_new, v_new: [nrows, hkv, d] of the cache's dtype (last dim contiguous)."""
-    _check_new_rows(cache, k_new, v_new, start)
+    n, ks, vs = _check_new_rows(cache, k_new, v_new, start)
     return _on_device(lib().rs_cache_append, cache.device, stream,
-                      (cache.ref, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), v_new.stride(0),
-                       v_new.stride(1), _at(start), k_new.shape[0], max_rows))
+                      (cache.ref, k_new.data_ptr(), v_new.data_ptr(), ks[0], ks[1], vs[0], vs[1], _at(start), n, max_rows))
 
 
 def rs_cache_commit(cache, naccept, max_new, path=None, stream=None):
@@ -737,16 +741,17 @@ class Rope:
         self.ref = C.byref(self.c)
 
 
-def _row_strides(t):
-    """Strides of [rows, heads, d] in elements; a dimension of one entry is given a row's length."""
-    return [t.stride(i) if t.shape[i] > 1 else t.shape[2] for i in (0, 1)]
+def _row_strides(shape, stride):
+    """Strides (row, head) of [rows, heads, d] in elements; a dimension of one entry is given a row's length."""
+    return stride[0] if shape[0] > 1 else shape[2], stride[1] if shape[1] > 1 else shape[2]
 
 
 def _rope_part(x, y):
-    _want(x.dim() == 3 and y.shape == x.shape and y.dtype is x.dtype and y.device == x.device
-          and (x.stride(2) == y.stride(2) == 1 or not x.numel()), "x and y must be [n, heads, d] alike, with a contiguous last dimension")
-    (xt, xh), (yt, yh) = _row_strides(x), _row_strides(y)
-    return RsRopePart(x=x.data_ptr(), y=y.data_ptr(), heads=x.shape[1], sx_t=xt, sx_h=xh, sy_t=yt, sy_h=yh)
+    shape, xs = x.shape, x.stride()
+    ys = xs if y is x else y.stride()
+    _want(len(shape) == 3 and (y is x or (y.shape == shape and y.dtype is x.dtype and y.get_device() == x.get_device()))
+          and (xs[2] == ys[2] == 1 or not x.numel()), "x and y must be [n, heads, d] alike, with a contiguous last dimension")
+    return RsRopePart(x.data_ptr(), y.data_ptr(), shape[1], 0, *_row_strides(shape, xs), *_row_strides(shape, ys))
 
 
 class RopeRows:
@@ -778,16 +783,18 @@ def rs_cache_append_rope(cache, rope, k_new, v_new, q=None, q_out=None, max_rows
     """As rs_cache_append, K rotated; q (or None): [nrows, hq, d], rotated into q_out (None: in place); pos: int32 [nrows] or
     None."""
     import torch
-    _check_new_rows(cache, k_new, v_new, start)
-    _want(_like(pos, torch.int32, (k_new.shape[0],), cache.device), "pos must be contiguous int32 [nrows]")
+    n, ks, vs = _check_new_rows(cache, k_new, v_new, start)
+    _want(pos is None or _like(pos, torch.int32, (n,), cache.device), "pos must be contiguous int32 [nrows]")
     part = None
     if q is not None:
-        _want(q.dim() == 3 and q.shape[0] == k_new.shape[0] and q.shape[2] == cache.d and q.dtype is cache.dtype
-              and q.device == cache.device, "q must be [nrows, hq, d] with the cache's dtype and device")
-        part = C.byref(_rope_part(q, q if q_out is None else q_out))
+        part = _rope_part(q, q if q_out is None else q_out)
+        shape = q.shape
+        _want(shape[0] == n and shape[2] == cache.d and q.dtype is cache.dtype and q.get_device() == cache.k.get_device(),
+              "q must be [nrows, hq, d] with the cache's dtype and device")
+        part = C.byref(part)
     return _on_device(lib().rs_cache_append_rope, cache.device, stream,
-                      (cache.ref, rope.ref, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1), v_new.stride(0),
-                       v_new.stride(1), part, _at(pos), _at(start), k_new.shape[0], max_rows))
+                      (cache.ref, rope.ref, k_new.data_ptr(), v_new.data_ptr(), ks[0], ks[1], vs[0], vs[1], part, _at(pos), _at(start),
+                       n, max_rows))
 
 
 # ---- cross attention -------------------------------------------------------------------------
@@ -805,7 +812,7 @@ class Cross:
         _want(kmask is None or kmask.dim() == 2, "kmask must be [nseq, nwords]")
         self.q, self.start, self.mask = q, start, kmask
         self.nrows, self.hq, self.d, self.device = q.shape[0], q.shape[1], q.shape[2], q.device
-        st, sh = _row_strides(q)
+        st, sh = _row_strides(q.shape, q.stride())
         self.c = RsCross(q=q.data_ptr(), hq=q.shape[1], nrows=q.shape[0], max_rows=max_rows,
                          nwords=kmask.shape[1] if kmask is not None else 0, sq_t=st, sq_h=sh, start=_at(start), kmask=_at(kmask),
                          scale=scale)

@@ -3,9 +3,10 @@
 //
 // Pair i of a row at position p turns by a = p f_i:  y_1 = m (x_1 cos a - x_2 sin a), y_2 = m (x_2 cos a + x_1 sin a).
 // Every element is read and written once, so memory bounds both calls (and the launch the short ones).  A lane takes 8
-// pairs of a row, two 16-byte chunks (four in fp32), computes their cosines and sines once and uses them for head after
-// head, so that the angles cost little beside the copying: no table of them is read from memory, and positions have no
-// upper end.
+// pairs of a row, two vectors of 16 bytes (four in fp32); the workgroup computes each cosine and sine of its rows once, into
+// LDS, for all heads, so that they cost little beside the copying: no table of them is read from memory, and positions have
+// no upper end.  131072 rows of 32 + 8 heads of 128 in bf16: 471 us, 5.7 TB/s (a large copy: 5.0); a step's few rows: the
+// launch.
 #include "rope.h"
 #include "cache.h"
 
@@ -29,116 +30,120 @@ __device__ __forceinline__ void turn(double t, float &c, float &s) {
   s = q >= 2 ? -b : b;
 }
 
-// What a lane holds of a row: 8 elements each of two chunks, in 32 bits.
-struct Piece {
-  float a[8], b[8];
-};
+// Rows are written past the caches (nontemporal), so that what is read stays in the 256 MB memory-side cache: 8191 fp32 rows
+// of 32 heads of 64 35 -> 26 us, 224 MiB of bf16 rows 90 -> 69 us, 90 -> 86 where other rows were read since.  Inputs beyond that
+// size are read past them too (NTL): nothing of them is left there, and what is there may be of use (1 GiB between two passes of
+// another kernel over it: 404 -> 349 us); smaller ones not (96 MiB: 31 -> 35 us), nor where an instruction reads half
+// lines, which would be fetched twice (30001 rows of 32 + 8 heads, half of each turned: 122 -> 133 us).
+template <bool NTL>
+__device__ __forceinline__ u32x4 load16(const char *p) {
+  if constexpr (NTL) return __builtin_nontemporal_load((const u32x4 *)p);
+  return *(const u32x4 *)p;
+}
+__device__ __forceinline__ void store16(char *p, u32x4 x) { __builtin_nontemporal_store(x, (u32x4 *)p); }
 
+// 16 elements of a row per lane, as vectors of 16 bytes: NV of them, V elements each.
 template <typename T>
-struct Raw;  // a chunk as it lies in memory
-template <>
-struct Raw<bf16> {
-  u32x4 x;
-  __device__ __forceinline__ void load(const char *p) { x = *(const u32x4 *)p; }
-  __device__ __forceinline__ void store(char *p) const { *(u32x4 *)p = x; }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
+struct Raw {
+  static constexpr int V = 16 / (int)sizeof(T), NV = 16 / V;
+  u32x4 x[NV];
+  __device__ __forceinline__ void get(float (&f)[16]) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t w = x[e];
-      f[2 * e] = __builtin_bit_cast(float, w << 16);
-      f[2 * e + 1] = __builtin_bit_cast(float, w & 0xffff0000u);
-    }
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t y = x[k][w];
+        if constexpr (V == 8) {
+          f[8 * k + 2 * w] = __builtin_bit_cast(float, y << 16);
+          f[8 * k + 2 * w + 1] = __builtin_bit_cast(float, y & 0xffff0000u);
+        } else {
+          f[4 * k + w] = __builtin_bit_cast(float, y);
+        }
+      }
   }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
+  __device__ __forceinline__ void set(const float (&f)[16]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
-  }
-};
-template <>
-struct Raw<float> {
-  f32x4 x, y;
-  __device__ __forceinline__ void load(const char *p) { x = *(const f32x4 *)p, y = *(const f32x4 *)(p + 16); }
-  __device__ __forceinline__ void store(char *p) const { *(f32x4 *)p = x, *(f32x4 *)(p + 16) = y; }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = x[e], f[4 + e] = y[e];
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = f[e], y[e] = f[4 + e];
+      for (int w = 0; w < 4; ++w) {
+        if constexpr (V == 8) x[k][w] = pack_bf16x2(f[8 * k + 2 * w], f[8 * k + 2 * w + 1]);
+        else x[k][w] = __builtin_bit_cast(uint32_t, f[4 * k + w]);
+      }
   }
 };
 
-// How the pairs of a row lie in a lane's two chunks.
-//   R_HALF   dim a multiple of 16: lanes below dim / 16 hold elements 8l .. and dim / 2 + 8l .., pair e in element e of
-//            both; the others 16 elements that stay as they are;
-//   R_INTER  elements 16l .. 16l + 15, pair e in elements 2e and 2e + 1; pairs from dim / 2 on stay;
+// How the pairs of a row lie in a lane's vectors: neighbouring lanes take neighbouring vectors, so that an instruction
+// reads whole lines (with a lane's 16 elements in one piece, 8191 fp32 rows of 32 heads of 64: 57 us; so, 35).
+//   R_HALF   dim a multiple of 16: the dim / 16 first lanes hold vectors of the first half, then those of the second at the
+//            same places (pair e in elements e and 8 + e); the others hold 16 elements that stay as they are;
+//   R_INTER  vectors of the row, LPR apart: pair e in elements 2e and 2e + 1; pairs from dim / 2 on stay;
 //   R_ANY    half layout of any even dim: elements one by one, pair 8l + e in elements 8l + e and dim / 2 + 8l + e, and
 //            from pair dim / 2 on, two neighbours that stay.
 enum { R_HALF = 0, R_INTER = 1, R_ANY = 2 };
 
-// A lane's cosines and sines, its places in a row and the number of its pairs that turn.
-template <typename T, int MODE>
+// A lane's cosines and sines and its places in a row.
+template <typename T, int MODE, int LPR>
 struct Turner {
+  static constexpr int V = Raw<T>::V, NV = Raw<T>::NV;
   float c[8], s[8];
-  int oa, ob, np;  // byte offsets of the chunks (R_ANY: of the first element of the first and the second kind)
+  int l, dim;
+  bool some;    // R_HALF: the lane's elements turn
+  int off[NV];  // byte offsets of its vectors
 
-  __device__ __forceinline__ void places(int dim, int l) {
-    const int half = dim >> 1;
-    np = clampi(half - 8 * l, 0, 8);
-    if constexpr (MODE == R_HALF) {
-      oa = np ? 8 * l : 16 * l;
-      ob = np ? half + 8 * l : 16 * l + 8;
-    } else if constexpr (MODE == R_INTER) {
-      oa = 16 * l;
-      ob = 16 * l + 8;
-    } else {
-      oa = 8 * l;
-      ob = half + 8 * l;
+  __device__ __forceinline__ Turner(int lane, int rot) : l(lane), dim(rot) {
+    const int q = dim >> 4;
+    some = MODE != R_HALF || l < q;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      int i = l + k * LPR;
+      if constexpr (MODE == R_HALF) {
+        const int kk = k % (NV / 2);
+        i = some ? l + kk * q + (k >= NV / 2 ? (dim >> 1) / V : 0) : dim / V + (l - q) + k * (LPR - q);
+      }
+      off[k] = 16 * i;
     }
-    oa *= (int)sizeof(T);
-    ob *= (int)sizeof(T);
   }
-  __device__ __forceinline__ void angles(const rs_rope &r, int l, double pos, bool back) {
+  // the pair whose turn is c[e], s[e]
+  __device__ __forceinline__ int pair_of(int e) const {
+    if constexpr (MODE == R_HALF) return V * (l + e / V * (dim >> 4)) + e % V;
+    if constexpr (MODE == R_INTER) return V / 2 * (l + e / (V / 2) * LPR) + e % (V / 2);
+    return 8 * l + e;
+  }
+  __device__ __forceinline__ bool turns(int e) const { return MODE == R_HALF ? some : pair_of(e) < dim >> 1; }
+  // the lane's pairs from the row's table of cosines, then sines
+  __device__ __forceinline__ void take(const float *row) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      c[e] = 1.f, s[e] = 0.f;
-      if (e < np) {
-        turn(pos * r.turns[8 * l + e], c[e], s[e]);
-        c[e] *= r.mscale;
-        s[e] *= back ? -r.mscale : r.mscale;
-      }
+      const int i = turns(e) ? pair_of(e) : 0;
+      c[e] = row[i], s[e] = row[8 * LPR + i];
     }
   }
   __device__ __forceinline__ void pair(int e, float &x, float &y) const {
     const float u = x * c[e] - y * s[e], v = y * c[e] + x * s[e];
     x = u, y = v;
   }
-  __device__ __forceinline__ void turn_piece(Raw<T> &ra, Raw<T> &rb) const {
-    if (np == 0) return;  // (what stays keeps its bits)
-    Piece p;
-    ra.get(p.a);
-    rb.get(p.b);
+  __device__ __forceinline__ void turn_raw(Raw<T> &r) const {
+    if (!some) return;  // (what stays keeps its bits)
+    float f[16];
+    r.get(f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if constexpr (MODE == R_HALF) {
-        pair(e, p.a[e], p.b[e]);
+        pair(e, f[e], f[8 + e]);
       } else {
-        float &x = e < 4 ? p.a[2 * e & 7] : p.b[2 * e & 7], &y = e < 4 ? p.a[(2 * e & 7) + 1] : p.b[(2 * e & 7) + 1];
-        float u = x, v = y;
+        float u = f[2 * e], v = f[2 * e + 1];
         pair(e, u, v);
-        x = e < np ? u : x;
-        y = e < np ? v : y;
+        f[2 * e] = turns(e) ? u : f[2 * e];
+        f[2 * e + 1] = turns(e) ? v : f[2 * e + 1];
       }
     }
-    ra.set(p.a);
-    rb.set(p.b);
+    r.set(f);
   }
-  // N rows of one position: heads h0, h0 + step, ... below `end`; all are loaded before any is stored, so that the loads
-  // are in flight together.  skip: y is x, and lanes whose elements stay have nothing to do.
-  template <int N>
-  __device__ __forceinline__ void rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, int end, int dim, int d,
-                                       int l, bool skip) const {
+  // Rows of one position: heads h0, h0 + step, ... below `end`, N of them loaded before any is stored.  N = 2 (16 registers)
+  // where the heads lie together; apart, one, whose 48 registers leave room for eight waves per SIMD (131072 rows of 32 + 8 heads of
+  // 128: 471 us, with the registers of four 551).  skip: y is x, and vectors that stay need not move.
+  template <int N, bool NTL>
+  __device__ __forceinline__ void rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, int end, int d, bool skip) const {
     if constexpr (MODE == R_ANY) {
       for (int h = h0; h < end; h += step) {
         const T *xr = (const T *)(x + h * sx);
@@ -146,40 +151,47 @@ struct Turner {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int i = 8 * l + e, half = dim >> 1;
-          if (2 * i >= d) break;
-          const int ia = e < np ? i : 2 * i, ib = e < np ? half + i : 2 * i + 1;
-          if (e >= np && skip) continue;
+          if (i >= half && skip) continue;
+          const int ia = i < half ? i : 2 * i, ib = i < half ? half + i : 2 * i + 1;
           const T xa = xr[ia], xb = xr[ib];
           float a = (float)xa, b = (float)xb;
           pair(e, a, b);
-          yr[ia] = e < np ? (T)a : xa;
-          yr[ib] = e < np ? (T)b : xb;
+          yr[ia] = i < half ? (T)a : xa;
+          yr[ib] = i < half ? (T)b : xb;
         }
       }
     } else {
-      if (np == 0 && skip) return;
-      for (; h0 < end; h0 += N * step) {
-        Raw<T> ra[N], rb[N];
+      bool move[NV];
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const char *p = x + (h0 + k * step < end ? h0 + k * step : h0) * sx;
-          ra[k].load(p + oa);
-          rb[k].load(p + ob);
-        }
+      for (int k = 0; k < NV; ++k) move[k] = !skip || (MODE == R_HALF ? some : off[k] < dim * (int)sizeof(T));
+      for (; h0 + (N - 1) * step < end; h0 += N * step) some_rows<N, NTL>(x, y, sx, sy, h0, step, move);
+      if constexpr (N > 1)
+        for (; h0 < end; h0 += step) some_rows<1, NTL>(x, y, sx, sy, h0, step, move);
+    }
+  }
+  template <int N, bool NTL>
+  __device__ __forceinline__ void some_rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, const bool (&move)[NV]) const {
+    Raw<T> r[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          if (h0 + k * step >= end) break;
-          turn_piece(ra[k], rb[k]);
-          char *p = y + (h0 + k * step) * sy;
-          ra[k].store(p + oa);
-          rb[k].store(p + ob);
-        }
-      }
+    for (int n = 0; n < N; ++n) {
+      const char *p = x + (h0 + n * step) * sx;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (move[k]) r[n].x[k] = load16<NTL>(p + off[k]);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      turn_raw(r[n]);
+      char *p = y + (h0 + n * step) * sy;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (move[k]) store16(p + off[k], r[n].x[k]);
     }
   }
 };
 
 constexpr int kThreads = 256;
+constexpr int64_t kSideCache = 256ll << 20;  // bytes of the memory-side cache
 
 struct RopePart {
   const char *x;
@@ -197,19 +209,39 @@ struct RopeArgs {
   bool back;
 };
 
+// Cosines and sines of the `rows` rows of a workgroup, every one computed once: tab[row] holds 8 LPR of each.  pos(row): its
+// position.
+template <int LPR, typename F>
+__device__ __forceinline__ void angle_table(float *tab, const rs_rope &r, int rows, bool back, F pos) {
+  const int half = r.dim >> 1;
+  for (int x = threadIdx.x; x < rows * 8 * LPR; x += kThreads) {
+    const int row = x / (8 * LPR), i = x % (8 * LPR);
+    if (i >= half) continue;
+    float c, s;
+    turn(pos(row) * r.turns[i], c, s);
+    tab[row * 16 * LPR + i] = c * r.mscale;
+    tab[row * 16 * LPR + 8 * LPR + i] = s * (back ? -r.mscale : r.mscale);
+  }
+  __syncthreads();
+}
+
 // A workgroup takes 256 / (lanes of a row x groups) rows.
-template <typename T, int MODE, int LPR>
+template <typename T, int MODE, int LPR, int N, bool NTL>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
-  const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1);
-  const int r = blockIdx.x * (kThreads / LPR >> a.lg) + (x >> a.lg);
+  __shared__ float tab[kThreads * 16];
+  const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
+  const int r0 = blockIdx.x * rows, r = r0 + (x >> a.lg);
+  angle_table<LPR>(tab, a.rope, rows, a.back, [&](int i) {
+    const int at = r0 + i < a.n ? r0 + i : a.n - 1;
+    return (double)(a.pos ? (int64_t)a.pos[at] : a.pos0 + at);
+  });
   if (r >= a.n) return;
-  Turner<T, MODE> t;
-  t.places(a.rope.dim, l);
-  t.angles(a.rope, l, (double)(a.pos ? (int64_t)a.pos[r] : a.pos0 + r), a.back);
+  Turner<T, MODE, LPR> t(l, a.rope.dim);
+  t.take(tab + (r - r0) * 16 * LPR);
   int first = g;  // heads of all parts one after the other are dealt to the groups
   for (int k = 0; k < a.nparts; ++k) {
     const RopePart &p = a.part[k];
-    t.template rows<4>(p.x + r * p.sx_t, p.y + r * p.sy_t, p.sx_h, p.sy_h, first, groups, p.heads, a.rope.dim, a.d, l, p.inplace);
+    t.template rows<N, NTL>(p.x + r * p.sx_t, p.y + r * p.sy_t, p.sx_h, p.sy_h, first, groups, p.heads, a.d, p.inplace);
     first = (first - p.heads) & (groups - 1);
   }
 }
@@ -225,60 +257,83 @@ struct AppendRopeArgs {
 };
 
 // As rope_kernel, a sequence's rows: heads of K with those of V, then of Q.
-template <typename T, int MODE, int LPR>
+template <typename T, int MODE, int LPR, int N, bool NTL>
 __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeArgs a) {
+  __shared__ float tab[kThreads * 16];
   const CacheView &c = a.c;
-  const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1);
-  const int b = blockIdx.y, i = blockIdx.x * (kThreads / LPR >> a.lg) + (x >> a.lg);
+  const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
+  const int b = blockIdx.y, i0 = blockIdx.x * rows, i = i0 + (x >> a.lg);
   const RowRange rr = new_rows(a.start, b, a.nrows, a.max_rows);
-  if (i >= rr.count) return;
+  if (i0 >= rr.count) return;
   const int len = cache_len(c, b);
+  const int64_t pos0 = c.seen ? c.seen[b] : len;
+  angle_table<LPR>(tab, a.rope, rows, false, [&](int k) {
+    const int at = i0 + k < rr.count ? i0 + k : rr.count - 1;
+    return (double)(a.pos ? (int64_t)a.pos[rr.first + at] : pos0 + at);
+  });
+  if (i >= rr.count) return;
   const int64_t row = rr.first + i;
-  Turner<T, MODE> t;
-  t.places(a.rope.dim, l);
-  t.angles(a.rope, l, (double)(a.pos ? (int64_t)a.pos[row] : (int64_t)(c.seen ? c.seen[b] : len) + i), false);
+  Turner<T, MODE, LPR> t(l, a.rope.dim);
+  t.take(tab + (i - i0) * 16 * LPR);
   const int64_t j = (int64_t)len + i;
   const int p = j < c.cap ? page_of(c, (int)j) : 0, id = j < c.cap ? page_id(c, b, p) : -1;
   if (id >= 0) {
     const char *kr = a.kn + row * a.skt, *vr = a.vn + row * a.svt;
     const int64_t ko = k_offset(c, id, p, (int)j, 0), vo = v_offset(c, id, p, (int)j, 0);
     for (int h = g; h < c.hkv; h += groups) {
-      Raw<T> va, vb;
-      va.load(vr + h * a.svh + 16 * l * (int)sizeof(T));
-      vb.load(vr + h * a.svh + (16 * l + 8) * (int)sizeof(T));
-      t.template rows<1>(kr, c.k + ko, a.skh, c.sk_h, h, groups, h + 1, a.rope.dim, a.d, l, false);
-      char *vp = c.v + vo + h * c.sv_h + 16 * l * (int)sizeof(T);
-      va.store(vp);
-      vb.store(vp + 8 * sizeof(T));
+      Raw<T> v;
+#pragma unroll
+      for (int k = 0; k < Raw<T>::NV; ++k) v.x[k] = load16<NTL>(vr + h * a.svh + 16 * (l + k * LPR));
+      t.template rows<1, NTL>(kr, c.k + ko, a.skh, c.sk_h, h, groups, h + 1, a.d, false);
+#pragma unroll
+      for (int k = 0; k < Raw<T>::NV; ++k) store16(c.v + vo + h * c.sv_h + 16 * (l + k * LPR), v.x[k]);
       if (c.acc && l == 0) c.acc[((int64_t)b * c.hkv + h) * c.cap + j] = 0.f;
     }
   }
   const int first = (g - c.hkv) & (groups - 1);
-  t.template rows<4>(a.q.x + row * a.q.sx_t, a.q.y + row * a.q.sy_t, a.q.sx_h, a.q.sy_h, first, groups, a.q.heads, a.rope.dim, a.d,
-                     l, a.q.inplace);
+  t.template rows<N, NTL>(a.q.x + row * a.q.sx_t, a.q.y + row * a.q.sy_t, a.q.sx_h, a.q.sy_h, first, groups, a.q.heads, a.d, a.q.inplace);
 }
 
 RopePart part_of(const rs_rope_part &p, int e) {
   return RopePart{(const char *)p.x, (char *)p.y, p.sx_t * e, p.sx_h * e, p.sy_t * e, p.sy_h * e, p.heads, p.x == p.y};
 }
 
-// log2 of the groups of heads: a row is split over so many lanes that the rows fill the chip's 2^19 lanes, up to a
-// workgroup's 256 or one head each.
-int head_groups(int64_t rows, int d, int heads) {
+// log2 of the groups of heads that share a row.  Where a token's heads lie together a workgroup takes one row, a head per
+// group, so that it reads and writes long pieces of memory; where a head's tokens do, one group with a row per LPR lanes does,
+// split further only until the rows fill the chip's 2^19 lanes.  (32768 rows of 32 + 2 x 8 heads of 128 appended: 137 us, with
+// 8 groups 140 and with one 157; 30001 rows of 32 + 8, half of each turned: 124, 127, 135.)
+int head_groups(int64_t rows, int d, int heads, bool tokens) {
+  const int most = d == 128 ? 5 : 6;
   int lg = 0;
-  while (lg < (d == 128 ? 5 : 6) && (1 << lg) < heads && rows * (d / 16) << lg < 1 << 19) ++lg;
+  while (lg < most && (1 << lg) < heads && (tokens || rows * (d / 16) << lg < 1 << 19)) ++lg;
   return lg;
 }
 
+// f(type, mode, lanes of a row, heads at a time, loads that bypass) of a call over `bytes` of input.
 template <typename F>
-void by_shape(int dtype, int d, const rs_rope &r, F f) {
+void by_shape(int dtype, int d, const rs_rope &r, bool tokens, int64_t bytes, F f) {
+  using std::integral_constant;
+  auto with_n = [&](auto t, auto m, auto l) {
+    constexpr int M = decltype(m)::value, L = decltype(l)::value, many = sizeof(t) == 2 ? 2 : 1;
+    if constexpr (M == R_ANY) {
+      f(t, m, l, integral_constant<int, 1>{}, std::false_type{});
+    } else {
+      const bool lines = L == 8 && (M == R_INTER || r.dim == d);  // a row's lanes read whole lines of 128 bytes
+      auto with_l = [&](auto n) {
+        if constexpr (L == 8)
+          if (lines && bytes > kSideCache) return f(t, m, l, n, std::true_type{});
+        f(t, m, l, n, std::false_type{});
+      };
+      tokens ? with_l(integral_constant<int, many>{}) : with_l(integral_constant<int, 1>{});
+    }
+  };
   auto with_l = [&](auto t, auto m) {
-    d == 128 ? f(t, m, std::integral_constant<int, 8>{}) : f(t, m, std::integral_constant<int, 4>{});
+    d == 128 ? with_n(t, m, integral_constant<int, 8>{}) : with_n(t, m, integral_constant<int, 4>{});
   };
   auto with_m = [&](auto t) {
-    if (r.layout == RS_ROPE_INTERLEAVED) with_l(t, std::integral_constant<int, R_INTER>{});
-    else if (r.dim % 16 == 0) with_l(t, std::integral_constant<int, R_HALF>{});
-    else with_l(t, std::integral_constant<int, R_ANY>{});
+    if (r.layout == RS_ROPE_INTERLEAVED) with_l(t, integral_constant<int, R_INTER>{});
+    else if (r.dim % 16 == 0) with_l(t, integral_constant<int, R_HALF>{});
+    else with_l(t, integral_constant<int, R_ANY>{});
   };
   dtype == RS_BF16 ? with_m(bf16{}) : with_m(float{});
 }
@@ -295,10 +350,12 @@ rs_status rope_launch(const rs_rope &rope, const rs_rope_rows &rows, bool transp
     a.part[k] = part_of(rows.part[k], e);
     heads += rows.part[k].heads;
   }
-  a.lg = head_groups(rows.n, rows.d, heads);
+  const bool tokens = rows.part[0].sx_h < rows.part[0].sx_t;
+  a.lg = head_groups(rows.n, rows.d, heads, tokens);
   const int per = kThreads / (rows.d / 16) >> a.lg;
-  by_shape(rows.dtype, rows.d, rope, [&](auto t, auto m, auto l) {
-    rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value><<<(rows.n + per - 1) / per, kThreads, 0, st>>>(a);
+  by_shape(rows.dtype, rows.d, rope, tokens, (int64_t)rows.n * heads * rows.d * e, [&](auto t, auto m, auto l, auto n, auto ntl) {
+    rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value>
+        <<<(rows.n + per - 1) / per, kThreads, 0, st>>>(a);
   });
   RS_HIP(hipGetLastError());
   return RS_OK;
@@ -317,10 +374,11 @@ rs_status append_rope_launch(const CacheView &c, int dtype, int d, const rs_rope
   a.pos = pos, a.start = start, a.nrows = nrows, a.max_rows = max_rows, a.d = d;
   const int most = max_rows < nrows ? max_rows : nrows;  // rows of a sequence at most
   const int64_t all = (int64_t)c.nseq * most;
-  a.lg = head_groups(all < nrows ? all : nrows, d, c.hkv + a.q.heads);
+  const bool tokens = skh < skt;
+  a.lg = head_groups(all < nrows ? all : nrows, d, c.hkv + a.q.heads, tokens);
   const int per = kThreads / (d / 16) >> a.lg;
-  by_shape(dtype, d, rope, [&](auto t, auto m, auto l) {
-    append_rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value>
+  by_shape(dtype, d, rope, tokens, (int64_t)nrows * (2 * c.hkv + a.q.heads) * d * e, [&](auto t, auto m, auto l, auto n, auto ntl) {
+    append_rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value>
         <<<dim3((most + per - 1) / per, c.nseq), kThreads, 0, st>>>(a);
   });
   RS_HIP(hipGetLastError());
