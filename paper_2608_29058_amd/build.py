@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "librs.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
-HIP_SOURCES = ["attn.hip", "probe.hip", "topk.hip", "route_dev.hip", "decode.hip", "cache.hip", "rope.hip"]
+HIP_SOURCES = ["attn.hip", "probe.hip", "topk.hip", "route_dev.hip", "decode.hip", "cache.hip", "rope.hip", "cross.hip"]
 # sources whose fp64 operation order is part of their definition
 NO_CONTRACT = {"route_dev.hip"}
 HOST_HIP_SOURCES = ["api.cpp", "cache_api.cpp", "rope_api.cpp"]

@@ -975,7 +975,7 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
     np = a.pieces;
   } else {
     Seq q = seq_at<WHAT>(a, lane);
-    const int groups = plan_groups<WHAT>(a, q, lane);
+    const int groups = WHAT == W_CROSS && a.resident ? *a.plan : plan_groups<WHAT>(a, q, lane);
     int base = 0, b = -1, first = 0;
     np = 0;
     for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
@@ -1492,9 +1492,14 @@ int tile_rows(bool f32, int d, bool sel, int rows) {
 
 struct DraftShape {
   int trows, rtiles, slots, least, grid, pieces, waves;
+  int resident;  // cross.hip's workgroups at once, 0 for the other kernels
 };
 
 constexpr int kShort = 256;
+#ifndef RS_CROSS_ROWS
+#define RS_CROSS_ROWS 64
+#endif
+constexpr int kCrossRows = RS_CROSS_ROWS;  // rows of a head beyond which a prompt takes tiles of 128
 constexpr int kMaxGrid = 1 << 23;  // workgroups of up to 512 threads, of which a launch has fewer than 2^32
 
 DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int what) {
@@ -1503,11 +1508,13 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   const int G = q.hq / c.hkv, most_rows = what == W_CROSS && q.nrows < q.max_rows ? q.nrows : q.max_rows;
   const int rows = nsel ? G : G * most_rows;
   s.trows = tile_rows(f32, d, nsel > 0, rows);
+  const bool prompt = what == W_CROSS && !f32 && rows > kCrossRows;  // cross.hip
+  if (prompt) s.trows = 128;
   s.rtiles = (rows + s.trows - 1) / s.trows;
   // workgroups that the chip holds at once: with stages three per CU (d = 64: 16 sequences of 16000 rows, 256 rows of Q,
   // 233 us, planned for two 295), two (d = 128, four waves) or one; else two with d = 64 or 16 rows of bf16, or one
   const bool two = d == 64 || (!f32 && s.trows == 16), wide = s.trows > 32;
-  const int resident = 256 * (!wide ? 1 + two : d == 64 ? 3 : s.trows < 256 ? 2 : 1);
+  const int resident = 256 * (!wide ? 1 + two : prompt ? 2 : d == 64 ? 3 : s.trows < 256 ? 2 : 1);
   if (nsel) {
     const int64_t items = (int64_t)q.nrows * c.hkv * s.rtiles;
     const int most = (int)(((int64_t)nsel * 64 + 63 + q.max_rows + kGroup - 1) / kGroup);
@@ -1523,6 +1530,15 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
     tiles = tiles < own ? tiles : own;
   }
   const int64_t items = tiles * c.hkv, most = items * ((c.cap + kGroup - 1) / kGroup);
+  if (prompt) {  // rounds of workgroups, planned on the device: cross.hip
+    s.resident = resident;
+    s.least = 4;
+    s.slots = c.cap <= s.least * kGroup || items >= 8 * resident ? 0 : 1;
+    int64_t n = !s.slots ? items : items < resident ? resident : items + 4 * resident;
+    n = n < most ? n : most;
+    s.grid = n < kMaxGrid ? (int)n : kMaxGrid;
+    return s;
+  }
   // A short cache stays in one piece and needs no joining launch (4 us): up to kShort rows in four waves, twice that in
   // eight where a CU holds two waves per SIMD (8 heads over 500 rows: one sequence 12.6 -> 10.0 us, 64 of them 36.7 ->
   // 27.5).  Longer ones gain from pieces (one token over 1001 rows: 14.7 us in one piece, 12.3 in several): few items
@@ -1559,6 +1575,8 @@ void by_tiles(bool f32, int d, int trows, F f) {
 
 template <bool F32, int D, int WHAT>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
+  if constexpr (WHAT == W_CROSS && !F32)
+    if (s.trows == 128) return cross_wide_launch(a, D, s.grid, st);
   if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
     if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
@@ -1576,10 +1594,12 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   a.least = s.least;
   a.pieces = s.pieces;
   a.grid = s.grid;
+  a.resident = s.resident;
   // (a single piece is the result itself; its call asks for one line all the same, so that no caller does without one)
   const size_t rows = s.slots > 0 || s.pieces > 1 ? (size_t)s.grid * s.trows : 0;
   a.po = ar.take<float>(rows ? rows * d : 64);
   a.pml = ar.take<float>(rows * 2);
+  a.plan = ar.take<int32_t>(1);
   return a;
 }
 

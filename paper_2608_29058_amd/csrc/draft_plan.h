@@ -23,6 +23,8 @@ struct DraftArgs {
   const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
   int nsel, pieces;  // with a list: pieces per item
   int grid;          // workgroups, and slots of pieces
+  int resident;      // cross.hip: workgroups that the chip holds at once
+  int32_t *plan;     // cross.hip: where it leaves the groups of a piece for the joining kernel
 };
 
 // Launch of the matrix-rate kernel of W_CROSS, bf16, row tiles of 128 (cross.hip).
@@ -128,11 +130,9 @@ __device__ __forceinline__ int plan_groups(const DraftArgs &a, const Seq &first,
   return groups > a.least ? (int)groups : a.least;
 }
 
-// The id-th piece overall; false: there are fewer.
+// The id-th piece overall, at `groups` groups a piece; false: there are fewer.  q: the sequences of the first round of lanes.
 template <int WHAT>
-__device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
-  Seq q = seq_at<WHAT>(a, lane);
-  const int groups = plan_groups<WHAT>(a, q, lane);
+__device__ __forceinline__ bool find_piece(const DraftArgs &a, Seq q, int groups, int id, int lane, Item &it) {
   int base = 0;
   for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
     if (b0) q = seq_at<WHAT>(a, b0 + lane);
@@ -157,6 +157,11 @@ __device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
     base += all;
   }
   return false;
+}
+template <int WHAT>
+__device__ bool find_item(const DraftArgs &a, int id, int lane, Item &it) {
+  const Seq q = seq_at<WHAT>(a, lane);
+  return find_piece<WHAT>(a, q, plan_groups<WHAT>(a, q, lane), id, lane, it);
 }
 
 }  // namespace
