@@ -975,7 +975,7 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
     np = a.pieces;
   } else {
     Seq q = seq_at<WHAT>(a, lane);
-    const int groups = WHAT == W_CROSS && a.resident ? *a.plan : plan_groups<WHAT>(a, q, lane);
+    const int groups = plan_groups<WHAT>(a, q, lane);
     int base = 0, b = -1, first = 0;
     np = 0;
     for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
@@ -1492,7 +1492,7 @@ int tile_rows(bool f32, int d, bool sel, int rows) {
 
 struct DraftShape {
   int trows, rtiles, slots, least, grid, pieces, waves;
-  int resident;  // cross.hip's workgroups at once, 0 for the other kernels
+  int resident, items;  // cross.hip's workgroups at once (0: the other kernels) and items
 };
 
 constexpr int kShort = 256;
@@ -1532,6 +1532,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   const int64_t items = tiles * c.hkv, most = items * ((c.cap + kGroup - 1) / kGroup);
   if (prompt) {  // rounds of workgroups, planned on the device: cross.hip
     s.resident = resident;
+    s.items = items < kMaxGrid ? (int)items : kMaxGrid;
     s.least = 4;
     s.slots = c.cap <= s.least * kGroup || items >= 8 * resident ? 0 : 1;
     int64_t n = !s.slots ? items : items < resident ? resident : items + 4 * resident;
@@ -1576,7 +1577,7 @@ void by_tiles(bool f32, int d, int trows, F f) {
 template <bool F32, int D, int WHAT>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
   if constexpr (WHAT == W_CROSS && !F32)
-    if (s.trows == 128) return cross_wide_launch(a, D, s.grid, st);
+    if (s.resident) return cross_wide_launch(a, D, s.items, st);
   if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
     if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
@@ -1634,7 +1635,7 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
         draft_kernel<F, D, NQ, WHAT><<<s.grid, 256, 0, st>>>(a);
       }
     });
-  if (SEL ? s.pieces > 1 : s.slots > 0) {
+  if (SEL ? s.pieces > 1 : s.slots > 0 && !s.resident) {
     if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
       const dim3 grid(a.q.nrows, (a.q.hq + kWaves - 1) / kWaves);
       d == 128 ? draft_join_kernel<128, WHAT, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, WHAT, 1><<<grid, 256, 0, st>>>(a);

@@ -27,8 +27,8 @@ struct DraftArgs {
   int32_t *plan;     // cross.hip: where it leaves the groups of a piece for the joining kernel
 };
 
-// Launch of the matrix-rate kernel of W_CROSS, bf16, row tiles of 128 (cross.hip).
-void cross_wide_launch(const DraftArgs &a, int d, int grid, hipStream_t st);
+// Launches of the matrix-rate kernel of W_CROSS, bf16, row tiles of 128, over at most `items` of them, and of its join (cross.hip).
+void cross_wide_launch(const DraftArgs &a, int d, int items, hipStream_t st);
 
 #if defined(__HIPCC__)
 namespace {
