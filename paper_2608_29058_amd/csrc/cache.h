@@ -100,6 +100,21 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
+// Sum of x >= 0 whose sum may pass 32 bits, and maximum of x >= 0, over the wave.
+__device__ __forceinline__ long long wave_sum_long(long long x) {
+  return ((long long)wave_sum((int)(x >> 20)) << 20) + wave_sum((int)(x & 0xfffff));
+}
+__device__ __forceinline__ int larger(int a, int b) { return a > b ? a : b; }
+__device__ __forceinline__ int wave_most(int x) {
+  x = larger(x, dpp_or_0<0x111, 0xf>(x));
+  x = larger(x, dpp_or_0<0x112, 0xf>(x));
+  x = larger(x, dpp_or_0<0x114, 0xf>(x));
+  x = larger(x, dpp_or_0<0x118, 0xf>(x));
+  x = larger(x, dpp_or_0<0x142, 0xa>(x));
+  x = larger(x, dpp_or_0<0x143, 0xc>(x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Exclusive prefix sum of x over the NT threads of a workgroup, and the total; sw: NT / 64 words of LDS.
 template <int NT>
 __device__ __forceinline__ int block_scan(int x, int *sw, int *total) {

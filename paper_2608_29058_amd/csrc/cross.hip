@@ -51,7 +51,7 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Groups per piece.  The chip works in rounds of `resident` workgroups, so that the time is about that of the rounds' pieces
 // and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us).  Of pieces
-// of the longest sequence's whole, 1/2, 1/3, 1/4, 1/6, 1/9 and 1/13 the fastest.
+// of the longest sequence's whole, 1/2, 1/3, 1/4, 1/6, 1/9, 1/13 .. the fastest.
 __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first, int lane) {
   if (a.slots == 0) return kMaxN;  // one piece each
   auto all = [&](auto f) {  // sum over the sequences
@@ -61,19 +61,11 @@ __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first,
   };
   const int items = all([&](const Seq &q) { return items_of<W_CROSS>(a, q); });
   int longest = first.groups;
-  for (int b0 = 64; b0 < a.c.nseq; b0 += 64) {
-    const int g = seq_at<W_CROSS>(a, b0 + lane).groups;
-    longest = longest > g ? longest : g;
-  }
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) {
-    const int g = __shfl_xor(longest, x);
-    longest = longest > g ? longest : g;
-  }
-  longest = uniform(longest);
+  for (int b0 = 64; b0 < a.c.nseq; b0 += 64) longest = larger(longest, seq_at<W_CROSS>(a, b0 + lane).groups);
+  longest = wave_most(longest);
   const auto rounds = [&](int n) { return (n + a.resident - 1) / a.resident; };
   int best = kMaxN, cost = rounds(items) * longest * 128;
-  for (int k = 2; k <= 16; k += k < 4 ? 1 : k / 2) {  // 2, 3, 4, 6, 9, 13
+  for (int k = 2; k < kMaxN / kGroup; k += k < 4 ? 1 : k / 2) {
     const int per = (longest + k - 1) / k;
     if (per < a.least) break;
     const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^10: ceil by the product, less half a step)
@@ -81,7 +73,8 @@ __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first,
       return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
     });
     const int c = rounds(n) * per * 128 + n;
-    if (n <= a.grid && c < cost) cost = c, best = per;
+    if (n > a.grid) break;
+    if (c < cost) cost = c, best = per;
   }
   return best;
 }
@@ -473,9 +466,10 @@ __global__ __launch_bounds__(256, 2) void cross_kernel(const DraftArgs) {
   if (!cross_walk<D, MASK, false>(it, lds)) cross_walk<D, MASK, true>(it, lds);
 }
 
-// Joins the pieces of an item, 32 of its rows per workgroup (grid: items x 4).  A row's D / 4 lanes hold 4 dimensions each.
+// Joins the pieces of an item, `rows` of its rows per workgroup (grid: items x 128 / rows).  A row's D / 4 lanes hold 4
+// dimensions each.
 template <int D>
-__global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a) {
+__global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a, int rows) {
   constexpr int LPR = D / 4, RPI = 256 / LPR, kAhead = 4;
   const int lane = threadIdx.x & 63, groups = *a.plan;
   int id = blockIdx.x, slot = -1, np = 0, per = 0, first = 0, t = 0, base = 0;
@@ -500,9 +494,8 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a) {
   if (np <= 1 || slot + (np - 1) * per >= a.grid) return;
   const int rt = id / a.c.hkv, g = id - rt * a.c.hkv, G = a.q.hq / a.c.hkv;
   const int d0 = threadIdx.x % LPR * 4;
-#pragma unroll
-  for (int x = 0; x < 32 / RPI; ++x) {
-    const int in = blockIdx.y * 32 + x * RPI + threadIdx.x / LPR, row = rt * kRows + in;
+  for (int x = 0; x < rows; x += RPI) {
+    const int in = blockIdx.y * rows + x + threadIdx.x / LPR, row = rt * kRows + in;
     if (row >= G * t) return;
     const float *pml = a.pml + ((int64_t)slot * kRows + in) * 2, *po = a.po + ((int64_t)slot * kRows + in) * D + d0;
     const int64_t step = (int64_t)per * kRows;
@@ -541,8 +534,9 @@ void cross_wide_launch(const DraftArgs &a, int d, int items, hipStream_t st) {
   if (a.q.mask) d == 128 ? cross_kernel<128, true><<<a.grid, 256, 0, st>>>(a) : cross_kernel<64, true><<<a.grid, 256, 0, st>>>(a);
   else d == 128 ? cross_kernel<128, false><<<a.grid, 256, 0, st>>>(a) : cross_kernel<64, false><<<a.grid, 256, 0, st>>>(a);
   if (a.slots == 0) return;
-  const dim3 grid(items, kRows / 32);
-  d == 128 ? cross_join_kernel<128><<<grid, 256, 0, st>>>(a) : cross_join_kernel<64><<<grid, 256, 0, st>>>(a);
+  const int rows = items >= 256 ? 32 : d == 128 ? 8 : 16;  // few items have many pieces
+  const dim3 grid(items, kRows / rows);
+  d == 128 ? cross_join_kernel<128><<<grid, 256, 0, st>>>(a, rows) : cross_join_kernel<64><<<grid, 256, 0, st>>>(a, rows);
 }
 
 }  // namespace rs

@@ -1492,15 +1492,27 @@ int tile_rows(bool f32, int d, bool sel, int rows) {
 
 struct DraftShape {
   int trows, rtiles, slots, least, grid, pieces, waves;
-  int resident, items;  // cross.hip's workgroups at once (0: the other kernels) and items
+  int resident, items;  // W_CROSS: workgroups at once where the device plans with them; items of cross.hip, 0: the other kernels
 };
 
 constexpr int kShort = 256;
-#ifndef RS_CROSS_ROWS
-#define RS_CROSS_ROWS 64
-#endif
-constexpr int kCrossRows = RS_CROSS_ROWS;  // rows of a head beyond which a prompt takes tiles of 128
 constexpr int kMaxGrid = 1 << 23;  // workgroups of up to 512 threads, of which a launch has fewer than 2^32
+
+// Row tiles of all sequences at `trows` rows: a sequence has those of its own rows, less than one of them not full.
+int64_t cross_tiles(const CacheView &c, const DraftView &q, int rows, int trows) {
+  const int64_t all = (int64_t)c.nseq * ((rows + trows - 1) / trows), own = (int64_t)(q.hq / c.hkv) * q.nrows / trows + c.nseq;
+  return all < own ? all : own;
+}
+
+// Whether cross attention in bf16 takes the kernel of prompts (cross.hip, 128 rows and two workgroups per CU): where it has
+// full tiles, or enough of them that the stages of the kernels above, which share a tile of rows among more workgroups, gain
+// nothing.  32 heads of 128 over 8, us of this kernel and of those: 80 rows, 8 x 3000 states 36 and 38, 16 x 4000 61 and 83, 2 x
+// 16384 55 and 45; 48 rows, 32 x 500 states 20 and 28, 64 x 1000 59 and 85, 4 x 8000 43 and 35; 192 rows, 65536 states 107 and 146,
+// of d = 64 78 and 67.
+bool cross_prompt(const CacheView &c, const DraftView &q, bool f32, int d, int rows) {
+  const int64_t items = cross_tiles(c, q, rows, 128) * c.hkv;
+  return !f32 && (rows > (d == 128 ? 128 : 256) || (rows > 64 && items >= 32) || (rows > 32 && items >= 128));
+}
 
 DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, int nsel, int what) {
   DraftShape s{};
@@ -1508,7 +1520,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   const int G = q.hq / c.hkv, most_rows = what == W_CROSS && q.nrows < q.max_rows ? q.nrows : q.max_rows;
   const int rows = nsel ? G : G * most_rows;
   s.trows = tile_rows(f32, d, nsel > 0, rows);
-  const bool prompt = what == W_CROSS && !f32 && rows > kCrossRows;  // cross.hip
+  const bool prompt = what == W_CROSS && cross_prompt(c, q, f32, d, rows);
   if (prompt) s.trows = 128;
   s.rtiles = (rows + s.trows - 1) / s.trows;
   // workgroups that the chip holds at once: with stages three per CU (d = 64: 16 sequences of 16000 rows, 256 rows of Q,
@@ -1524,11 +1536,7 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
     s.grid = (int)(items * s.pieces);
     return s;
   }
-  int64_t tiles = (int64_t)c.nseq * s.rtiles;
-  if (what == W_CROSS) {  // a sequence has the row tiles of its own rows, less than one that is not full
-    const int64_t own = (int64_t)G * q.nrows / s.trows + c.nseq;
-    tiles = tiles < own ? tiles : own;
-  }
+  const int64_t tiles = what == W_CROSS ? cross_tiles(c, q, rows, s.trows) : (int64_t)c.nseq * s.rtiles;
   const int64_t items = tiles * c.hkv, most = items * ((c.cap + kGroup - 1) / kGroup);
   if (prompt) {  // rounds of workgroups, planned on the device: cross.hip
     s.resident = resident;
@@ -1557,7 +1565,9 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   s.slots = items <= resident / 2 ? resident - (int)items : 4 * resident;
   s.least = items <= resident / 2 ? 1 : s.trows >= 128 ? 16 : s.trows / 16;
   if (c.cap <= s.least * kGroup) s.slots = 0;  // no sequence is long enough for two pieces
-  const int64_t grid = items + s.slots;
+  // (cross attention of so many items decides on the device between both, by how even they are: plan_groups)
+  if (what == W_CROSS && s.slots && items > resident / 8 && items <= resident / 2) s.resident = resident;
+  const int64_t grid = items + (s.resident ? 4 * resident : s.slots);
   const int64_t n = grid < most && s.slots ? grid : s.slots ? most : items;
   s.grid = n < kMaxGrid ? (int)n : kMaxGrid;  // (refused)
   return s;
@@ -1577,7 +1587,7 @@ void by_tiles(bool f32, int d, int trows, F f) {
 template <bool F32, int D, int WHAT>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
   if constexpr (WHAT == W_CROSS && !F32)
-    if (s.resident) return cross_wide_launch(a, D, s.items, st);
+    if (s.items) return cross_wide_launch(a, D, s.items, st);
   if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
     if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
@@ -1635,7 +1645,7 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
         draft_kernel<F, D, NQ, WHAT><<<s.grid, 256, 0, st>>>(a);
       }
     });
-  if (SEL ? s.pieces > 1 : s.slots > 0 && !s.resident) {
+  if (SEL ? s.pieces > 1 : s.slots > 0 && !s.items) {
     if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
       const dim3 grid(a.q.nrows, (a.q.hq + kWaves - 1) / kWaves);
       d == 128 ? draft_join_kernel<128, WHAT, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, WHAT, 1><<<grid, 256, 0, st>>>(a);

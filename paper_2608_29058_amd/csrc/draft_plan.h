@@ -23,7 +23,7 @@ struct DraftArgs {
   const int32_t *list;  // selected blocks [nrows * hkv][nsel], or NULL: all rows
   int nsel, pieces;  // with a list: pieces per item
   int grid;          // workgroups, and slots of pieces
-  int resident;      // cross.hip: workgroups that the chip holds at once
+  int resident;      // W_CROSS: workgroups that the chip holds at once, 0: plan by slots alone
   int32_t *plan;     // cross.hip: where it leaves the groups of a piece for the joining kernel
 };
 
@@ -110,15 +110,28 @@ template <int WHAT>
 __device__ __forceinline__ int plan_groups(const DraftArgs &a, const Seq &first, int lane) {
   if (a.slots == 0) return kMaxN;  // one piece each
   if constexpr (WHAT == W_CROSS) {
-    // (the host bounds row tiles by 2^23, so that tiles x groups of all sequences pass 32 bits)
-    long long work = (long long)items_of<WHAT>(a, first) * first.groups;
-    for (int b0 = 64; b0 < a.c.nseq; b0 += 64) {
-      const Seq q = seq_at<WHAT>(a, b0 + lane);
-      work += (long long)items_of<WHAT>(a, q) * q.groups;
+    // f's sum over the sequences (the host bounds row tiles by 2^23: tiles x groups pass 32 bits)
+    auto all = [&](auto f) {
+      long long x = f(first);
+      for (int b0 = 64; b0 < a.c.nseq; b0 += 64) x += f(seq_at<WHAT>(a, b0 + lane));
+      return wave_sum_long(x);
+    };
+    const long long work = all([&](const Seq &q) { return (long long)items_of<WHAT>(a, q) * q.groups; });
+    long long groups = (work + a.slots - 1) / a.slots;
+    groups = groups > a.least ? groups : a.least;
+    if (a.resident) {
+      // One round of workgroups, each with a piece, unless sequences differ so much that a fifth of the round's time would
+      // pass with some of them idle: then pieces of a quarter of a round (32 sequences of 0 to
+      // 16384 states, 8 heads: 238 -> 200 us).
+      int most = 0;
+      for (int b0 = 0; b0 < a.c.nseq; b0 += 64) {
+        const Seq q = b0 ? seq_at<WHAT>(a, b0 + lane) : first;
+        const int n = q.groups > 0 ? (q.groups + pieces_of(q.groups, (int)groups) - 1) / pieces_of(q.groups, (int)groups) : 0;
+        most = larger(most, n);
+      }
+      most = wave_most(most);
+      if (work * 5 < (long long)most * a.resident * 4) groups = (work + 4 * a.resident - 1) / (4 * a.resident);
     }
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) work += __shfl_xor(work, x);
-    const long long groups = (work + a.slots - 1) / a.slots;
     return groups > a.least ? (int)groups : a.least;
   }
   int work = first.groups;  // (at most 65535 sequences of 2048 groups)
