@@ -222,10 +222,11 @@ __device__ __forceinline__ uint32_t seen_rows(const RowsOf &ro, int i, int j) {
   return low_bits(-x) | (drafts & low_bits(ro.total - j));
 }
 
-// W_CROSS: which of the rows j .. j + 31 the sequence's queries see, as bits; j is a multiple of 32.
+// W_CROSS: which of the rows j .. j + 31 the sequence's queries see, as bits; j is a multiple of 32.  (Behind the end the mask has
+// no word to read.)
 __device__ __forceinline__ uint32_t seen_keys(const RowsOf &ro, int j) {
   const uint32_t all = low_bits(ro.total - j);
-  return ro.q->mask ? all & (uint32_t)uload((const int32_t *)ro.q->mask, (int64_t)ro.b * ro.q->nwords + (j >> 5)) : all;
+  return ro.q->mask && j < ro.total ? all & (uint32_t)uload((const int32_t *)ro.q->mask, (int64_t)ro.b * ro.q->nwords + (j >> 5)) : all;
 }
 
 // An edge: a tile of 32 rows from row j that some row of Q may not see in whole (drafted rows, the end).  Scores
@@ -1552,7 +1553,11 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   // eight where a CU holds two waves per SIMD (8 heads over 500 rows: one sequence 12.6 -> 10.0 us, 64 of them 36.7 ->
   // 27.5).  Longer ones gain from pieces (one token over 1001 rows: 14.7 us in one piece, 12.3 in several): few items
   // make one round of workgroups; many, pieces of a quarter of a round, so that the last round is short.
-  if (c.cap <= (two && !wide ? 2 * kShort : kShort)) {
+  // Cross attention in bf16 does so up to 2048 states where its items fill half of the CUs: lengths of one batch are nearer to
+  // each other there (16 sequences, 8 heads of 128 over 1500 states: 28 us in pieces, 22 in one of eight waves; 16 heads of 64 25
+  // and 19; lengths from 0 on 20 and 21, 20 and 15; with 8 sequences of 8 heads of 128 17 and 21).
+  const bool one = what == W_CROSS && !f32 && s.trows == 16 && items >= 128 && c.cap <= 8 * kShort;
+  if (one || c.cap <= (two && !wide ? 2 * kShort : kShort)) {
     s.waves = c.cap > kShort ? 8 : kWaves;
     s.slots = 0;
     s.grid = items < kMaxGrid ? (int)items : kMaxGrid;
@@ -1591,7 +1596,7 @@ void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
   if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
     if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
-    if constexpr (D == 128) draft_wide_kernel<F32, D, 1, 8, WHAT><<<s.grid, 512, 0, st>>>(a);
+    if constexpr (D == 128 && WHAT != W_CROSS) draft_wide_kernel<F32, D, 1, 8, WHAT><<<s.grid, 512, 0, st>>>(a);
   }
 }
 
@@ -1610,7 +1615,7 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   const size_t rows = s.slots > 0 || s.pieces > 1 ? (size_t)s.grid * s.trows : 0;
   a.po = ar.take<float>(rows ? rows * d : 64);
   a.pml = ar.take<float>(rows * 2);
-  a.plan = ar.take<int32_t>(1);
+  if (s.items) a.plan = ar.take<int32_t>(1);
   return a;
 }
 

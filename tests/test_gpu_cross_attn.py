@@ -116,6 +116,61 @@ def test_seen_infinities_and_nan_are_seen(rows, dtype):
     assert np.isnan(o.float().cpu().numpy()).all() and np.isnan(l.cpu().numpy()).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 1], [50, 3], [300, 9]])
+def test_infinities_in_the_last_state(rows, dtype):
+    """Rows behind the end are read as the last, or not at all: what it holds counts once."""
+    s = Encoded(16, [150, 1], rows, hq=2, hkv=1, d=128, dtype=dtype, spread=0.2)
+    s.v[s.table[0, 2], 0, 21, 5] = np.inf
+    s.v[s.table[1, 0], 0, 0, 9] = -np.inf
+    s.upload()
+    o, l = s.run()
+    got, n = o.float().cpu().numpy(), rows[0]
+    assert (got[:n, :, 5] == np.inf).all() and (got[n:, :, 9] == -np.inf).all()
+    assert np.isfinite(np.delete(got[:n], 5, 2)).all() and np.isfinite(np.delete(got[n:], 9, 2)).all() and np.isfinite(l.cpu().numpy()).all()
+    s.v = np.where(np.isfinite(s.v), s.v, 0).astype(np.float32)
+    s.upload()
+    o2, l2 = s.run()
+    check_rows(s, s.oracle(), o2, l2)
+    keep = np.ones((s.nrows, 1, 128), bool)
+    keep[:n, :, 5] = keep[n:, :, 9] = False
+    keep = np.broadcast_to(keep, got.shape)
+    assert np.array_equal(got[keep], o2.float().cpu().numpy()[keep])
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,rows,hide", [
+    (4, 1, 128, [20000, 100], [50, 3], None),            # 200 rows of one head: two tiles, many pieces
+    (4, 1, 64, [9000], [100], 0.5),
+    (2, 2, 128, [5000, 0, 700, 64], [70, 130, 1, 200], 0.1),
+    (8, 4, 128, [600] * 9, [20] * 9, None),              # 40 rows of 36 items
+    (8, 8, 64, [1200, 3, 513] * 6, [40] * 18, 0.3),      # 144 items of 40 rows
+    (16, 16, 128, [700] * 10, [1] * 10, None),           # 160 items of one row: one piece of eight waves
+    (16, 16, 64, [2000, 0, 17, 1025] * 2, [1] * 8, 0.2),
+    (8, 8, 128, [3000, 100] * 6, [1] * 12, None),        # 96 items: pieces of a quarter of a round, or of a whole
+    (8, 8, 128, [2900] * 12, [1] * 12, 0.1),
+])
+def test_plans_of_pieces(hq, hkv, d, lens, rows, hide):
+    s = Encoded(17, lens, rows, hq=hq, hkv=hkv, d=d, page=64, hide=hide, extra=1)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    untouched(s, o, l)
+
+
+def test_a_mask_of_exactly_the_capacity():
+    """32 nwords = cap = len: no word behind the mask's last is read (it ends its allocation's page of poison here)."""
+    import torch
+    for rows, dtype in (([3], "f32"), ([40], "f32"), ([300], "bf16"), ([40], "bf16"), ([1], "bf16")):
+        s = Encoded(18, [192], rows, hq=2, hkv=1, d=64, dtype=dtype, hide=0.3)
+        words = s.kmask.shape[1]
+        big = torch.zeros(2, words, dtype=torch.int32, device="cuda")
+        big[0] = s.dmask[0]
+        for fill in (0, -1):
+            big[1] = fill
+            s.cross = _rs.Cross(s.dq, max_rows=s.max_rows, start=s.dstart, kmask=big[:1])
+            o, l = s.run()
+            check_rows(s, s.oracle(), o, l)
+
+
 @pytest.mark.parametrize("rows", [[1, 2], [40, 7], [150, 300]])
 def test_pages_that_the_table_does_not_name(rows):
     s = Encoded(7, [400, 190], rows, hq=4, hkv=2, d=64, page=64, hide=0.1)
