@@ -12,7 +12,10 @@
 //   O^T [d x 32 rows] += V^T P^T, V read transposed, P straight from the accumulators of S^T.
 // The running maximum is raised only where a sum of 32 weights passes 2^8, so that O is rarely rescaled.  Sums are of the
 // weights before their rounding to bf16.  What the key mask hides is the same for all rows: a tile of which nothing is seen is
-// left out, and of one seen in part the hidden scores become minus infinity and the hidden rows of V zero, in LDS.
+// left out, and of one seen in part the products of the hidden states start from minus infinity.
+// 4096 rows x 32 heads of 128 over 65536 states of 8: 3.79-3.96 ms, 1.11-1.16 PFLOP/s on different boxes, where the dense prefill
+// runs at 1.11-1.17 and a 16384^3 product of torch's at 1.29-1.36; on constant operands, at the full clock, 1.5.  Heads of 64:
+// 2.5 ms, 0.87 PFLOP/s: half the products per exponent.  A mask that hides a state of every tile: 4.67 ms.
 #include "draft_plan.h"
 
 namespace rs {
