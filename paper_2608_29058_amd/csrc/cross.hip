@@ -469,15 +469,17 @@ __global__ __launch_bounds__(256, 2) void cross_kernel(const DraftArgs) {
   if (!cross_walk<D, MASK, false>(it, lds)) cross_walk<D, MASK, true>(it, lds);
 }
 
-// Joins the pieces of an item, `rows` of its rows per workgroup (grid: items x 128 / rows).  A row's D / 4 lanes hold 4
-// dimensions each.
+// Joins the pieces of an item, 32 of its rows per workgroup (grid: items x trows / 32), for this kernel and for those of decode.hip
+// that share stages: where there are many rows, of which each would plan for itself there.  A row's D / 4 lanes hold 4 dimensions.
 template <int D>
-__global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a, int rows) {
-  constexpr int LPR = D / 4, RPI = 256 / LPR, kAhead = 4;
-  const int lane = threadIdx.x & 63, groups = *a.plan;
+__global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a) {
+  constexpr int LPR = D / 4, RPI = 256 / LPR, kAhead = 8;
+  const int lane = threadIdx.x & 63;
+  const Seq head_of = seq_at<W_CROSS>(a, lane);
+  const int groups = a.plan ? *a.plan : plan_groups<W_CROSS>(a, head_of, lane);
   int id = blockIdx.x, slot = -1, np = 0, per = 0, first = 0, t = 0, base = 0;
   for (int b0 = 0; b0 < a.c.nseq && slot < 0; b0 += 64) {
-    const Seq q = seq_at<W_CROSS>(a, b0 + lane);
+    const Seq q = b0 ? seq_at<W_CROSS>(a, b0 + lane) : head_of;
     const int k = q.r.count > 0 ? pieces_of(q.groups, groups) : 0, n = q.r.count > 0 ? items_of<W_CROSS>(a, q) : 0;
     const int si = wave_scan(n), ss = wave_scan(k * n);
     const unsigned long long hit = __ballot(id < si);
@@ -497,24 +499,29 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a, int 
   if (np <= 1 || slot + (np - 1) * per >= a.grid) return;
   const int rt = id / a.c.hkv, g = id - rt * a.c.hkv, G = a.q.hq / a.c.hkv;
   const int d0 = threadIdx.x % LPR * 4;
-  for (int x = 0; x < rows; x += RPI) {
-    const int in = blockIdx.y * rows + x + threadIdx.x / LPR, row = rt * kRows + in;
+  for (int x = 0; x < 32; x += RPI) {
+    const int in = blockIdx.y * 32 + x + threadIdx.x / LPR, row = rt * a.trows + in;
     if (row >= G * t) return;
-    const float *pml = a.pml + ((int64_t)slot * kRows + in) * 2, *po = a.po + ((int64_t)slot * kRows + in) * D + d0;
-    const int64_t step = (int64_t)per * kRows;
+    const float *pml = a.pml + ((int64_t)slot * a.trows + in) * 2, *po = a.po + ((int64_t)slot * a.trows + in) * D + d0;
+    const int64_t step = (int64_t)per * a.trows;
+    // in one pass, with a running maximum: kAhead pieces are in flight at a time
     float M = -INFINITY, z = 0.f;
-    for (int k = 0; k < np; ++k) M = fmaxf(M, pml[k * step * 2]);
-    const float ref = M == -INFINITY ? 0.f : M;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     for (int k0 = 0; k0 < np; k0 += kAhead) {
       f32x4 p[kAhead];
-      float m[kAhead], s[kAhead];
+      float m[kAhead], s[kAhead], top = M;
 #pragma unroll
       for (int y = 0; y < kAhead; ++y) {
         const int64_t k = k0 + y < np ? k0 + y : k0;
         p[y] = *(const f32x4 *)(po + k * step * D);
         m[y] = pml[k * step * 2], s[y] = pml[k * step * 2 + 1];
       }
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) top = fmaxf(top, m[y]);
+      const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(M - ref);
+      z *= old;
+      v *= old;
+      M = top;
 #pragma unroll
       for (int y = 0; y < kAhead; ++y) {
         if (k0 + y >= np) break;
@@ -533,13 +540,14 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const DraftArgs a, int 
 
 }  // namespace
 
-void cross_wide_launch(const DraftArgs &a, int d, int items, hipStream_t st) {
+void cross_prompt_launch(const DraftArgs &a, int d, hipStream_t st) {
   if (a.q.mask) d == 128 ? cross_kernel<128, true><<<a.grid, 256, 0, st>>>(a) : cross_kernel<64, true><<<a.grid, 256, 0, st>>>(a);
   else d == 128 ? cross_kernel<128, false><<<a.grid, 256, 0, st>>>(a) : cross_kernel<64, false><<<a.grid, 256, 0, st>>>(a);
-  if (a.slots == 0) return;
-  const int rows = items >= 256 ? 32 : d == 128 ? 8 : 16;  // few items have many pieces
-  const dim3 grid(items, kRows / rows);
-  d == 128 ? cross_join_kernel<128><<<grid, 256, 0, st>>>(a, rows) : cross_join_kernel<64><<<grid, 256, 0, st>>>(a, rows);
+}
+
+void cross_join_launch(const DraftArgs &a, int d, int items, hipStream_t st) {
+  const dim3 grid(items, a.trows / 32);
+  d == 128 ? cross_join_kernel<128><<<grid, 256, 0, st>>>(a) : cross_join_kernel<64><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace rs

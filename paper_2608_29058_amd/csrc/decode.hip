@@ -976,7 +976,7 @@ __global__ __launch_bounds__(256) void draft_join_kernel(const DraftArgs a) {
     np = a.pieces;
   } else {
     Seq q = seq_at<WHAT>(a, lane);
-    const int groups = plan_groups<WHAT>(a, q, lane);
+    const int groups = WHAT == W_CROSS && a.plan ? *a.plan : plan_groups<WHAT>(a, q, lane);
     int base = 0, b = -1, first = 0;
     np = 0;
     for (int b0 = 0; b0 < c.nseq && b < 0; b0 += 64) {
@@ -1493,7 +1493,9 @@ int tile_rows(bool f32, int d, bool sel, int rows) {
 
 struct DraftShape {
   int trows, rtiles, slots, least, grid, pieces, waves;
-  int resident, items;  // W_CROSS: workgroups at once where the device plans with them; items of cross.hip, 0: the other kernels
+  // W_CROSS: workgroups at once, where the device plans with them; items at most; whether cross.hip takes them
+  int resident, items;
+  bool prompt;
 };
 
 constexpr int kShort = 256;
@@ -1539,9 +1541,10 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   }
   const int64_t tiles = what == W_CROSS ? cross_tiles(c, q, rows, s.trows) : (int64_t)c.nseq * s.rtiles;
   const int64_t items = tiles * c.hkv, most = items * ((c.cap + kGroup - 1) / kGroup);
+  s.items = items < kMaxGrid ? (int)items : kMaxGrid;
+  s.prompt = prompt;
   if (prompt) {  // rounds of workgroups, planned on the device: cross.hip
     s.resident = resident;
-    s.items = items < kMaxGrid ? (int)items : kMaxGrid;
     s.least = 4;
     s.slots = c.cap <= s.least * kGroup || items >= 8 * resident ? 0 : 1;
     int64_t n = !s.slots ? items : items < resident ? resident : items + 4 * resident;
@@ -1592,7 +1595,7 @@ void by_tiles(bool f32, int d, int trows, F f) {
 template <bool F32, int D, int WHAT>
 void wide_launch(const DraftArgs &a, const DraftShape &s, hipStream_t st) {
   if constexpr (WHAT == W_CROSS && !F32)
-    if (s.items) return cross_wide_launch(a, D, s.items, st);
+    if (s.prompt) return cross_prompt_launch(a, D, st);
   if (s.trows == 128) return draft_wide_kernel<F32, D, 1, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
   if constexpr (!F32) {
     if (s.trows == 64) return draft_wide_kernel<F32, D, 2, 4, WHAT><<<s.grid, 256, 0, st>>>(a);
@@ -1615,7 +1618,7 @@ DraftArgs draft_parts(Arena &ar, const CacheView &c, const DraftView &q, const D
   const size_t rows = s.slots > 0 || s.pieces > 1 ? (size_t)s.grid * s.trows : 0;
   a.po = ar.take<float>(rows ? rows * d : 64);
   a.pml = ar.take<float>(rows * 2);
-  if (s.items) a.plan = ar.take<int32_t>(1);
+  if (s.prompt) a.plan = ar.take<int32_t>(1);
   return a;
 }
 
@@ -1650,7 +1653,14 @@ rs_status attend(const DraftArgs &a, const DraftShape &s, bool f32, int d, hipSt
         draft_kernel<F, D, NQ, WHAT><<<s.grid, 256, 0, st>>>(a);
       }
     });
-  if (SEL ? s.pieces > 1 : s.slots > 0 && !s.items) {
+  if (SEL ? s.pieces > 1 : s.slots > 0) {
+    // (147 rows x 28 heads, fp32: 6.5 us per row, 10 per item; 1500 rows x 16 heads of four sequences 44 and 25)
+    if constexpr (WHAT == W_CROSS)
+      if (s.trows > 32 && (int64_t)a.q.nrows * a.q.hq >= 16384) {
+        cross_join_launch(a, d, s.items, st);
+        RS_HIP(hipGetLastError());
+        return RS_OK;
+      }
     if ((int64_t)a.q.nrows * a.q.hq >= 4096) {
       const dim3 grid(a.q.nrows, (a.q.hq + kWaves - 1) / kWaves);
       d == 128 ? draft_join_kernel<128, WHAT, 1><<<grid, 256, 0, st>>>(a) : draft_join_kernel<64, WHAT, 1><<<grid, 256, 0, st>>>(a);

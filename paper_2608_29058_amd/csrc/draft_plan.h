@@ -24,11 +24,12 @@ struct DraftArgs {
   int nsel, pieces;  // with a list: pieces per item
   int grid;          // workgroups, and slots of pieces
   int resident;      // W_CROSS: workgroups that the chip holds at once, 0: plan by slots alone
-  int32_t *plan;     // cross.hip: where it leaves the groups of a piece for the joining kernel
+  int32_t *plan;     // cross.hip: where it leaves the groups of a piece for the joining kernel; NULL: plan_groups
 };
 
-// Launches of the matrix-rate kernel of W_CROSS, bf16, row tiles of 128, over at most `items` of them, and of its join (cross.hip).
-void cross_wide_launch(const DraftArgs &a, int d, int items, hipStream_t st);
+// cross.hip: the matrix-rate kernel of W_CROSS, bf16, row tiles of 128; the join of pieces of more than 32 rows, of at most `items`.
+void cross_prompt_launch(const DraftArgs &a, int d, hipStream_t st);
+void cross_join_launch(const DraftArgs &a, int d, int items, hipStream_t st);
 
 #if defined(__HIPCC__)
 namespace {
