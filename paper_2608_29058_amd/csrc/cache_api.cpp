@@ -161,6 +161,7 @@ rs_status rs_cache_append_rope(const rs_cache *cache, const rs_rope *rope, const
   rs_status st;
   if ((st = check_append(cache, &c, k_new, v_new, sk_t, sk_h, sv_t, sv_h, start, nrows, max_rows)) != RS_OK) return st;
   if ((st = check_rope(rope, cache->d)) != RS_OK) return st;
+  if (nrows > 1 << 24) return fail(RS_ERR_UNSUPPORTED, "append: at most 16777216 rows to rotate");
   if (nrows == 0) return RS_OK;
   if (q && (st = check_rope_part(q, cache->dtype, cache->d, nrows, "append: q")) != RS_OK) return st;
   return append_rope_launch(c, cache->dtype, cache->d, *rope, k_new, v_new, sk_t, sk_h, sv_t, sv_h, q, pos, start, nrows, max_rows,

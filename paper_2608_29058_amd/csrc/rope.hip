@@ -123,21 +123,18 @@ struct Turner {
     x = u, y = v;
   }
   __device__ __forceinline__ void turn_raw(Raw<T> &r) const {
-    if (!some) return;  // (what stays keeps its bits)
+    if (!some) return;
     float f[16];
     r.get(f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (MODE == R_HALF) {
-        pair(e, f[e], f[8 + e]);
-      } else {
-        float u = f[2 * e], v = f[2 * e + 1];
-        pair(e, u, v);
-        f[2 * e] = turns(e) ? u : f[2 * e];
-        f[2 * e + 1] = turns(e) ? v : f[2 * e + 1];
-      }
-    }
-    r.set(f);
+    for (int e = 0; e < 8; ++e) MODE == R_HALF ? pair(e, f[e], f[8 + e]) : pair(e, f[2 * e], f[2 * e + 1]);
+    Raw<T> y;
+    y.set(f);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w)  // what stays keeps its bits, those of a NaN too
+        r.x[k][w] = MODE == R_HALF || turns((4 * k + w) * 8 / (4 * NV)) ? y.x[k][w] : r.x[k][w];
   }
   // Rows of one position: heads h0, h0 + step, ... below `end`, N of them loaded before any is stored.  N = 2 (16 registers)
   // where the heads lie together; apart, one, whose 48 registers leave room for eight waves per SIMD (131072 rows of 32 + 8 heads of
@@ -301,11 +298,12 @@ RopePart part_of(const rs_rope_part &p, int e) {
 // log2 of the groups of heads that share a row.  Where a token's heads lie together a workgroup takes one row, a head per
 // group, so that it reads and writes long pieces of memory; where a head's tokens do, one group with a row per LPR lanes does,
 // split further only until the rows fill the chip's 2^19 lanes.  (32768 rows of 32 + 2 x 8 heads of 128 appended: 137 us, with
-// 8 groups 140 and with one 157; 30001 rows of 32 + 8, half of each turned: 124, 127, 135.)
+// 8 groups 140 and with one 157; 30001 rows of 32 + 8, half of each turned: 124, 127, 135.)  A launch has fewer than 2^32
+// lanes, which 2^24 rows in groups of their own would pass.
 int head_groups(int64_t rows, int d, int heads, bool tokens) {
   const int most = d == 128 ? 5 : 6;
   int lg = 0;
-  while (lg < most && (1 << lg) < heads && (tokens || rows * (d / 16) << lg < 1 << 19)) ++lg;
+  while (lg < most && (1 << lg) < heads && rows * (d / 16) << lg < (tokens ? 1ll << 31 : 1ll << 19)) ++lg;
   return lg;
 }
 

@@ -164,3 +164,23 @@ def test_without_starts_a_replayed_graph_of_steps():
         torch.cuda.synchronize()
         assert torch.equal(bits(s.dk), bits(want)) and torch.equal(bits(out), bits(rq))
         assert seen.tolist() == [step + 1, 1031 + step, 64 + step]
+
+
+def test_the_most_rows():
+    """2^24 rows of 64 heads, of which the cache has room for 128; heads share their rows."""
+    import torch
+    n, d, hkv, cap = 1 << 24, 64, 64, 128
+    k = torch.zeros(n, 1, d, dtype=torch.bfloat16, device="cuda")
+    k[:200] = torch.randn(200, 1, d, generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+    rot = Rot(64)
+    got = []
+    for m in (n, 200):
+        x = k[:m].expand(m, hkv, d)
+        dk, dv = (torch.full((1, hkv, cap, d), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        c = _rs.KvCache(dk, dv, torch.full((1,), 7, dtype=torch.int32, device="cuda"))
+        _rs.rs_cache_append_rope(c, rot.rope, x, x, max_rows=m)
+        assert torch.equal(dv[0, :, 7:], k[:cap - 7, 0].expand(hkv, cap - 7, d)) and (dk[0, :, :7] == 3).all()
+        got.append(dk)
+    assert torch.equal(*got)
+    want, ab = rot.oracle(k[:cap - 7].double().cpu().numpy(), 7 + np.arange(cap - 7))
+    check(got[0][0, 5, 7:, None].double().cpu().numpy(), want, ab, "bf16", rot, [cap])

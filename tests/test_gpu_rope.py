@@ -187,3 +187,17 @@ def test_no_rows_another_stream_and_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(bits(y), bits(turn(rot, x, pos0=11 * k)))
+
+
+@pytest.mark.parametrize("d,dim", [(128, 2), (128, 10), (128, 126), (64, 20), (64, 62)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_what_does_not_turn_keeps_the_bits_of_any_nan(d, dim, inter):
+    import torch
+    x, _ = rows(dim, 9, 3, d, "bf16")
+    bits(x)[..., dim::2] = 0x7f81  # a NaN that an arithmetic instruction would change
+    bits(x)[..., dim + 1::2] = -(1 << 15) + 0x7fa5
+    rot = Rot(dim, inter)
+    got = turn(rot, x, pos0=5)
+    assert torch.equal(bits(got[..., dim:]), bits(x[..., dim:])) and not got[..., :dim].isnan().any()
+    same = x.clone()
+    assert torch.equal(bits(turn(rot, same, pos0=5, y=same)), bits(got))

@@ -142,6 +142,7 @@ def test_rotated_appends_are_refused():
     for kw in BAD_PARTS:
         assert call(q=kw) == INV, kw
     assert call(n=0) == _rs.RS_OK and call(n=0, kn=None, q=dict(x=None)) == _rs.RS_OK
+    assert call(n=(1 << 24) + 1) == UNS
 
 
 def cross(**kw):
