@@ -13,9 +13,11 @@
 // The running maximum is raised only where a sum of 32 weights passes 2^8, so that O is rarely rescaled.  Sums are of the
 // weights before their rounding to bf16.  What the key mask hides is the same for all rows: a tile of which nothing is seen is
 // left out, and of one seen in part the products of the hidden states start from minus infinity.
-// 4096 rows x 32 heads of 128 over 65536 states of 8: 3.79-3.96 ms, 1.11-1.16 PFLOP/s on different boxes, where the dense prefill
-// runs at 1.11-1.17 and a 16384^3 product of torch's at 1.29-1.36; on constant operands, at the full clock, 1.5.  Heads of 64:
-// 2.5 ms, 0.87 PFLOP/s: half the products per exponent.  A mask that hides a state of every tile: 4.67 ms.
+// 4096 rows x 32 heads of 128 over 65536 states of 8: 3.75-3.96 ms, 1.11-1.17 PFLOP/s, where the dense prefill runs at 1.11-1.17 and
+// a 16384^3 product of torch's at 1.29-1.36: the matrix instructions are at work in 62 % of the cycles, the exponents (two vector
+// instructions and a half per score) in most of the others, and the clock falls to 1.75 GHz; on constant operands, at the full clock, 1.5.
+// Heads of 64: 2.36 ms, 0.93 PFLOP/s: half the products per exponent.  A mask that hides a state of every tile: 4.41 ms; one that
+// hides nothing 4.00.
 #include "draft_plan.h"
 
 namespace rs {
@@ -52,9 +54,9 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Groups per piece.  The chip works in rounds of `resident` workgroups, so that the time is about that of the rounds' pieces
-// and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us).  Of pieces
-// of the longest sequence's whole, 1/2, 1/3, 1/4, 1/6, 1/9, 1/13 .. the fastest.
+// Groups per piece.  The chip works in rounds of `resident` workgroups, so that the time is about that of the rounds' longest pieces
+// and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us).  For each
+// number of rounds the shortest pieces that fit are found; of those, and of whole items, the fastest are taken.
 __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first, int lane) {
   if (a.slots == 0) return kMaxN;  // one piece each
   auto all = [&](auto f) {  // sum over the sequences
@@ -63,21 +65,32 @@ __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first,
     return wave_sum(x);
   };
   const int items = all([&](const Seq &q) { return items_of<W_CROSS>(a, q); });
+  const int work = all([&](const Seq &q) { return items_of<W_CROSS>(a, q) * q.groups; });
   int longest = first.groups;
   for (int b0 = 64; b0 < a.c.nseq; b0 += 64) longest = larger(longest, seq_at<W_CROSS>(a, b0 + lane).groups);
   longest = wave_most(longest);
-  const auto rounds = [&](int n) { return (n + a.resident - 1) / a.resident; };
-  int best = kMaxN, cost = rounds(items) * longest * 128;
-  for (int k = 2; k < kMaxN / kGroup; k += k < 4 ? 1 : k / 2) {
-    const int per = (longest + k - 1) / k;
-    if (per < a.least) break;
-    const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^10: ceil by the product, less half a step)
-    const int n = all([&](const Seq &q) {
-      return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
-    });
-    const int c = rounds(n) * per * 128 + n;
-    if (n > a.grid) break;
-    if (c < cost) cost = c, best = per;
+  const int fewest = (items + a.resident - 1) / a.resident;
+  int best = kMaxN, cost = fewest * longest * 128;
+  for (int r = fewest > 0 ? fewest : 1; r < fewest + 4 && r * a.resident <= a.grid; ++r) {
+    const int room = r * a.resident;
+    int lo = (work + room - 1) / room;
+    lo = larger(lo, a.least);
+    if (r * lo * 128 + items >= cost) continue;
+    // (an item of n groups has less than n / per + 1 pieces)
+    int hi = room > items ? (work + room - items - 1) / (room - items) : longest, n = items;
+    hi = larger(lo, hi < longest ? hi : longest);
+    while (true) {
+      const int per = (lo + hi) >> 1;
+      const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^11: ceil by the product, less half a step)
+      n = all([&](const Seq &q) {
+        return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
+      });
+      if (lo >= hi) break;
+      if (n <= room) hi = per;
+      else lo = per + 1;
+    }
+    const int c = r * lo * 128 + n;
+    if (n <= room && c < cost) cost = c, best = lo;
   }
   return best;
 }
