@@ -71,23 +71,27 @@ __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first,
   longest = wave_most(longest);
   const int fewest = (items + a.resident - 1) / a.resident;
   int best = kMaxN, cost = fewest * longest * 128;
+  const auto pieces = [&](int per) {
+    const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^11: ceil by the product, less half a step)
+    return all([&](const Seq &q) {
+      return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
+    });
+  };
   for (int r = fewest > 0 ? fewest : 1; r < fewest + 4 && r * a.resident <= a.grid; ++r) {
     const int room = r * a.resident;
-    int lo = (work + room - 1) / room;
-    lo = larger(lo, a.least);
-    if (r * lo * 128 + items >= cost) continue;
-    // (an item of n groups has less than n / per + 1 pieces)
-    int hi = room > items ? (work + room - items - 1) / (room - items) : longest, n = items;
-    hi = larger(lo, hi < longest ? hi : longest);
-    while (true) {
-      const int per = (lo + hi) >> 1;
-      const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^11: ceil by the product, less half a step)
-      n = all([&](const Seq &q) {
-        return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
-      });
-      if (lo >= hi) break;
-      if (n <= room) hi = per;
-      else lo = per + 1;
+    int lo = larger((work + room - 1) / room, a.least);
+    if (r * lo * 128 + larger(items, work / lo) >= cost) continue;
+    int n = pieces(lo);
+    if (n > room) {
+      // (an item of n groups has less than n / per + 1 pieces)
+      int hi = room > items ? (work + room - items - 1) / (room - items) : longest;
+      hi = hi < longest ? hi : longest;
+      for (++lo; lo < hi;) {
+        const int per = (lo + hi) >> 1;
+        if (pieces(per) <= room) hi = per;
+        else lo = per + 1;
+      }
+      n = pieces(lo);
     }
     const int c = r * lo * 128 + n;
     if (n <= room && c < cost) cost = c, best = lo;
