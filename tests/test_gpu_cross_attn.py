@@ -117,6 +117,47 @@ def test_seen_infinities_and_nan_are_seen(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 1], [9, 2], [50, 3], [300, 9]])
+def test_infinities_in_the_first_seen_state_of_a_tile(rows, dtype):
+    """Hidden states may be read as another: what it holds counts once."""
+    s = Encoded(18, [300, 40], rows, hq=2, hkv=1, d=128, dtype=dtype, spread=0.2, hide=0.6)
+    see = np.unpackbits(s.kmask.view(np.uint8), axis=1, bitorder="little").astype(bool)
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    dims = []
+    for i, j0 in enumerate(range(0, 288, 32)):
+        j = j0 + int(np.argmax(see[0, j0:j0 + 32]))
+        assert see[0, j]
+        s.v[s.table[0, j // 64], 0, j % 64, i] = np.inf
+        dims.append(i)
+    s.upload()
+    o2, l2 = s.run()
+    got, n = o2.float().cpu().numpy(), rows[0]
+    assert (got[:n][..., dims] == np.inf).all()
+    got[:n][..., dims] = 0
+    want = o.float().cpu().numpy()
+    want[:n][..., dims] = 0
+    assert np.array_equal(got, want) and np.array_equal(l.cpu().numpy(), l2.cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 1, 1], [9, 2, 1], [50, 3, 7], [300, 9, 100]])
+def test_hidden_stretches(rows, dtype):
+    """Masks that hide whole tiles and pages: a beginning, a middle, all but one state, padding behind an end."""
+    s = Encoded(19, [700, 700, 700], rows, hq=4, hkv=2, d=64, dtype=dtype, hide=0.0)
+    see = np.ones((3, s.kmask.shape[1] * 32), bool)
+    see[0, 31:97] = see[0, 128:513] = False
+    see[1, :] = False
+    see[1, 650] = True
+    see[2, 201:] = False
+    s.kmask = np.packbits(see, axis=1, bitorder="little").view(np.int32)
+    s.upload()
+    o, l = s.run()
+    check_rows(s, s.oracle(), o, l)
+    untouched(s, o, l)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [[1, 1], [50, 3], [300, 9]])
 def test_infinities_in_the_last_state(rows, dtype):
     """Rows behind the end are read as the last, or not at all: what it holds counts once."""
