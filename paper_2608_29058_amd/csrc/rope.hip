@@ -5,8 +5,8 @@
 // Every element is read and written once, so memory bounds both calls (and the launch the short ones).  A lane takes 8
 // pairs of a row, two vectors of 16 bytes (four in fp32); the workgroup computes each cosine and sine of its rows once, into
 // LDS, for all heads, so that they cost little beside the copying: no table of them is read from memory, and positions have
-// no upper end.  131072 rows of 32 + 8 heads of 128 in bf16: 471 us, 5.7 TB/s (a large copy: 5.0); a step's few rows: the
-// launch.
+// no upper end.  131072 rows of 32 + 8 heads of 128 in bf16: 492 us, 5.5 TB/s (a large copy: 5.15); a step's few rows:
+// the launch.
 #include "rope.h"
 #include "cache.h"
 
@@ -34,7 +34,7 @@ __device__ __forceinline__ void turn(double t, float &c, float &s) {
 // of 32 heads of 64 35 -> 26 us, 224 MiB of bf16 rows 90 -> 69 us, 90 -> 86 where other rows were read since.  Inputs beyond that
 // size are read past them too (NTL): nothing of them is left there, and what is there may be of use (1 GiB between two passes of
 // another kernel over it: 404 -> 349 us); smaller ones not (96 MiB: 31 -> 35 us), nor where an instruction reads half
-// lines, which would be fetched twice (30001 rows of 32 + 8 heads, half of each turned: 122 -> 133 us).
+// lines, which would be fetched twice (30001 rows of 32 + 8 heads, with lanes that read so: 122 -> 133 us).
 template <bool NTL>
 __device__ __forceinline__ u32x4 load16(const char *p) {
   if constexpr (NTL) return __builtin_nontemporal_load((const u32x4 *)p);
@@ -72,99 +72,107 @@ struct Raw {
   }
 };
 
-// How the pairs of a row lie in a lane's vectors: neighbouring lanes take neighbouring vectors, so that an instruction
-// reads whole lines (with a lane's 16 elements in one piece, 8191 fp32 rows of 32 heads of 64: 57 us; so, 35).
-//   R_HALF   dim a multiple of 16: the dim / 16 first lanes hold vectors of the first half, then those of the second at the
-//            same places (pair e in elements e and 8 + e); the others hold 16 elements that stay as they are;
-//   R_INTER  vectors of the row, LPR apart: pair e in elements 2e and 2e + 1; pairs from dim / 2 on stay;
-//   R_ANY    half layout of any even dim: elements one by one, pair 8l + e in elements 8l + e and dim / 2 + 8l + e, and
-//            from pair dim / 2 on, two neighbours that stay.
-enum { R_HALF = 0, R_INTER = 1, R_ANY = 2 };
+constexpr int kThreads = 256;
+
+// Neighbouring lanes take neighbouring vectors of a row, LPR apart, so that an instruction moves whole lines (with a lane's 16
+// elements in one piece, 8191 fp32 rows of 32 heads of 64: 57 us; so, 35).  Where the pairs of a row are then:
+//   R_HALF   half layout of the whole head: both in the lane, elements x and 8 + x;
+//   R_INTER  interleaved: neighbours; pairs from dim / 2 on stay;
+//   R_PART   half layout of a part of the head whose half is made of vectors: the other of each pair in another lane's vector, which
+//            passes through LDS (79652 rows of 32 + 8 heads of 128, 32 of each rotated: 297 us, with lanes that read both halves of
+//            their pairs, and so parts of lines, 816);
+//   R_ANY    half layout of any even dim: the same, element by element (43998 rows of 64 + 8 heads of 128, 126 of each rotated: 331 us, with elements from
+//            memory 1100).
+enum { R_HALF = 0, R_INTER = 1, R_PART = 2, R_ANY = 3 };
 
 // A lane's cosines and sines and its places in a row.
 template <typename T, int MODE, int LPR>
 struct Turner {
-  static constexpr int V = Raw<T>::V, NV = Raw<T>::NV;
-  float c[8], s[8];
+  static constexpr bool STAGED = MODE == R_PART || MODE == R_ANY;
+  static constexpr int V = Raw<T>::V, NV = Raw<T>::NV, E = sizeof(T), NC = STAGED ? 16 : 8;
+  static constexpr int kStage = STAGED ? kThreads * 16 * E / 4 : 0;  // floats of LDS
+  float c[NC], s[NC];  // of each pair (STAGED: of each element, the sine with the sign that it has there)
   int l, dim;
-  bool some;    // R_HALF: the lane's elements turn
-  int off[NV];  // byte offsets of its vectors
+  int mate[MODE == R_ANY ? 16 : NV];  // STAGED: byte offset of the other element of a pair, R_PART: of a vector of them
+  char *stage;                        // STAGED: the row in LDS
 
-  __device__ __forceinline__ Turner(int lane, int rot) : l(lane), dim(rot) {
-    const int q = dim >> 4;
-    some = MODE != R_HALF || l < q;
+  __device__ __forceinline__ Turner(int lane, int rot, char *lds) : l(lane), dim(rot), stage(lds) {
+    if constexpr (MODE == R_PART)
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      int i = l + k * LPR;
-      if constexpr (MODE == R_HALF) {
-        const int kk = k % (NV / 2);
-        i = some ? l + kk * q + (k >= NV / 2 ? (dim >> 1) / V : 0) : dim / V + (l - q) + k * (LPR - q);
-      }
-      off[k] = 16 * i;
-    }
+      for (int k = 0; k < NV; ++k) mate[k] = E * mate_of(V * (l + k * LPR));
+    if constexpr (MODE == R_ANY)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) mate[x] = E * mate_of(element(x));
   }
-  // the pair whose turn is c[e], s[e]
+  __device__ __forceinline__ int off(int k) const { return 16 * (l + k * LPR); }
+  __device__ __forceinline__ int element(int x) const { return V * (l + x / V * LPR) + x % V; }
+  __device__ __forceinline__ int mate_of(int i) const { return i >= dim ? i : i < dim >> 1 ? i + (dim >> 1) : i - (dim >> 1); }
+  // R_HALF, R_INTER: the pair whose turn is c[e], s[e]
   __device__ __forceinline__ int pair_of(int e) const {
-    if constexpr (MODE == R_HALF) return V * (l + e / V * (dim >> 4)) + e % V;
     if constexpr (MODE == R_INTER) return V / 2 * (l + e / (V / 2) * LPR) + e % (V / 2);
-    return 8 * l + e;
+    return element(e);
   }
-  __device__ __forceinline__ bool turns(int e) const { return MODE == R_HALF ? some : pair_of(e) < dim >> 1; }
   // the lane's pairs from the row's table of cosines, then sines
   __device__ __forceinline__ void take(const float *row) {
+    const int half = dim >> 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = turns(e) ? pair_of(e) : 0;
-      c[e] = row[i], s[e] = row[8 * LPR + i];
+    for (int e = 0; e < NC; ++e) {
+      int i = STAGED ? element(e) : pair_of(e);
+      const bool first = !STAGED || i < half;
+      i = STAGED && !first ? i - half : i;
+      i = i < half ? i : 0;
+      c[e] = row[i], s[e] = STAGED && first ? -row[8 * LPR + i] : row[8 * LPR + i];
     }
   }
   __device__ __forceinline__ void pair(int e, float &x, float &y) const {
     const float u = x * c[e] - y * s[e], v = y * c[e] + x * s[e];
     x = u, y = v;
   }
-  __device__ __forceinline__ void turn_raw(Raw<T> &r) const {
-    if (!some) return;
+  __device__ __forceinline__ void turn_raw(Raw<T> &r, const bool (&move)[NV]) const {
     float f[16];
     r.get(f);
+    if constexpr (STAGED) {
+      // a row's lanes are of one wave, whose accesses of LDS follow each other
 #pragma unroll
-    for (int e = 0; e < 8; ++e) MODE == R_HALF ? pair(e, f[e], f[8 + e]) : pair(e, f[2 * e], f[2 * e + 1]);
+      for (int k = 0; k < NV; ++k)
+        if (move[k]) *(u32x4 *)(stage + off(k)) = r.x[k];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+      float g[16];
+      if constexpr (MODE == R_PART) {
+        Raw<T> o;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) o.x[k] = *(const u32x4 *)(stage + mate[k]);
+        o.get(g);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) g[x] = (float)*(const T *)(stage + mate[x]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+#pragma unroll
+      for (int x = 0; x < 16; ++x) f[x] = f[x] * c[x] + g[x] * s[x];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) MODE == R_HALF ? pair(e, f[e], f[8 + e]) : pair(e, f[2 * e], f[2 * e + 1]);
+    }
     Raw<T> y;
     y.set(f);
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int w = 0; w < 4; ++w)  // what stays keeps its bits, those of a NaN too
-        r.x[k][w] = MODE == R_HALF || turns((4 * k + w) * 8 / (4 * NV)) ? y.x[k][w] : r.x[k][w];
+      for (int w = 0; w < 4; ++w)  // what stays keeps its bits, those of a NaN too (dim is even: a word of two bf16 turns or stays)
+        r.x[k][w] = MODE == R_HALF || V * (l + k * LPR) + w * (V / 4) < dim ? y.x[k][w] : r.x[k][w];
   }
   // Rows of one position: heads h0, h0 + step, ... below `end`, N of them loaded before any is stored.  N = 2 (16 registers)
   // where the heads lie together; apart, one, whose 48 registers leave room for eight waves per SIMD (131072 rows of 32 + 8 heads of
-  // 128: 471 us, with the registers of four 551).  skip: y is x, and vectors that stay need not move.
+  // 128: 492 us, with four 551).  skip: y is x, and vectors that stay need not move.
   template <int N, bool NTL>
-  __device__ __forceinline__ void rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, int end, int d, bool skip) const {
-    if constexpr (MODE == R_ANY) {
-      for (int h = h0; h < end; h += step) {
-        const T *xr = (const T *)(x + h * sx);
-        T *yr = (T *)(y + h * sy);
+  __device__ __forceinline__ void rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, int end, bool skip) const {
+    bool move[NV];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = 8 * l + e, half = dim >> 1;
-          if (i >= half && skip) continue;
-          const int ia = i < half ? i : 2 * i, ib = i < half ? half + i : 2 * i + 1;
-          const T xa = xr[ia], xb = xr[ib];
-          float a = (float)xa, b = (float)xb;
-          pair(e, a, b);
-          yr[ia] = i < half ? (T)a : xa;
-          yr[ib] = i < half ? (T)b : xb;
-        }
-      }
-    } else {
-      bool move[NV];
-#pragma unroll
-      for (int k = 0; k < NV; ++k) move[k] = !skip || (MODE == R_HALF ? some : off[k] < dim * (int)sizeof(T));
-      for (; h0 + (N - 1) * step < end; h0 += N * step) some_rows<N, NTL>(x, y, sx, sy, h0, step, move);
-      if constexpr (N > 1)
-        for (; h0 < end; h0 += step) some_rows<1, NTL>(x, y, sx, sy, h0, step, move);
-    }
+    for (int k = 0; k < NV; ++k) move[k] = MODE == R_HALF || !skip || off(k) < dim * E;
+    for (; h0 + (N - 1) * step < end; h0 += N * step) some_rows<N, NTL>(x, y, sx, sy, h0, step, move);
+    if constexpr (N > 1)
+      for (; h0 < end; h0 += step) some_rows<1, NTL>(x, y, sx, sy, h0, step, move);
   }
   template <int N, bool NTL>
   __device__ __forceinline__ void some_rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, const bool (&move)[NV]) const {
@@ -174,20 +182,19 @@ struct Turner {
       const char *p = x + (h0 + n * step) * sx;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (move[k]) r[n].x[k] = load16<NTL>(p + off[k]);
+        if (move[k]) r[n].x[k] = load16<NTL>(p + off(k));
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      turn_raw(r[n]);
+      turn_raw(r[n], move);
       char *p = y + (h0 + n * step) * sy;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (move[k]) store16(p + off[k], r[n].x[k]);
+        if (move[k]) store16(p + off(k), r[n].x[k]);
     }
   }
 };
 
-constexpr int kThreads = 256;
 constexpr int64_t kSideCache = 256ll << 20;  // bytes of the memory-side cache
 
 struct RopePart {
@@ -200,7 +207,7 @@ struct RopePart {
 struct RopeArgs {
   rs_rope rope;
   RopePart part[4];
-  int nparts, n, d, lg;  // 1 << lg: groups of heads that share a row
+  int nparts, n, lg;  // 1 << lg: groups of heads that share a row
   const int32_t *pos;
   int64_t pos0;
   bool back;
@@ -225,7 +232,7 @@ __device__ __forceinline__ void angle_table(float *tab, const rs_rope &r, int ro
 // A workgroup takes 256 / (lanes of a row x groups) rows.
 template <typename T, int MODE, int LPR, int N, bool NTL>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
-  __shared__ float tab[kThreads * 16];
+  __shared__ __align__(16) float tab[kThreads * 16 + Turner<T, MODE, LPR>::kStage];
   const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
   const int r0 = blockIdx.x * rows, r = r0 + (x >> a.lg);
   angle_table<LPR>(tab, a.rope, rows, a.back, [&](int i) {
@@ -233,12 +240,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs a) {
     return (double)(a.pos ? (int64_t)a.pos[at] : a.pos0 + at);
   });
   if (r >= a.n) return;
-  Turner<T, MODE, LPR> t(l, a.rope.dim);
+  Turner<T, MODE, LPR> t(l, a.rope.dim, (char *)(tab + kThreads * 16) + x * LPR * 16 * (int)sizeof(T));
   t.take(tab + (r - r0) * 16 * LPR);
   int first = g;  // heads of all parts one after the other are dealt to the groups
   for (int k = 0; k < a.nparts; ++k) {
     const RopePart &p = a.part[k];
-    t.template rows<N, NTL>(p.x + r * p.sx_t, p.y + r * p.sy_t, p.sx_h, p.sy_h, first, groups, p.heads, a.d, p.inplace);
+    t.template rows<N, NTL>(p.x + r * p.sx_t, p.y + r * p.sy_t, p.sx_h, p.sy_h, first, groups, p.heads, p.inplace);
     first = (first - p.heads) & (groups - 1);
   }
 }
@@ -250,13 +257,13 @@ struct AppendRopeArgs {
   int64_t skt, skh, svt, svh;  // bytes
   RopePart q;                  // heads 0: none
   const int32_t *pos, *start;
-  int nrows, max_rows, d, lg;
+  int nrows, max_rows, lg;
 };
 
 // As rope_kernel, a sequence's rows: heads of K with those of V, then of Q.
 template <typename T, int MODE, int LPR, int N, bool NTL>
 __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeArgs a) {
-  __shared__ float tab[kThreads * 16];
+  __shared__ __align__(16) float tab[kThreads * 16 + Turner<T, MODE, LPR>::kStage];
   const CacheView &c = a.c;
   const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
   const int b = blockIdx.y, i0 = blockIdx.x * rows, i = i0 + (x >> a.lg);
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeA
   });
   if (i >= rr.count) return;
   const int64_t row = rr.first + i;
-  Turner<T, MODE, LPR> t(l, a.rope.dim);
+  Turner<T, MODE, LPR> t(l, a.rope.dim, (char *)(tab + kThreads * 16) + x * LPR * 16 * (int)sizeof(T));
   t.take(tab + (i - i0) * 16 * LPR);
   const int64_t j = (int64_t)len + i;
   const int p = j < c.cap ? page_of(c, (int)j) : 0, id = j < c.cap ? page_id(c, b, p) : -1;
@@ -281,14 +288,14 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeA
       Raw<T> v;
 #pragma unroll
       for (int k = 0; k < Raw<T>::NV; ++k) v.x[k] = load16<NTL>(vr + h * a.svh + 16 * (l + k * LPR));
-      t.template rows<1, NTL>(kr, c.k + ko, a.skh, c.sk_h, h, groups, h + 1, a.d, false);
+      t.template rows<1, NTL>(kr, c.k + ko, a.skh, c.sk_h, h, groups, h + 1, false);
 #pragma unroll
       for (int k = 0; k < Raw<T>::NV; ++k) store16(c.v + vo + h * c.sv_h + 16 * (l + k * LPR), v.x[k]);
       if (c.acc && l == 0) c.acc[((int64_t)b * c.hkv + h) * c.cap + j] = 0.f;
     }
   }
   const int first = (g - c.hkv) & (groups - 1);
-  t.template rows<N, NTL>(a.q.x + row * a.q.sx_t, a.q.y + row * a.q.sy_t, a.q.sx_h, a.q.sy_h, first, groups, a.q.heads, a.d, a.q.inplace);
+  t.template rows<N, NTL>(a.q.x + row * a.q.sx_t, a.q.y + row * a.q.sy_t, a.q.sx_h, a.q.sy_h, first, groups, a.q.heads, a.q.inplace);
 }
 
 RopePart part_of(const rs_rope_part &p, int e) {
@@ -312,25 +319,21 @@ template <typename F>
 void by_shape(int dtype, int d, const rs_rope &r, bool tokens, int64_t bytes, F f) {
   using std::integral_constant;
   auto with_n = [&](auto t, auto m, auto l) {
-    constexpr int M = decltype(m)::value, L = decltype(l)::value, many = sizeof(t) == 2 ? 2 : 1;
-    if constexpr (M == R_ANY) {
-      f(t, m, l, integral_constant<int, 1>{}, std::false_type{});
-    } else {
-      const bool lines = L == 8 && (M == R_INTER || r.dim == d);  // a row's lanes read whole lines of 128 bytes
-      auto with_l = [&](auto n) {
-        if constexpr (L == 8)
-          if (lines && bytes > kSideCache) return f(t, m, l, n, std::true_type{});
-        f(t, m, l, n, std::false_type{});
-      };
-      tokens ? with_l(integral_constant<int, many>{}) : with_l(integral_constant<int, 1>{});
-    }
+    constexpr int L = decltype(l)::value, many = sizeof(t) == 2 ? 2 : 1;
+    auto with_l = [&](auto n) {
+      if constexpr (L == 8)  // a row's lanes read whole lines of 128 bytes
+        if (bytes > kSideCache) return f(t, m, l, n, std::true_type{});
+      f(t, m, l, n, std::false_type{});
+    };
+    tokens ? with_l(integral_constant<int, many>{}) : with_l(integral_constant<int, 1>{});
   };
   auto with_l = [&](auto t, auto m) {
     d == 128 ? with_n(t, m, integral_constant<int, 8>{}) : with_n(t, m, integral_constant<int, 4>{});
   };
   auto with_m = [&](auto t) {
     if (r.layout == RS_ROPE_INTERLEAVED) with_l(t, integral_constant<int, R_INTER>{});
-    else if (r.dim % 16 == 0) with_l(t, integral_constant<int, R_HALF>{});
+    else if (r.dim == d) with_l(t, integral_constant<int, R_HALF>{});
+    else if (r.dim % (32 / (int)sizeof(t)) == 0) with_l(t, integral_constant<int, R_PART>{});
     else with_l(t, integral_constant<int, R_ANY>{});
   };
   dtype == RS_BF16 ? with_m(bf16{}) : with_m(float{});
@@ -342,7 +345,7 @@ rs_status rope_launch(const rs_rope &rope, const rs_rope_rows &rows, bool transp
   const int e = rows.dtype == RS_BF16 ? 2 : 4;
   RopeArgs a{};
   a.rope = rope;
-  a.nparts = rows.nparts, a.n = rows.n, a.d = rows.d, a.pos = rows.pos, a.pos0 = rows.pos0, a.back = transpose;
+  a.nparts = rows.nparts, a.n = rows.n, a.pos = rows.pos, a.pos0 = rows.pos0, a.back = transpose;
   int heads = 0;
   for (int k = 0; k < rows.nparts; ++k) {
     a.part[k] = part_of(rows.part[k], e);
@@ -369,7 +372,7 @@ rs_status append_rope_launch(const CacheView &c, int dtype, int d, const rs_rope
   a.kn = (const char *)kn, a.vn = (const char *)vn;
   a.skt = skt * e, a.skh = skh * e, a.svt = svt * e, a.svh = svh * e;
   if (q) a.q = part_of(*q, e);
-  a.pos = pos, a.start = start, a.nrows = nrows, a.max_rows = max_rows, a.d = d;
+  a.pos = pos, a.start = start, a.nrows = nrows, a.max_rows = max_rows;
   const int most = max_rows < nrows ? max_rows : nrows;  // rows of a sequence at most
   const int64_t all = (int64_t)c.nseq * most;
   const bool tokens = skh < skt;
