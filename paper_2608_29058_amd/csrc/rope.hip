@@ -303,12 +303,13 @@ RopePart part_of(const rs_rope_part &p, int e) {
 }
 
 // log2 of the groups of heads that share a row.  Where a token's heads lie together a workgroup takes one row, a head per
-// group, so that it reads and writes long pieces of memory; where a head's tokens do, one group with a row per LPR lanes does,
-// split further only until the rows fill the chip's 2^19 lanes.  (32768 rows of 32 + 2 x 8 heads of 128 appended: 137 us, with
-// 8 groups 140 and with one 157; 30001 rows of 32 + 8, half of each turned: 124, 127, 135.)  A launch has fewer than 2^32
-// lanes, which 2^24 rows in groups of their own would pass.
-int head_groups(int64_t rows, int d, int heads, bool tokens) {
-  const int most = d == 128 ? 5 : 6;
+// group, so that it reads and writes long pieces of memory, or two rows where pairs pass through LDS, so that a group has a second
+// head to load meanwhile; where a head's tokens lie together, one group with a row per LPR lanes does, split further only until the rows
+// fill the chip's 2^19 lanes.  (8192 rows of 32 + 2 x 8 heads of 128 appended to four sequences each: one row 133 us, two 133, four 139;
+// 30001 rows of 32 + 8: 96, 97, 101; half of each turned: 131, 104, 105.)  A launch has fewer than 2^32 lanes, which 2^24 rows in groups
+// of their own would pass.
+int head_groups(int64_t rows, int d, int heads, bool tokens, const rs_rope &r) {
+  const int most = (d == 128 ? 5 : 6) - (r.layout == RS_ROPE_HALF && r.dim < d);
   int lg = 0;
   while (lg < most && (1 << lg) < heads && rows * (d / 16) << lg < (tokens ? 1ll << 31 : 1ll << 19)) ++lg;
   return lg;
@@ -352,7 +353,7 @@ rs_status rope_launch(const rs_rope &rope, const rs_rope_rows &rows, bool transp
     heads += rows.part[k].heads;
   }
   const bool tokens = rows.part[0].sx_h < rows.part[0].sx_t;
-  a.lg = head_groups(rows.n, rows.d, heads, tokens);
+  a.lg = head_groups(rows.n, rows.d, heads, tokens, rope);
   const int per = kThreads / (rows.d / 16) >> a.lg;
   by_shape(rows.dtype, rows.d, rope, tokens, (int64_t)rows.n * heads * rows.d * e, [&](auto t, auto m, auto l, auto n, auto ntl) {
     rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value>
@@ -376,7 +377,7 @@ rs_status append_rope_launch(const CacheView &c, int dtype, int d, const rs_rope
   const int most = max_rows < nrows ? max_rows : nrows;  // rows of a sequence at most
   const int64_t all = (int64_t)c.nseq * most;
   const bool tokens = skh < skt;
-  a.lg = head_groups(all < nrows ? all : nrows, d, c.hkv + a.q.heads, tokens);
+  a.lg = head_groups(all < nrows ? all : nrows, d, c.hkv + a.q.heads, tokens, rope);
   const int per = kThreads / (d / 16) >> a.lg;
   by_shape(dtype, d, rope, tokens, (int64_t)nrows * (2 * c.hkv + a.q.heads) * d * e, [&](auto t, auto m, auto l, auto n, auto ntl) {
     append_rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value>
