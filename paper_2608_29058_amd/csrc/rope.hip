@@ -163,7 +163,7 @@ struct Turner {
         r.x[k][w] = MODE == R_HALF || V * (l + k * LPR) + w * (V / 4) < dim ? y.x[k][w] : r.x[k][w];
   }
   // Rows of one position: heads h0, h0 + step, ... below `end`, N of them loaded before any is stored.  N = 2 (16 registers)
-  // where the heads lie together; apart, one, whose 48 registers leave room for eight waves per SIMD (131072 rows of 32 + 8 heads of
+  // where the heads lie together; apart, one, whose 50 registers leave room for eight waves per SIMD (131072 rows of 32 + 8 heads of
   // 128: 492 us, with four 551).  skip: y is x, and vectors that stay need not move.
   template <int N, bool NTL>
   __device__ __forceinline__ void rows(const char *x, char *y, int64_t sx, int64_t sy, int h0, int step, int end, bool skip) const {
