@@ -54,9 +54,7 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Groups per piece.  The chip works in rounds of `resident` workgroups, so that the time is about that of the rounds' longest pieces
-// and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us).  For each
-// number of rounds the shortest pieces that fit are found; of those, and of whole items, the fastest are taken.
+// Groups per piece, from all lengths.
 __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first, int lane) {
   if (a.slots == 0) return kMaxN;  // one piece each
   auto all = [&](auto f) {  // sum over the sequences
@@ -69,34 +67,10 @@ __device__ __forceinline__ int plan_rounds(const DraftArgs &a, const Seq &first,
   int longest = first.groups;
   for (int b0 = 64; b0 < a.c.nseq; b0 += 64) longest = larger(longest, seq_at<W_CROSS>(a, b0 + lane).groups);
   longest = wave_most(longest);
-  const int fewest = (items + a.resident - 1) / a.resident;
-  int best = kMaxN, cost = fewest * longest * 128;
-  const auto pieces = [&](int per) {
-    const float inv = 1.f / (float)per;  // (quotients of at most 2^11 by at most 2^11: ceil by the product, less half a step)
-    return all([&](const Seq &q) {
-      return items_of<W_CROSS>(a, q) * (q.groups > per ? (int)__builtin_ceilf(((float)q.groups - 0.5f) * inv) : 1);
-    });
-  };
-  for (int r = fewest > 0 ? fewest : 1; r < fewest + 4 && r * a.resident <= a.grid; ++r) {
-    const int room = r * a.resident;
-    int lo = larger((work + room - 1) / room, a.least);
-    if (r * lo * 128 + larger(items, work / lo) >= cost) continue;
-    int n = pieces(lo);
-    if (n > room) {
-      // (an item of n groups has less than n / per + 1 pieces)
-      int hi = room > items ? (work + room - items - 1) / (room - items) : longest;
-      hi = hi < longest ? hi : longest;
-      for (++lo; lo < hi;) {
-        const int per = (lo + hi) >> 1;
-        if (pieces(per) <= room) hi = per;
-        else lo = per + 1;
-      }
-      n = pieces(lo);
-    }
-    const int c = r * lo * 128 + n;
-    if (n <= room && c < cost) cost = c, best = lo;
-  }
-  return best;
+  return rounds_groups(items, work, longest, a.resident, a.grid, a.least, [&](int per) {
+    const float inv = 1.f / (float)per;
+    return all([&](const Seq &q) { return items_of<W_CROSS>(a, q) * pieces_by(q.groups, per, inv); });
+  });
 }
 
 // A tile of the walk: its first state, page, and the states that are seen as bits; j < 0: none.

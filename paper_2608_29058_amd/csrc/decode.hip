@@ -1511,13 +1511,6 @@ struct DraftShape {
 };
 
 constexpr int kShort = 256;
-constexpr int kMaxGrid = 1 << 23;  // workgroups of up to 512 threads, of which a launch has fewer than 2^32
-
-// Row tiles of all sequences at `trows` rows: a sequence has those of its own rows, less than one of them not full.
-int64_t cross_tiles(const CacheView &c, const DraftView &q, int rows, int trows) {
-  const int64_t all = (int64_t)c.nseq * ((rows + trows - 1) / trows), own = (int64_t)(q.hq / c.hkv) * q.nrows / trows + c.nseq;
-  return all < own ? all : own;
-}
 
 // Whether cross attention in bf16 takes the kernel of prompts (cross.hip, 128 rows and two workgroups per CU): where it has
 // full tiles, or enough of them that the stages of the kernels above, which share a tile of rows among more workgroups, gain
@@ -1556,12 +1549,9 @@ DraftShape draft_shape(const CacheView &c, const DraftView &q, bool f32, int d, 
   s.items = items < kMaxGrid ? (int)items : kMaxGrid;
   s.prompt = prompt;
   if (prompt) {  // rounds of workgroups, planned on the device: cross.hip
+    const RoundsShape r = rounds_shape(items, c.cap, resident);
     s.resident = resident;
-    s.least = 4;
-    s.slots = c.cap <= s.least * kGroup || items >= 8 * resident ? 0 : 1;
-    int64_t n = !s.slots ? items : items < resident ? resident : items + 4 * resident;
-    n = n < most ? n : most;
-    s.grid = n < kMaxGrid ? (int)n : kMaxGrid;
+    s.least = r.least, s.slots = r.split, s.grid = r.grid;
     return s;
   }
   // A short cache stays in one piece and needs no joining launch (4 us): up to kShort rows in four waves, twice that in

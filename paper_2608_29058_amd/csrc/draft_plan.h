@@ -4,6 +4,7 @@
 
 #include "common.h"
 #include "cache.h"
+#include "cross_plan.h"
 
 namespace rs {
 
@@ -34,8 +35,6 @@ void cross_join_launch(const DraftArgs &a, int d, int items, hipStream_t st);
 #if defined(__HIPCC__)
 namespace {
 
-constexpr int kTile = 32, kWaves = 4, kGroup = kTile * kWaves;  // rows per wave and step, per workgroup and step
-
 // Wave-uniform loads through the scalar cache of arrays that the kernel does not write.
 __device__ __forceinline__ int uload(const int32_t *p, int64_t i) {
   typedef const __attribute__((address_space(4))) int32_t cint;
@@ -46,9 +45,6 @@ __device__ __forceinline__ int uload(const int32_t *p, int64_t i) {
 // Sequences differ in length, and their lengths are known on the device only.  Every workgroup reads all
 // lengths and derives the same plan: the pieces of every item (sequence, head, row tile) in groups of 128
 // rows, equal to within one, so that all items together make about `slots` pieces.
-
-// Pieces of a sequence of `tiles` groups at `per` groups a piece.
-RS_HD int pieces_of(int tiles, int per) { return tiles > per ? (tiles + per - 1) / per : 1; }
 
 // Rows of keys of sequence b that the kernels walk: cached rows, and drafts where they are seen.
 template <int WHAT>
