@@ -7,6 +7,8 @@ import subprocess
 import numpy as np
 import pytest
 
+from cross_shapes import ITEMS, ROWS
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 SOURCE = r'''
@@ -120,3 +122,10 @@ def test_one_round_is_shared_among_its_workgroups(plan):
             checked += 1
             assert per <= bound, (hq, hkv, lens, rows, per, bound)
     assert checked > 100
+
+
+def test_the_batches_of_the_value_tests_have_several_pieces(plan):
+    """Those that the kernel of prompts takes in tests of the joins."""
+    shapes = ITEMS + ROWS
+    for x, (grid, most, items, per, pieces) in zip(shapes, plan([(hq, hkv, lens, rows) for hq, hkv, d, dtype, lens, rows, extra, hide in shapes])):
+        assert items < pieces <= grid, x
