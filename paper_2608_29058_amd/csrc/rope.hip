@@ -9,6 +9,7 @@
 // the launch.
 #include "rope.h"
 #include "cache.h"
+#include "rope_plan.h"
 
 namespace rs {
 
@@ -72,7 +73,7 @@ struct Raw {
   }
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRopeThreads;
 
 // Neighbouring lanes take neighbouring vectors of a row, LPR apart, so that an instruction moves whole lines (with a lane's 16
 // elements in one piece, 8191 fp32 rows of 32 heads of 64: 57 us; so, 35).  Where the pairs of a row are then:
@@ -260,25 +261,50 @@ struct AppendRopeArgs {
   int nrows, max_rows, lg;
 };
 
-// As rope_kernel, a sequence's rows: heads of K with those of V, then of Q.
-template <typename T, int MODE, int LPR, int N, bool NTL>
+// As rope_kernel, a sequence's rows: heads of K with those of V, then of Q.  BYROW: the rows are the batch's, and each has a
+// sequence of its own, or none.
+template <typename T, int MODE, int LPR, int N, bool NTL, bool BYROW>
 __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeArgs a) {
   __shared__ __align__(16) float tab[kThreads * 16 + Turner<T, MODE, LPR>::kStage];
+  __shared__ uint64_t own[BYROW ? kThreads / LPR : 1];  // sequence and place in it of each row, ~0: none
   const CacheView &c = a.c;
   const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
-  const int b = blockIdx.y, i0 = blockIdx.x * rows, i = i0 + (x >> a.lg);
-  const RowRange rr = new_rows(a.start, b, a.nrows, a.max_rows);
-  if (i0 >= rr.count) return;
-  const int len = cache_len(c, b);
-  const int64_t pos0 = c.seen ? c.seen[b] : len;
-  angle_table<LPR>(tab, a.rope, rows, false, [&](int k) {
-    const int at = i0 + k < rr.count ? i0 + k : rr.count - 1;
-    return (double)(a.pos ? (int64_t)a.pos[rr.first + at] : pos0 + at);
-  });
-  if (i >= rr.count) return;
-  const int64_t row = rr.first + i;
+  const int x0 = blockIdx.x * rows, at = x >> a.lg;
+  int b = blockIdx.y, i = x0 + at, len = 0;
+  int64_t row = i;
+  if constexpr (BYROW) {
+    if ((int)threadIdx.x < rows) own[threadIdx.x] = ~0ull;
+    __syncthreads();
+    for (int s = threadIdx.x; s < c.nseq; s += kThreads) {
+      const RowRange rr = new_rows(a.start, s, a.nrows, a.max_rows);
+      const int first = rr.first > x0 ? rr.first : x0, end = rr.first + rr.count < x0 + rows ? rr.first + rr.count : x0 + rows;
+      for (int r = first; r < end; ++r) own[r - x0] = (uint64_t)s << 32 | (uint32_t)(r - rr.first);
+    }
+    __syncthreads();
+    angle_table<LPR>(tab, a.rope, rows, false, [&](int k) {
+      const uint64_t o = own[k];
+      if (o == ~0ull) return 0.0;
+      const int s = (int)(o >> 32);
+      return (double)(a.pos ? (int64_t)a.pos[x0 + k] : (c.seen ? c.seen[s] : cache_len(c, s)) + (int64_t)(uint32_t)o);
+    });
+    const uint64_t o = own[at];
+    if (o == ~0ull) return;
+    b = (int)(o >> 32), i = (int)(uint32_t)o;
+    len = cache_len(c, b);
+  } else {
+    const RowRange rr = new_rows(a.start, b, a.nrows, a.max_rows);
+    if (x0 >= rr.count) return;
+    len = cache_len(c, b);
+    const int64_t pos0 = c.seen ? c.seen[b] : len;
+    angle_table<LPR>(tab, a.rope, rows, false, [&](int k) {
+      const int y = x0 + k < rr.count ? x0 + k : rr.count - 1;
+      return (double)(a.pos ? (int64_t)a.pos[rr.first + y] : pos0 + y);
+    });
+    if (i >= rr.count) return;
+    row = rr.first + i;
+  }
   Turner<T, MODE, LPR> t(l, a.rope.dim, (char *)(tab + kThreads * 16) + x * LPR * 16 * (int)sizeof(T));
-  t.take(tab + (i - i0) * 16 * LPR);
+  t.take(tab + at * 16 * LPR);
   const int64_t j = (int64_t)len + i;
   const int p = j < c.cap ? page_of(c, (int)j) : 0, id = j < c.cap ? page_id(c, b, p) : -1;
   if (id >= 0) {
@@ -300,19 +326,6 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeA
 
 RopePart part_of(const rs_rope_part &p, int e) {
   return RopePart{(const char *)p.x, (char *)p.y, p.sx_t * e, p.sx_h * e, p.sy_t * e, p.sy_h * e, p.heads, p.x == p.y};
-}
-
-// log2 of the groups of heads that share a row.  Where a token's heads lie together a workgroup takes one row, a head per
-// group, so that it reads and writes long pieces of memory, or two rows where pairs pass through LDS, so that a group has a second
-// head to load meanwhile; where a head's tokens lie together, one group with a row per LPR lanes does, split further only until the rows
-// fill the chip's 2^19 lanes.  (8192 rows of 32 + 2 x 8 heads of 128 appended to four sequences each: one row 133 us, two 133, four 139;
-// 30001 rows of 32 + 8: 96, 97, 101; half of each turned: 131, 104, 105.)  A launch has fewer than 2^32 lanes, which 2^24 rows in groups
-// of their own would pass.
-int head_groups(int64_t rows, int d, int heads, bool tokens, const rs_rope &r) {
-  const int most = (d == 128 ? 5 : 6) - (r.layout == RS_ROPE_HALF && r.dim < d);
-  int lg = 0;
-  while (lg < most && (1 << lg) < heads && rows * (d / 16) << lg < (tokens ? 1ll << 31 : 1ll << 19)) ++lg;
-  return lg;
 }
 
 // f(type, mode, lanes of a row, heads at a time, loads that bypass) of a call over `bytes` of input.
@@ -374,14 +387,16 @@ rs_status append_rope_launch(const CacheView &c, int dtype, int d, const rs_rope
   a.skt = skt * e, a.skh = skh * e, a.svt = svt * e, a.svh = svh * e;
   if (q) a.q = part_of(*q, e);
   a.pos = pos, a.start = start, a.nrows = nrows, a.max_rows = max_rows;
-  const int most = max_rows < nrows ? max_rows : nrows;  // rows of a sequence at most
-  const int64_t all = (int64_t)c.nseq * most;
   const bool tokens = skh < skt;
-  a.lg = head_groups(all < nrows ? all : nrows, d, c.hkv + a.q.heads, tokens, rope);
-  const int per = kThreads / (d / 16) >> a.lg;
+  const AppendShape sh = append_rope_shape(c.nseq, c.cap, nrows, max_rows, start, d, c.hkv, a.q.heads, tokens, rope);
+  a.lg = sh.lg;
+  const dim3 grid((unsigned)sh.x, (unsigned)sh.y);
   by_shape(dtype, d, rope, tokens, (int64_t)nrows * (2 * c.hkv + a.q.heads) * d * e, [&](auto t, auto m, auto l, auto n, auto ntl) {
-    append_rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value>
-        <<<dim3((most + per - 1) / per, c.nseq), kThreads, 0, st>>>(a);
+    auto launch = [&](auto byrow) {
+      append_rope_kernel<decltype(t), decltype(m)::value, decltype(l)::value, decltype(n)::value, decltype(ntl)::value, decltype(byrow)::value>
+          <<<grid, kThreads, 0, st>>>(a);
+    };
+    sh.byrow ? launch(std::true_type{}) : launch(std::false_type{});
   });
   RS_HIP(hipGetLastError());
   return RS_OK;
