@@ -72,6 +72,22 @@ RS_HD RowRange new_rows(const int32_t *start, int b, int nrows, int max_rows) {
   return RowRange{f, e - f < max_rows ? e - f : max_rows};
 }
 
+RS_HD uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
+// Which of the rows j .. j + 31 (j a multiple of 32) of a sequence's `total` a key mask leaves, as bits.  word(w): word w of the
+// sequence's mask, which is asked for only where it has a bit of a row before `total`: behind the end there may be no word.
+template <typename Word>
+RS_HD uint32_t seen_word(int total, int j, Word word) {
+  return j < total ? low_bits(total - j) & word(j >> 5) : 0u;
+}
+
+// The same of the rows j .. j + 63, j < total.
+template <typename Word>
+RS_HD uint64_t seen_words(int total, int j, Word word) {
+  const uint64_t all = total - j >= 64 ? ~0ull : (1ull << (total - j)) - 1;
+  return all & ((uint64_t)word(j >> 5) | (j + 32 < total ? (uint64_t)word((j >> 5) + 1) << 32 : 0ull));
+}
+
 // rs_draft by value: strides in elements.
 struct DraftView {
   const void *q;

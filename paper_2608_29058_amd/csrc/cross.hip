@@ -146,8 +146,8 @@ __device__ __forceinline__ bool cross_walk(const Item &it, const CrossLds<D> &ld
       ok = e >= 0 && e < a->c.npages;
       if constexpr (MASK) {
         const uint32_t *m = a->q.mask + (int64_t)it.b * a->q.nwords;
-        const int w = j >> 5;
-        const uint64_t see = prefix_mask(total - j) & ((uint64_t)m[w] | (w + 1 < a->q.nwords ? (uint64_t)m[w + 1] << 32 : 0ull));
+        const auto word = [&](int w) RS_INLINE { return m[w]; };
+        const uint64_t see = seen_words(total, j, word);
         wlo = (uint32_t)see;
         whi = (uint32_t)(see >> 32);
         ok = ok && see != 0;

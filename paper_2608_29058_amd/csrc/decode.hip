@@ -214,8 +214,6 @@ __device__ __forceinline__ void score_rows(const u32x4 (&k)[D / 32][F32 ? 2 : 1]
   }
 }
 
-__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
-
 // Which of the rows j .. j + 31 of its cache the i-th new row of the sequence sees, as bits: the cached ones,
 // and of the drafted ones those of its mask row, or up to itself.
 __device__ __forceinline__ uint32_t seen_rows(const RowsOf &ro, int i, int j) {
@@ -230,11 +228,10 @@ __device__ __forceinline__ uint32_t seen_rows(const RowsOf &ro, int i, int j) {
   return low_bits(-x) | (drafts & low_bits(ro.total - j));
 }
 
-// W_CROSS: which of the rows j .. j + 31 the sequence's queries see, as bits; j is a multiple of 32.  (Behind the end the mask has
-// no word to read.)
+// W_CROSS: which of the rows j .. j + 31 the sequence's queries see, as bits; j is a multiple of 32.
 __device__ __forceinline__ uint32_t seen_keys(const RowsOf &ro, int j) {
-  const uint32_t all = low_bits(ro.total - j);
-  return ro.q->mask && j < ro.total ? all & (uint32_t)uload((const int32_t *)ro.q->mask, (int64_t)ro.b * ro.q->nwords + (j >> 5)) : all;
+  if (!ro.q->mask) return low_bits(ro.total - j);
+  return seen_word(ro.total, j, [&](int w) { return (uint32_t)uload((const int32_t *)ro.q->mask, (int64_t)ro.b * ro.q->nwords + w); });
 }
 
 // An edge: a tile of 32 rows from row j that some row of Q may not see in whole (drafted rows, the end).  Scores
