@@ -563,7 +563,8 @@ typedef struct rs_cross {
 
 /* O (bf16) and lse as rs_draft_attn writes them, with its arithmetic: rows that see nothing (no states, all hidden) get
  * O = 0 and lse = -inf, hidden states count for nothing whatever they hold, and rows of no sequence are neither read nor written.
- * Of the cache only k, v, table and len are read. */
+ * Of the cache only k, v, table and len are read.  The workspace holds pieces of long caches, up to 128 rows of d + 2
+ * fp32 each: some hundred MB for prompts of hundreds of row tiles. */
 size_t rs_cross_attn_workspace_size(const rs_cache *cache, const rs_cross *cross);
 rs_status rs_cross_attn(const rs_cache *cache, const rs_cross *cross, void *o, int64_t so_t, int64_t so_h, float *lse,
                         void *ws, size_t ws_bytes, rs_stream stream);

@@ -40,7 +40,8 @@ inline RoundsShape rounds_shape(int64_t items, int cap, int resident) {
 }
 
 // Groups per piece.  The chip works in rounds of `resident` workgroups, so that the time is about that of the rounds' longest pieces
-// and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us).  For each
+// and of what pieces write and the join reads: 132 KB each, at 5 TB/s 1/128 of the time of a round's group (3.9 us; heads of 128, and
+// about right for those of 64, which write half and take two thirds).  For each
 // number of rounds the shortest pieces that fit are found; of those, and of whole items, the fastest are taken.  (64 rows of 32 heads of
 // 128 over 3900 states of 8, 496 groups: 31 us, in one piece per item 83.)
 // items, work: items, and their groups in all; longest: groups of the longest; pieces(per): pieces at `per` groups each.
