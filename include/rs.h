@@ -494,7 +494,7 @@ rs_status rs_rope_apply(const rs_rope *rope, const rs_rope_rows *rows, int32_t t
  * cache's dtype, row r the query of the new row r, and q->y (which may be q->x) is what rs_draft_attn then reads.  Row
  * start[b] + i has the position pos[start[b] + i] (a tree's depths, say), or without pos seen[b] + i, or without that
  * len[b] + i.  V enters as it is.  nrows <= 2^24.  Queries of rows behind cap or in no page are rotated all the same; those of rows of no
- * sequence are neither read nor written. */
+ * sequence are neither read nor written.  start ascends: rows that several sequences claim enter the first of them at least. */
 rs_status rs_cache_append_rope(const rs_cache *cache, const rs_rope *rope, const void *k_new, const void *v_new,
                                int64_t sk_t, int64_t sk_h, int64_t sv_t, int64_t sv_h, const rs_rope_part *q,
                                const int32_t *pos, const int32_t *start, int32_t nrows, int32_t max_rows, rs_stream stream);

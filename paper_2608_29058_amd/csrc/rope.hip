@@ -266,7 +266,7 @@ struct AppendRopeArgs {
 template <typename T, int MODE, int LPR, int N, bool NTL, bool BYROW>
 __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeArgs a) {
   __shared__ __align__(16) float tab[kThreads * 16 + Turner<T, MODE, LPR>::kStage];
-  __shared__ uint64_t own[BYROW ? kThreads / LPR : 1];  // sequence and place in it of each row, ~0: none
+  __shared__ unsigned long long own[BYROW ? kThreads / LPR : 1];  // sequence and place in it of each row, ~0: none
   const CacheView &c = a.c;
   const int l = threadIdx.x % LPR, x = threadIdx.x / LPR, groups = 1 << a.lg, g = x & (groups - 1), rows = kThreads / LPR >> a.lg;
   const int x0 = blockIdx.x * rows, at = x >> a.lg;
@@ -278,16 +278,17 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(const AppendRopeA
     for (int s = threadIdx.x; s < c.nseq; s += kThreads) {
       const RowRange rr = new_rows(a.start, s, a.nrows, a.max_rows);
       const int first = rr.first > x0 ? rr.first : x0, end = rr.first + rr.count < x0 + rows ? rr.first + rr.count : x0 + rows;
-      for (int r = first; r < end; ++r) own[r - x0] = (uint64_t)s << 32 | (uint32_t)(r - rr.first);
+      // (a row that several sequences claim, which a start that descends allows, is the first one's)
+      for (int r = first; r < end; ++r) atomicMin(&own[r - x0], (unsigned long long)s << 32 | (uint32_t)(r - rr.first));
     }
     __syncthreads();
     angle_table<LPR>(tab, a.rope, rows, false, [&](int k) {
-      const uint64_t o = own[k];
+      const unsigned long long o = own[k];
       if (o == ~0ull) return 0.0;
       const int s = (int)(o >> 32);
       return (double)(a.pos ? (int64_t)a.pos[x0 + k] : (c.seen ? c.seen[s] : cache_len(c, s)) + (int64_t)(uint32_t)o);
     });
-    const uint64_t o = own[at];
+    const unsigned long long o = own[at];
     if (o == ~0ull) return;
     b = (int)(o >> 32), i = (int)(uint32_t)o;
     len = cache_len(c, b);

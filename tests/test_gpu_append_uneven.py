@@ -104,6 +104,31 @@ def test_absurd_starts_stay_in_bounds():
         compare(s, Rot(128), *batch(8, s), torch.tensor(start, dtype=torch.int32, device="cuda"), ABSURD[5][0])
 
 
+def test_rows_that_several_sequences_claim_enter_the_first():
+    """A start that descends, which the call does not allow: in bounds, and the same every time."""
+    import torch
+    start = [0, 12, 6, 18] + [18, 14] * 148 + [40]
+    assert len(start) == ABSURD[3] + 1
+    s = setup(3, ABSURD, [10, 20, 30, 0, 5], [40], room=20)
+    k, v, q = batch(3, s)
+    rot = Rot(128)
+    st = torch.tensor(start, dtype=torch.int32, device="cuda")
+    rk = torch.empty_like(k)
+    at = torch.arange(s.nrows, dtype=torch.int32, device="cuda") + 10
+    _rs.rs_rope_apply(rot.rope, _rs.RopeRows([(k, rk)], pos=at))
+    was, got = (s.dk.clone(), s.dv.clone()), []
+    for _ in range(5):
+        s.dk.copy_(was[0])
+        s.dv.copy_(was[1])
+        out = torch.full_like(q, -7.0)
+        _rs.rs_cache_append_rope(s.cache(), rot.rope, k, v, q=q, q_out=out, max_rows=ABSURD[5][0], start=st)
+        got.append((s.dk.clone(), s.dv.clone(), out))
+        page = s.table[0, 0]
+        assert torch.equal(bits(s.dk[page, :, 10:22]), bits(rk[:12].transpose(0, 1))) and torch.equal(bits(s.dv[page, :, 10:22]), bits(v[:12].transpose(0, 1)))
+        for a, b in zip(got[0], got[-1]):
+            assert torch.equal(bits(a), bits(b))
+
+
 def test_a_replayed_graph():
     """Starts and lengths as they are at each replay."""
     import torch
